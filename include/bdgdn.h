@@ -489,6 +489,225 @@ int bdgdn_shortconv_bwd_noalloc(const bdgdn_conv_desc_t *desc, const void *x, co
                                 const int32_t *cu_seqlens_dev, const int32_t *cu_seqlens_host, void *dx,
                                 void *dxn, float *dw, float *dbias, void *stream);
 
+/*
+ * ------------------------------------------------------------------------------------
+ * The softmax half of a serving round.  In a hybrid backbone the layers between the Gated
+ * DeltaNet ones attend over a cache of keys and values.  The entry points below serve them
+ * beside bdgdn_denoise_step / bdgdn_commit / bdgdn_commit_record: attention of a block of new
+ * nodes over the cache (bdgdn_tree_attn), the verify decision of an AR-Trust round
+ * (bdgdn_verify), whose counts bdgdn_accept_states takes, and the pages of the cache
+ * (bdgdn_cache_append, _fork, _compact, _truncate).
+ *
+ * The cache.  A pool holds the keys, or the values, of one layer in n_pages pages of `page`
+ * tokens; element e of head h of token t of page p lies at
+ *     p * page_stride + t * token_stride + h * head_stride + e        (elements)
+ * so that [n_pages][page][h_kv][d], [n_pages][h_kv][page][d] and slices of larger arrays are
+ * all pools.  The sequence in slot s has seq_len[s] tokens; token t lies in page
+ * page_table[s][t / page] at place t % page.  Slots are rows of page_table; a `slot` array
+ * [R] names the slot of each request (attention takes NULL for slot[r] = r).
+ * Slot numbers outside [0, n_slots) count as empty sequences; a table entry outside
+ * [0, n_pages) is a page that is not there: its tokens are attended to by nobody.
+ */
+typedef struct {
+    int32_t n_pages;        /* pages of every pool                                        */
+    int32_t page;           /* tokens of a page, 1 .. 65536                               */
+    int32_t n_slots;        /* rows of page_table, entries of seq_len                     */
+    int32_t max_pages;      /* columns of page_table; max_pages * page < 2^31             */
+    int32_t h_kv, d;        /* heads and head dimension of the pools                      */
+    int32_t dtype;          /* bdgdn_dtype_t of the pools                                 */
+    int64_t page_stride, token_stride, head_stride;   /* elements, multiples of 16 bytes */
+} bdgdn_cache_desc_t;
+
+typedef enum {
+    BDGDN_MASK_FULL = 0,    /* every node sees every node (a diffusion block)             */
+    BDGDN_MASK_CAUSAL = 1,  /* node n sees nodes 0 .. n (a chain: anchor and drafts)      */
+    BDGDN_MASK_BITS = 2     /* node n sees node j where bit j of mask[r][n] is set        */
+} bdgdn_mask_t;
+
+typedef struct {
+    int32_t num_req;        /* R                                                          */
+    int32_t nodes;          /* N new nodes per request, 1 .. 64                           */
+    int32_t h_q, h_kv, d;   /* h_q % h_kv == 0; d in {64, 128, 256}                       */
+    float scale;
+    int32_t dtype;          /* bdgdn_dtype_t of q, k, v and the pools                     */
+    int32_t out_dtype;      /* bdgdn_dtype_t of o                                         */
+    int32_t mask;           /* bdgdn_mask_t                                               */
+    int64_t q_stride, k_stride, v_stride;   /* elements between the rows of two nodes, 0 for
+                               contiguous ones; multiples of 16 bytes (q, k, v may be parts
+                               of the rows of one projection)                             */
+} bdgdn_attn_desc_t;
+
+/* Bytes of device workspace bdgdn_tree_attn needs, 0 for descriptors that it rejects. */
+size_t bdgdn_tree_attn_workspace(const bdgdn_attn_desc_t *desc, const bdgdn_cache_desc_t *cache);
+
+/*
+ * Attention of N new nodes per request over the request's cached tokens and over the nodes
+ * themselves.  Node n of request r sees every cached token that is there and the nodes j <
+ * count[r] that the mask lets it see (itself only where the mask says so):
+ *     s_x = scale <q_n, k_x>,  o = sum_x exp(s_x) v_x / sum_x exp(s_x),  lse = log sum_x exp(s_x)
+ * A node that sees nothing, and a node n >= count[r], has o = 0 and lse = -inf.  What a node
+ * does not see has no part in its result, not even a NaN or an infinity.
+ *   q               [R][N][h_q][d] of dtype (head h reads key head h / (h_q / h_kv))
+ *   k, v            [R][N][h_kv][d] of dtype: the nodes' own keys and values
+ *   k_pages, v_pages  pools as described above, 16-byte aligned, of at most 2^36 bytes
+ *   page_table, seq_len   the cache's tables (read only; lengths beyond the table's columns
+ *                   count as max_pages * page)
+ *   slot            [R] int32, or NULL for slot[r] = r (then R <= n_slots)
+ *   count           [R] int32 nodes of each request, or NULL for N
+ *   mask            [R][N] 64-bit words (BDGDN_MASK_BITS), else NULL
+ *   o               [R][N][h_q][d] of out_dtype, every row written
+ *   lse             [R][N][h_q] fp32, or NULL
+ *   workspace       256-byte aligned, owned by the call until the stream passes it
+ * Scores, the softmax's statistics and all sums are fp32.  With bf16 inputs the products are
+ * exact in fp32 and the weights exp(s - m) are rounded to bf16 for the product with v, in two
+ * bf16 parts (16 significant bits) where the output is fp32; their sum, and lse with it, is
+ * that of the unrounded ones.  Results are deterministic.  (dtype, out_dtype) as for the other entry
+ * points: (bf16, bf16), (bf16, fp32), (fp32, fp32).
+ */
+int bdgdn_tree_attn(const bdgdn_attn_desc_t *desc, const bdgdn_cache_desc_t *cache, const void *q,
+                    const void *k, const void *v, const void *k_pages, const void *v_pages,
+                    const int32_t *page_table, const int32_t *seq_len, const int32_t *slot,
+                    const int32_t *count, const uint64_t *mask, void *o, float *lse,
+                    void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The mask words of drafted trees: bit j of mask[r][n] is set for n itself and for its
+ * ancestors.  parent is [R][N] int32 with parent[r][n] < n; any other value makes n a root.
+ * depth ([R][N] int32, or NULL) receives the number of ancestors, by which a node's position
+ * follows the sequence's length.  1 <= nodes <= 64.
+ */
+int bdgdn_tree_mask(int32_t num_req, int32_t nodes, const int32_t *parent, uint64_t *mask,
+                    int32_t *depth, void *stream);
+
+typedef struct {
+    int32_t num_req;        /* R                                                          */
+    int32_t nodes;          /* N nodes: the anchor (node 0) and N - 1 drafts, 1 .. 64     */
+    int32_t vocab;          /* V                                                          */
+    int32_t dtype;          /* bdgdn_dtype_t of target and draft                          */
+    int64_t target_req_stride, target_row_stride;   /* elements; rows are contiguous      */
+    int64_t draft_req_stride, draft_row_stride;
+    int64_t noise_stride;                           /* elements between requests' noise   */
+} bdgdn_verify_desc_t;
+
+/* Bytes of device workspace bdgdn_verify needs, 0 for a descriptor that it rejects. */
+size_t bdgdn_verify_workspace(const bdgdn_verify_desc_t *desc);
+
+/*
+ * Verification of drafted tokens (the exact rejection rule of AR-Trust decoding, for chains
+ * and trees of drafts), with the random numbers given.  Row n of target holds the target's
+ * logits after node n, p = softmax(target / T); row n of draft those that the children of n
+ * were drawn from, q = softmax(draft / T), each child by itself (two children may carry the
+ * same token).  The walk begins at node 0 and tries the children of the node that it is on
+ * in index order.  After j refusals the law of the next token is
+ *     (p - c q)+ / W,   c = 0, W = 1 at first; each refusal: c += W, W = sum (p - c q)+
+ * ((x/W - q)+ = (x - W q)+ / W, so the residuals of all refusals have this form), and the
+ * child with token d is accepted where u W q(d) < (p(d) - c q(d))+.  Without a draft the
+ * proposals are certain (a draft's most likely tokens): a refused token leaves the law, W is
+ * what remains, and d is accepted where u W < p(d).  When no child is accepted the next
+ * token is drawn from the law by the exponential race, argmax_t law(t) / noise(t), the lowest
+ * t of equals (where the law is zero everywhere, p takes its place).
+ *   target       [R][N][V] logits (strides in desc), aligned to an element
+ *   draft        [R][N or N-1][V] logits or NULL (the rows of nodes without children are not
+ *                read, so the last row may be absent)
+ *   token        [R][N] int32: the drafts' tokens (node 0's is not read); a token outside
+ *                [0, V) is refused and leaves the law as it is
+ *   parent       [R][N] int32 with 0 <= parent[r][n] < n for n >= 1 (other values: the node
+ *                is nobody's child), or NULL for chains (parent n - 1)
+ *   count        [R] int32 nodes of each request, or NULL for N
+ *   temperature  [R] fp32, or NULL for 1; T <= 0 (or NaN) is greedy: p is all on the target's
+ *                largest logit, the lowest index of equals, and the draft is not looked at
+ *   u            [R][N] fp32 in [0, 1): u[r][n] decides on node n
+ *   noise        [R][V] fp32 > 0, exponentially distributed (stride in desc)
+ *   n_accept     [R] int32: accepted drafts, the `accept` of bdgdn_accept_states for a chain
+ *                recorded with block N and n_record N - 1
+ *   n_path       [R] int32: n_accept + 1, the nodes of the path (bdgdn_cache_append's count),
+ *                or NULL
+ *   path         [R][N] int32: the path's nodes, node 0 first, then -1
+ *   next_token   [R] int32
+ * A row with a NaN, a +inf or nothing finite has no law: no child of its node is accepted,
+ * and if it is a target's, the next token is -1; so it is for count[r] < 1, with n_accept 0,
+ * n_path 0.
+ * Logits of -inf are tokens of probability zero.  Deterministic.
+ */
+int bdgdn_verify(const bdgdn_verify_desc_t *desc, const void *target, const void *draft,
+                 const int32_t *token, const int32_t *parent, const int32_t *count,
+                 const float *temperature, const float *u, const float *noise, int32_t *n_accept,
+                 int32_t *n_path, int32_t *path, int32_t *next_token, void *workspace,
+                 size_t workspace_bytes, void *stream);
+
+/*
+ * The tables of a cache (device memory).  refcount[p] is the number of table entries that
+ * hold page p; bit p % 32 of free_bits[p / 32] is set where that is zero.  An empty cache has
+ * seq_len and refcount zero and the bits of pages 0 .. n_pages - 1 set, those beyond clear.
+ * Pages are taken lowest first, in the order of the requests, so the tables depend on
+ * nothing but the calls.  The slots of a call must differ (calls with repeated slots race),
+ * and calls on one cache must be ordered by their streams.
+ */
+typedef struct {
+    int32_t *page_table;    /* [n_slots][max_pages]; entries past a sequence's pages are -1 */
+    int32_t *seq_len;       /* [n_slots]                                                    */
+    int32_t *refcount;      /* [n_pages]                                                    */
+    uint32_t *free_bits;    /* [(n_pages + 31) / 32]                                        */
+} bdgdn_cache_tables_t;
+
+/* What a cache call did with a request (status[r]). */
+#define BDGDN_CACHE_DONE     0
+#define BDGDN_CACHE_NO_PAGES 1   /* too few free pages for it, after the requests before it  */
+#define BDGDN_CACHE_NO_ROOM  2   /* more tokens than max_pages * page                        */
+#define BDGDN_CACHE_BAD_SLOT 3   /* a slot outside [0, n_slots); a fork into a slot in use   */
+#define BDGDN_CACHE_BAD_KEEP 4   /* positions to keep that do not rise or are not there      */
+
+/* Bytes of device workspace bdgdn_cache_append (rows_max: the rows that a request may add)
+ * and bdgdn_cache_compact (rows_max: the positions that it may keep) need for num_req
+ * requests, 0 for a descriptor or sizes that they reject. */
+size_t bdgdn_cache_workspace(const bdgdn_cache_desc_t *cache, int32_t num_req, int32_t rows_max);
+
+/*
+ * Appends rows to the sequences in slot[0 .. R-1]: rows path[r][0 .. count[r]-1] of request r
+ * (rows 0 .. count[r]-1 where path is NULL) go behind its last token, in every pool.  A last
+ * page that is not full and is shared with another sequence when the call begins is replaced
+ * by a page of its own with a copy of its tokens (copy on write).
+ *   pools        host array of n_pools device pointers (keys and values of every layer), each
+ *                with the geometry of `cache`, 16-byte aligned
+ *   rows         host array of n_pools device pointers: [R][N][h_kv][d] of the pools' dtype
+ *                with row_stride elements between the rows of two nodes (0: contiguous), the
+ *                k and v that bdgdn_tree_attn took; 16-byte aligned
+ *   path         [R][N] int32 (the path of bdgdn_verify), or NULL; a node outside [0, N)
+ *                gives a row of zeros
+ *   count        [R] int32, 0 .. N (values outside are clamped)
+ *   status       [R] int32, or NULL: what was done; a request that is not done leaves its
+ *                sequence as it was
+ *   workspace    at least bdgdn_cache_workspace(cache, R, N) bytes, 256-byte aligned
+ */
+int bdgdn_cache_append(const bdgdn_cache_desc_t *cache, const bdgdn_cache_tables_t *tables, void *const *pools,
+                       const void *const *rows, int32_t n_pools, int32_t num_req, int32_t nodes,
+                       int64_t row_stride, const int32_t *slot, const int32_t *path, const int32_t *count,
+                       int32_t *status, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Gives slot dst[i] the sequence of src[i] by sharing its pages, i = 0 .. num_req - 1.  The
+ * slots dst must be empty (seq_len 0, else BDGDN_CACHE_BAD_SLOT) and no slot may be both a
+ * source and a destination; a source may be forked many times. */
+int bdgdn_cache_fork(const bdgdn_cache_desc_t *cache, const bdgdn_cache_tables_t *tables, int32_t num_req,
+                     const int32_t *src, const int32_t *dst, int32_t *status, void *stream);
+
+/*
+ * Keeps the positions keep[r][0 .. count[r]-1] (rising, each below the sequence's length) of
+ * slot[r] and drops the others: token j of the sequence is now what token keep[r][j] was, in
+ * every pool.  Leading pages whose tokens all stay where they are are kept (also shared ones);
+ * the tokens behind them move to new pages, and the old ones are given back.  keep is [R][M]
+ * int32, count [R] int32 (values outside 0 .. M are clamped); pools, status and workspace
+ * (bdgdn_cache_workspace(cache, R, M)) as for bdgdn_cache_append.
+ */
+int bdgdn_cache_compact(const bdgdn_cache_desc_t *cache, const bdgdn_cache_tables_t *tables, void *const *pools,
+                        int32_t n_pools, int32_t num_req, int32_t keep_max, const int32_t *slot,
+                        const int32_t *keep, const int32_t *count, int32_t *status, void *workspace,
+                        size_t workspace_bytes, void *stream);
+
+/* Shortens the sequences in slot[0 .. R-1] to min(seq_len, length[r]) tokens (length NULL or
+ * negative: 0, which frees the slot) and gives back the pages that they no longer use. */
+int bdgdn_cache_truncate(const bdgdn_cache_desc_t *cache, const bdgdn_cache_tables_t *tables, int32_t num_req,
+                         const int32_t *slot, const int32_t *length, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

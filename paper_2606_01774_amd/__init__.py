@@ -28,6 +28,10 @@ __all__ = [
     "bdgdn_bwd_train_workspace", "bdgdn_bwd_train_workspace_segmented", "bdgdn_bwd_train",
     "bdgdn_fwd_train_views_workspace", "bdgdn_fwd_train_views",
     "bdgdn_bwd_train_views_workspace", "bdgdn_bwd_train_views", "bdgdn_denoise_step", "bdgdn_commit", "library_path", "load_library", "EXPORTED_SYMBOLS",
+    "BDGDN_MASK_FULL", "BDGDN_MASK_CAUSAL", "BDGDN_MASK_BITS", "BDGDN_CACHE_DONE", "BDGDN_CACHE_NO_PAGES",
+    "BDGDN_CACHE_NO_ROOM", "BDGDN_CACHE_BAD_SLOT", "BDGDN_CACHE_BAD_KEEP", "CacheTables", "make_cache_tables",
+    "bdgdn_tree_attn_workspace", "bdgdn_tree_attn", "bdgdn_tree_mask", "bdgdn_verify_workspace", "bdgdn_verify",
+    "bdgdn_cache_workspace", "bdgdn_cache_append", "bdgdn_cache_fork", "bdgdn_cache_compact", "bdgdn_cache_truncate",
 ]
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -57,7 +61,10 @@ EXPORTED_SYMBOLS = ("bdgdn_version", "bdgdn_status_string", "bdgdn_fwd_train_wor
                     "bdgdn_shortconv_bwd", "bdgdn_bwd_train_workspace", "bdgdn_bwd_train",
                     "bdgdn_fwd_train_views_workspace", "bdgdn_fwd_train_views",
                     "bdgdn_bwd_train_views_workspace", "bdgdn_bwd_train_views",
-                    "bdgdn_shortconv_bwd_noalloc", "bdgdn_bwd_train_workspace_segmented")
+                    "bdgdn_shortconv_bwd_noalloc", "bdgdn_bwd_train_workspace_segmented",
+                    "bdgdn_tree_attn_workspace", "bdgdn_tree_attn", "bdgdn_tree_mask", "bdgdn_verify_workspace",
+                    "bdgdn_verify", "bdgdn_cache_workspace", "bdgdn_cache_append", "bdgdn_cache_fork",
+                    "bdgdn_cache_compact", "bdgdn_cache_truncate")
 
 
 class FwdDesc(ctypes.Structure):
@@ -157,6 +164,7 @@ def load_library():
     lib.bdgdn_shortconv_bwd.restype = ctypes.c_int
     lib.bdgdn_shortconv_bwd_noalloc.argtypes = [ctypes.POINTER(ConvDesc)] + [P] * 13
     lib.bdgdn_shortconv_bwd_noalloc.restype = ctypes.c_int
+    rounds.bind(lib)
     _lib = lib
     return lib
 
@@ -722,3 +730,12 @@ def bdgdn_shortconv_bwd_noalloc(x, xn, w, bias, dy, dyn, *, block, activation=BD
                                          _ptr(dx), _ptr(dxn), _ptr(dw), _ptr(dbias), _stream(stream))
     _check(st, "bdgdn_shortconv_bwd_noalloc")
     return dx, dxn, dw, dbias
+
+
+# ------------------------------------------------------------------ the softmax half of a round
+from . import rounds  # noqa: E402  (its bindings use the helpers above)
+from .rounds import (  # noqa: E402
+    BDGDN_CACHE_BAD_KEEP, BDGDN_CACHE_BAD_SLOT, BDGDN_CACHE_DONE, BDGDN_CACHE_NO_PAGES, BDGDN_CACHE_NO_ROOM,
+    BDGDN_MASK_BITS, BDGDN_MASK_CAUSAL, BDGDN_MASK_FULL, CacheTables, bdgdn_cache_append, bdgdn_cache_compact,
+    bdgdn_cache_fork, bdgdn_cache_truncate, bdgdn_cache_workspace, bdgdn_tree_attn, bdgdn_tree_attn_workspace,
+    bdgdn_tree_mask, bdgdn_verify, bdgdn_verify_workspace, make_cache_tables)

@@ -1,0 +1,87 @@
+// round.hpp -- argument blocks and host-side launchers of the kernels that serve the softmax
+// half of a serving round: attention over a paged cache, verification of drafts, the cache's
+// pages.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace bdgdn {
+
+// ------------------------------------------------------------------ attention (attn_kernels.hip)
+struct AttnArgs {
+    const void *q, *k, *v, *kp, *vp;
+    const int32_t *table, *len, *slot, *count;
+    const uint64_t *mask;
+    void *o;
+    float *lse;
+    float *part_o, *part_ml;   // partial results of the splits: [wave][rows][d], [wave][rows][2]
+    int R, N, h_q, h_kv, G;    // G = h_q / h_kv query heads to a key head
+    int page, max_pages, n_slots, n_pages;
+    int mask_kind;             // bdgdn_mask_t
+    long q_stride, k_stride, v_stride;   // bytes between nodes' rows
+    long head_stride;                    // bytes between a pool's heads
+    uint32_t page16, token16;            // strides of a pool in units of 16 bytes
+    float c;                   // |scale| log2(e), or 1 for scale 0
+    uint32_t q_and, q_xor;     // applied to the words of q: the scale's sign, or zero
+    int RG;                    // groups of rows (of one key head) that different waves take
+    int items;                 // (request, split) pairs that the call aims at
+    int grid;                  // workgroups
+};
+
+// How a call is cut: rows of one wave, row groups, (request, split) pairs at most.
+struct AttnPlan {
+    int mt, RG, items, items_max;
+    size_t part_bytes;
+};
+AttnPlan attn_plan(bool bf16, int d, int R, int N, int h_q, int h_kv);
+hipError_t launch_tree_attn(bool bf16, bool f32_out, int d, const AttnPlan &p, AttnArgs &a, hipStream_t s);
+hipError_t launch_tree_mask(int R, int N, const int32_t *parent, uint64_t *mask, int32_t *depth, hipStream_t s);
+
+// ------------------------------------------------------------------ verification (verify_kernels.hip)
+struct VerifyArgs {
+    const void *target, *draft;
+    const int32_t *token, *parent, *count;
+    const float *temperature, *u, *noise;
+    int32_t *n_accept, *n_path, *path, *next;
+    float *stats;              // [2][R * N][splits][4]: max, sum, index of the max
+    int R, N, V, splits;
+    long t_req, t_row, d_req, d_row, noise_stride;   // elements
+};
+int verify_splits(int R, int N, int V);
+hipError_t launch_verify(bool bf16, const VerifyArgs &a, hipStream_t s);
+
+// ------------------------------------------------------------------ the cache's pages (cache_kernels.hip)
+constexpr int kPoolsPerLaunch = 96;
+
+struct CacheArgs {
+    int32_t *table, *len, *ref;
+    uint32_t *bits;
+    int n_pages, page, n_slots, max_pages;
+    int R, rows_max;           // requests; rows that one may add (append) or keep (compact)
+    const int32_t *slot, *path, *count;   // path: append's path or compact's positions
+    int32_t *status;
+    int32_t *meta, *alloc;     // workspace: kMeta ints per request, then the pages taken
+};
+
+// Per-request words of the workspace.
+enum { kOld = 0, kNew, kCow, kStart, kNeed, kOff, kStay, kMeta = 8 };
+
+struct MoveArgs {
+    CacheArgs c;
+    int n_pools;
+    int row16, head16_log;     // 16-byte chunks of a token's row; log2 of those of a head
+    long page_stride, token_stride, head_stride, row_stride;   // bytes
+    long head_bytes;           // of a head in the rows to append
+    unsigned char *pool[kPoolsPerLaunch];
+    const unsigned char *rows[kPoolsPerLaunch];
+};
+
+size_t cache_workspace(int R, int rows_max, int page);
+hipError_t launch_cache_plan(bool append, const CacheArgs &a, hipStream_t s);
+hipError_t launch_cache_move(bool append, const MoveArgs &a, hipStream_t s);
+hipError_t launch_cache_finish(const CacheArgs &a, hipStream_t s);
+hipError_t launch_cache_fork(const CacheArgs &a, const int32_t *src, const int32_t *dst, hipStream_t s);
+hipError_t launch_cache_truncate(const CacheArgs &a, hipStream_t s);
+
+}  // namespace bdgdn
