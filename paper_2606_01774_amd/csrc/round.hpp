@@ -45,11 +45,18 @@ struct VerifyArgs {
     const float *temperature, *u, *noise;
     int32_t *n_accept, *n_path, *path, *next;
     float *stats;              // [2][R * N][splits][4]: max, sum, index of the max
-    int R, N, V, splits;
+    void *walked, *best;       // the walks' results and the races' parts
+    int R, N, V;
+    int splits, part;          // parts of a row for its statistics, logits of a part
+    int race_splits, race_part;
     long t_req, t_row, d_req, d_row, noise_stride;   // elements
 };
-int verify_splits(int R, int N, int V);
-hipError_t launch_verify(bool bf16, const VerifyArgs &a, hipStream_t s);
+struct VerifyPlan {
+    int splits, part, race_splits, race_part;
+    size_t walked_at, best_at, bytes;   // offsets into the workspace, its size
+};
+VerifyPlan verify_plan(int R, int N, int V);
+hipError_t launch_verify(bool bf16, VerifyArgs &a, const VerifyPlan &p, void *workspace, hipStream_t s);
 
 // ------------------------------------------------------------------ the cache's pages (cache_kernels.hip)
 constexpr int kPoolsPerLaunch = 96;

@@ -195,8 +195,7 @@ int bdgdn_tree_mask(int32_t num_req, int32_t nodes, const int32_t *parent, uint6
 size_t bdgdn_verify_workspace(const bdgdn_verify_desc_t *desc)
 {
     if (check_verify(desc) != BDGDN_OK || desc->num_req == 0) return 0;
-    const size_t bytes = 2 * (size_t)desc->num_req * desc->nodes * verify_splits(desc->num_req, desc->nodes, desc->vocab) * 16;
-    return (bytes + 255) & ~(size_t)255;
+    return verify_plan(desc->num_req, desc->nodes, desc->vocab).bytes;
 }
 
 int bdgdn_verify(const bdgdn_verify_desc_t *desc, const void *target, const void *draft,
@@ -211,19 +210,17 @@ int bdgdn_verify(const bdgdn_verify_desc_t *desc, const void *target, const void
     if (!target || !token || !u || !noise || !n_accept || !path || !next_token) return BDGDN_ERR_INVALID_ARG;
     const size_t size = size_of(desc->dtype);
     if (!aligned(target, size) || !aligned(draft, size) || !aligned(workspace, 256)) return BDGDN_ERR_INVALID_ARG;
-    const size_t need = bdgdn_verify_workspace(desc);
-    if (workspace_bytes < need || !workspace) return BDGDN_ERR_WORKSPACE;
+    const VerifyPlan plan = verify_plan(desc->num_req, desc->nodes, desc->vocab);
+    if (workspace_bytes < plan.bytes || !workspace) return BDGDN_ERR_WORKSPACE;
     VerifyArgs a = {};
     a.target = target; a.draft = draft; a.token = token; a.parent = parent; a.count = count;
     a.temperature = temperature; a.u = u; a.noise = noise;
     a.n_accept = n_accept; a.n_path = n_path; a.path = path; a.next = next_token;
-    a.stats = static_cast<float *>(workspace);
     a.R = desc->num_req; a.N = desc->nodes; a.V = desc->vocab;
-    a.splits = verify_splits(a.R, a.N, a.V);
     a.t_req = desc->target_req_stride; a.t_row = desc->target_row_stride;
     a.d_req = desc->draft_req_stride; a.d_row = desc->draft_row_stride;
     a.noise_stride = desc->noise_stride;
-    return status_of(launch_verify(desc->dtype == BDGDN_BF16, a, static_cast<hipStream_t>(stream)));
+    return status_of(launch_verify(desc->dtype == BDGDN_BF16, a, plan, workspace, static_cast<hipStream_t>(stream)));
 }
 
 size_t bdgdn_cache_workspace(const bdgdn_cache_desc_t *cache, int32_t num_req, int32_t rows_max)

@@ -1,7 +1,13 @@
 // verify_kernels.hip -- verification of drafted tokens against the target's logits from given
-// random numbers.  A first kernel reads every row of logits that a walk may need once and
-// leaves its maximum and its sum of exponentials by parts of the vocabulary; a second one, a
-// workgroup per request, walks the tree and draws the next token by the exponential race.
+// random numbers, in three launches.
+//
+//   stats  (row, part of the vocabulary): reads every row of logits that a walk may need once
+//          and leaves the part's maximum and sum of exponentials, or (greedy requests) the
+//          index of its maximum.  This is where the bytes are.
+//   walk   (request): the rows' laws and every child's odds at once, then the walk itself in
+//          LDS.  Only a refusal with a sibling left reads a row again, for the residual's mass.
+//   race   (request, part): argmax of law(t) / noise(t) over one row; a request's workgroup
+//          that ends last joins the parts.
 #include "common.hpp"
 #include "round.hpp"
 
@@ -11,42 +17,138 @@ namespace {
 
 constexpr int kStatThreads = 256;
 constexpr int kWalkThreads = 1024;
+constexpr int kRaceThreads = 256;
+constexpr int kMaxNodes = 64;
 
-// A part's statistics: maximum, sum of exp2((x - max) k), index of the maximum.
+// Rows of logits begin anywhere: vectors of 16 bytes that are aligned to an element only.
+typedef u32x4 u32x4_e2 __attribute__((aligned(2)));
+typedef u32x4 u32x4_e4 __attribute__((aligned(4)));
+
+template <typename E> struct Vec;
+template <> struct Vec<__bf16> {
+    static constexpr int n = 8;
+    static __device__ __forceinline__ void load(float (&x)[8], const __bf16 *p)
+    {
+        const u32x4 w = *reinterpret_cast<const u32x4_e2 *>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = __uint_as_float(w[i] << 16);
+            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    }
+};
+template <> struct Vec<float> {
+    static constexpr int n = 4;
+    static __device__ __forceinline__ void load(float (&x)[4], const float *p)
+    {
+        const u32x4 w = *reinterpret_cast<const u32x4_e4 *>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(w[i]);
+    }
+};
+
+// A part's statistics: maximum, sum of exp2((x - max) k); greedy requests: maximum, NaN if
+// there is one among the logits and 1 if not, index of the maximum.
 struct Stat {
     float max, sum;
     int arg;
 };
 
-__device__ __forceinline__ float load_logit(const __bf16 *p) { return (float)*p; }
-__device__ __forceinline__ float load_logit(const float *p) { return *p; }
-
-__device__ __forceinline__ Stat join(Stat a, Stat b, float k)
+__device__ __forceinline__ Stat join(Stat a, Stat b, float k, bool greedy)
 {
     Stat r;
     const bool second = b.max > a.max || (b.max == a.max && b.arg < a.arg);
     r.max = second ? b.max : a.max;
     r.arg = second ? b.arg : a.arg;
     const float m = r.max == -INFINITY ? 0.f : r.max;
-    r.sum = a.sum * fexp2((a.max - m) * k) + b.sum * fexp2((b.max - m) * k);
+    r.sum = greedy ? a.sum * b.sum : a.sum * fexp2((a.max - m) * k) + b.sum * fexp2((b.max - m) * k);
     return r;
 }
 
-// log2(e) / T, or log2(e) for a greedy request (its sum only says whether the row has a law).
+// log2(e) / T, or 1 for a greedy request.
 __device__ __forceinline__ float temper(const VerifyArgs &a, int r, bool &greedy)
 {
     const float T = a.temperature ? a.temperature[r] : 1.f;
     greedy = !(T > 0.f);
-    return greedy ? kLog2e : kLog2e / T;
+    return greedy ? 1.f : kLog2e / T;
+}
+
+// Nodes of request r.
+__device__ __forceinline__ int nodes_of(const VerifyArgs &a, int r)
+{
+    return a.count ? min(a.count[r], a.N) : a.N;
+}
+
+// Running statistics of the elements that a thread reads.
+template <bool GREEDY> struct Running {
+    Stat s;
+    __device__ __forceinline__ Running() : s{-INFINITY, GREEDY ? 1.f : 0.f, 0x7fffffff} {}
+    template <int N> __device__ __forceinline__ void add(const float (&x)[N], int v, float k)
+    {
+        if (GREEDY) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                if (x[i] > s.max) {
+                    s.max = x[i];
+                    s.arg = v + i;
+                }
+                if (x[i] != x[i]) s.sum = x[i];
+            }
+        } else {
+            float m = s.max;
+#pragma unroll
+            for (int i = 0; i < N; ++i) m = fmaxf(m, x[i]);
+            const float base = m == -INFINITY ? 0.f : m;
+            s.sum *= fexp2((s.max - base) * k);
+            s.max = m;
+#pragma unroll
+            for (int i = 0; i < N; ++i) s.sum += fexp2((x[i] - base) * k);
+        }
+    }
+};
+
+template <typename E, bool GREEDY>
+__device__ __forceinline__ Stat part_stats(const E *x, int v0, int v1, float k)
+{
+    constexpr int N = Vec<E>::n, U = 4;   // four loads in flight
+    Running<GREEDY> run;
+    int v = v0 + threadIdx.x * N;
+    for (; v + (U - 1) * kStatThreads * N + N <= v1; v += U * kStatThreads * N) {
+        float y[U][N];
+#pragma unroll
+        for (int u = 0; u < U; ++u) Vec<E>::load(y[u], x + v + u * kStatThreads * N);
+        if (GREEDY) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) run.add(y[u], v + u * kStatThreads * N, k);
+        } else {
+            float z[U * N];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < N; ++i) z[u * N + i] = y[u][i];
+            run.add(z, v, k);
+        }
+    }
+    for (; v < v1; v += kStatThreads * N) {
+        float y[N];
+        if (v + N <= v1) {
+            Vec<E>::load(y, x + v);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) y[i] = v + i < v1 ? to_f(x[v + i]) : -INFINITY;
+        }
+        run.add(y, v, k);
+    }
+    return run.s;
 }
 
 template <typename E> __global__ void __launch_bounds__(kStatThreads) bdgdn_verify_stats_kernel(VerifyArgs a)
 {
     __shared__ Stat lds[kStatThreads / 64];
-    const int row = blockIdx.x, rows = a.R * a.N;
+    const int row = blockIdx.x / a.splits, split = blockIdx.x - row * a.splits, rows = a.R * a.N;
     const bool is_draft = row >= rows;
     const int rn = is_draft ? row - rows : row, r = rn / a.N, n = rn - r * a.N;
-    const int count = a.count ? min(a.count[r], a.N) : a.N;
+    const int count = nodes_of(a, r);
     if (n >= count) return;
     bool greedy;
     const float k = temper(a, r, greedy);
@@ -54,7 +156,8 @@ template <typename E> __global__ void __launch_bounds__(kStatThreads) bdgdn_veri
         if (greedy) return;
         bool child = false;
         if (a.parent) {
-            for (int c = n + 1; c < count; ++c) child |= a.parent[r * a.N + c] == n;
+            const int c = threadIdx.x & 63;
+            child = __any(c > n && c < count && a.parent[(long)r * a.N + min(c, a.N - 1)] == n);
         } else {
             child = n + 1 < count;
         }
@@ -62,33 +165,19 @@ template <typename E> __global__ void __launch_bounds__(kStatThreads) bdgdn_veri
     }
     const E *x = is_draft ? static_cast<const E *>(a.draft) + r * a.d_req + n * a.d_row
                           : static_cast<const E *>(a.target) + r * a.t_req + n * a.t_row;
-    const int per = (a.V + a.splits - 1) / a.splits;
-    const int v0 = blockIdx.y * per, v1 = min(v0 + per, a.V);
-    Stat st = {-INFINITY, 0.f, 0x7fffffff};
-    for (int v = v0 + threadIdx.x; v < v1; v += kStatThreads) {
-        const float y = load_logit(x + v);
-        if (y > st.max) {
-            st.sum = st.sum * fexp2((st.max - y) * k) + 1.f;
-            st.max = y;
-            st.arg = v;
-        } else {   // also a NaN, which stays in the sum, and -inf beside -inf, which adds nothing
-            st.sum += y == -INFINITY ? 0.f : fexp2((y - st.max) * k);
-        }
-    }
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int v0 = split * a.part, v1 = min(v0 + a.part, a.V);
+    Stat st = greedy ? part_stats<E, true>(x, v0, v1, k) : part_stats<E, false>(x, v0, v1, k);
 #pragma unroll
     for (int o = 32; o; o >>= 1) {
-        Stat b = {__shfl_xor(st.max, o), __shfl_xor(st.sum, o), __shfl_xor(st.arg, o)};
-        st = join(st, b, k);
+        const Stat b = {__shfl_xor(st.max, o), __shfl_xor(st.sum, o), __shfl_xor(st.arg, o)};
+        st = join(st, b, k, greedy);
     }
-    if (lane == 0) lds[wave] = st;
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = st;
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int w = 1; w < kStatThreads / 64; ++w) st = join(st, lds[w], k);
-        float *p = a.stats + ((long)row * a.splits + blockIdx.y) * 4;
-        p[0] = st.max;
-        p[1] = st.sum;
-        p[2] = __int_as_float(st.arg);
+        for (int w = 1; w < kStatThreads / 64; ++w) st = join(st, lds[w], k, greedy);
+        float *p = a.stats + ((long)row * a.splits + split) * 4;
+        *reinterpret_cast<f32x4 *>(p) = f32x4{st.max, st.sum, __int_as_float(st.arg), 0.f};
     }
 }
 
@@ -96,58 +185,83 @@ template <typename E> __global__ void __launch_bounds__(kStatThreads) bdgdn_veri
 struct Law {
     float max, inv, k;
     int arg;
-    bool ok;
+    __device__ __forceinline__ bool ok() const { return inv > 0.f; }
     __device__ __forceinline__ float at(float x, int v) const
     {
         return k == 0.f ? (v == arg ? inv : 0.f) : fexp2((x - max) * k) * inv;
     }
 };
 
-__device__ Law law_of(const VerifyArgs &a, bool is_draft, int r, int n, float k, bool greedy)
+// Joined by one wave, a part to a lane.
+__device__ __forceinline__ Law law_of(const VerifyArgs &a, long row, float k, bool greedy, int lane)
 {
-    const float *p = a.stats + ((long)((is_draft ? a.R * a.N : 0) + r * a.N + n) * a.splits) * 4;
-    Stat st = {p[0], p[1], __float_as_int(p[2])};
-    for (int s = 1; s < a.splits; ++s) st = join(st, Stat{p[4 * s], p[4 * s + 1], __float_as_int(p[4 * s + 2])}, k);
-    Law l;
-    l.ok = st.sum > 0.f && st.sum < INFINITY && fabsf(st.max) < INFINITY;
-    l.max = st.max;
-    l.arg = st.arg;
-    l.k = greedy ? 0.f : k;
-    l.inv = !l.ok ? 0.f : greedy ? 1.f : 1.f / st.sum;
-    return l;
+    Stat st = {-INFINITY, greedy ? 1.f : 0.f, 0x7fffffff};
+    if (lane < a.splits) {
+        const f32x4 p = *reinterpret_cast<const f32x4 *>(a.stats + (row * a.splits + lane) * 4);
+        st = Stat{p[0], p[1], __float_as_int(p[2])};
+    }
+#pragma unroll
+    for (int o = 32; o; o >>= 1) {
+        const Stat b = {__shfl_xor(st.max, o), __shfl_xor(st.sum, o), __shfl_xor(st.arg, o)};
+        st = join(st, b, k, greedy);
+    }
+    const bool ok = st.sum > 0.f && st.sum < INFINITY && fabsf(st.max) < INFINITY;
+    return Law{st.max, !ok ? 0.f : greedy ? 1.f : 1.f / st.sum, greedy ? 0.f : k, st.arg};
 }
 
-template <typename E> struct Walk {
-    const VerifyArgs &a;
-    const E *t, *d;          // rows of the current node (d null: certain proposals)
+// What the walk leaves for the race.
+struct Walked {
     Law p, q;
-    float c, W;
-    int gone[64], n_gone;    // refused tokens (certain proposals)
+    float c;          // law = (p - c q)+; c 0: q is not looked at
+    int node, n_gone; // node whose row is raced for, refused tokens that are out of the law
+    unsigned done;    // parts of the race that have ended
+    int gone[kMaxNodes];
+};
 
-    __device__ float residual(int v) const
+template <typename E> struct Residual {
+    const E *t, *d;
+    Law p, q;
+    float c;
+    // law of the tokens v .. v + N - 1 from their logits
+    template <int N> __device__ __forceinline__ void of(float (&x)[N], int v, const Walked &w, int n_gone) const
     {
-        const float pv = p.ok ? p.at(load_logit(t + v), v) : 0.f;
-        if (d) return q.ok ? fmaxf(pv - c * q.at(load_logit(d + v), v), 0.f) : pv;
-        for (int i = 0; i < n_gone; ++i)
-            if (gone[i] == v) return 0.f;
-        return pv;
+        if (c > 0.f) {
+            float y[N];
+            if constexpr (N > 1) Vec<E>::load(y, d + v);
+            else y[0] = to_f(d[v]);
+#pragma unroll
+            for (int i = 0; i < N; ++i) x[i] = fmaxf(p.at(x[i], v + i) - c * q.at(y[i], v + i), 0.f);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) x[i] = p.at(x[i], v + i);
+            for (int j = 0; j < n_gone; ++j) {
+                const unsigned at = (unsigned)(w.gone[j] - v);
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    if (at == (unsigned)i) x[i] = 0.f;
+            }
+        }
     }
 };
 
 template <typename E> __global__ void __launch_bounds__(kWalkThreads) bdgdn_verify_walk_kernel(VerifyArgs a)
 {
+    __shared__ Law s_law[2][kMaxNodes];
+    __shared__ float s_p[kMaxNodes], s_q[kMaxNodes], s_u[kMaxNodes];
+    __shared__ int s_parent[kMaxNodes], s_token[kMaxNodes];
     __shared__ float s_sum[kWalkThreads / 64];
-    __shared__ float s_best[2][kWalkThreads / 64];
-    __shared__ int s_at[2][kWalkThreads / 64];
+    __shared__ Walked s_w;
     const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int count = a.count ? min(a.count[r], a.N) : a.N;
-    int32_t *path = a.path + r * a.N;
+    const int count = nodes_of(a, r);
+    int32_t *path = a.path + (long)r * a.N;
+    Walked *out = static_cast<Walked *>(a.walked) + r;
     if (count < 1) {
         for (int n = tid; n < a.N; n += kWalkThreads) path[n] = -1;
         if (tid == 0) {
             a.n_accept[r] = 0;
             if (a.n_path) a.n_path[r] = 0;
             a.next[r] = -1;
+            out->node = -1;
         }
         return;
     }
@@ -156,107 +270,239 @@ template <typename E> __global__ void __launch_bounds__(kWalkThreads) bdgdn_veri
     const bool certain = greedy || !a.draft;
     const E *target = static_cast<const E *>(a.target) + r * a.t_req;
     const E *draft = certain ? nullptr : static_cast<const E *>(a.draft) + r * a.d_req;
-    Walk<E> w = {a, target, nullptr, {}, {}, 0.f, 1.f, {}, 0};
-    int cur = 0, steps = 0;
-    w.p = law_of(a, false, r, 0, k, greedy);
-    bool fresh = true;   // no child of cur has been tried
-    for (int n = 1; n < count; ++n) {
-        if ((a.parent ? a.parent[r * a.N + n] : n - 1) != cur) continue;
-        if (fresh && !certain) {
-            w.d = draft + cur * a.d_row;
-            w.q = law_of(a, true, r, cur, k, false);
+    if (tid < count) {
+        const int p = tid == 0 ? -1 : a.parent ? a.parent[(long)r * a.N + tid] : tid - 1;
+        const int t = tid == 0 ? -1 : a.token[(long)r * a.N + tid];
+        s_parent[tid] = p < tid ? p : -1;
+        s_token[tid] = (unsigned)t < (unsigned)a.V ? t : -1;
+        s_u[tid] = tid == 0 ? 0.f : a.u[(long)r * a.N + tid];
+    }
+    __syncthreads();
+    // every node's law and, where children were drawn from it, its draft's
+    for (int i = wave; i < 2 * count; i += kWalkThreads / 64) {
+        const int n = i >> 1;
+        if (i & 1) {
+            if (certain || !__any(lane > n && lane < count && s_parent[min(lane, count - 1)] == n)) continue;
         }
-        fresh = false;
-        const int tok = a.token[r * a.N + n];
-        const bool in = (unsigned)tok < (unsigned)a.V && (certain || w.q.ok);
-        const float left = in ? w.residual(tok) : 0.f;
-        const float odds = !in ? 0.f : certain ? 1.f : w.q.at(load_logit(w.d + tok), tok);
-        if (in && w.p.ok && a.u[r * a.N + n] * w.W * odds < left) {
+        const Law l = law_of(a, (long)(i & 1 ? a.R * a.N : 0) + (long)r * a.N + n, k, greedy, lane);
+        if (lane == 0) s_law[i & 1][n] = l;
+    }
+    __syncthreads();
+    if (tid < count && s_parent[tid] >= 0 && s_token[tid] >= 0) {
+        const int p = s_parent[tid], t = s_token[tid];
+        s_p[tid] = s_law[0][p].ok() ? s_law[0][p].at(to_f(target[p * a.t_row + t]), t) : 0.f;
+        s_q[tid] = certain ? 1.f : s_law[1][p].at(to_f(draft[p * a.d_row + t]), t);
+    }
+    __syncthreads();
+
+    int cur = 0, steps = 0, n_gone = 0;
+    float c = 0.f, W = 1.f;
+    for (int n = 1; n < count; ++n) {
+        if (s_parent[n] != cur) continue;
+        const int tok = s_token[n];
+        if (tok < 0 || !s_law[0][cur].ok() || (!certain && !s_law[1][cur].ok())) continue;
+        bool out_already = false;
+        for (int i = 0; i < n_gone; ++i) out_already |= s_w.gone[i] == tok;
+        const float left = certain ? (out_already ? 0.f : s_p[n]) : fmaxf(s_p[n] - c * s_q[n], 0.f);
+        if (s_u[n] * W * s_q[n] < left) {
             cur = n;
             ++steps;
             if (tid == 0) path[steps] = n;
-            w.t = target + cur * a.t_row;
-            w.p = law_of(a, false, r, cur, k, greedy);
-            w.d = nullptr;
-            w.c = 0.f;
-            w.W = 1.f;
-            w.n_gone = 0;
-            fresh = true;
+            c = 0.f;
+            W = 1.f;
+            n_gone = 0;
             continue;
         }
-        if (!in) continue;
         if (certain) {
-            w.gone[w.n_gone++] = tok;
+            if (out_already) continue;
+            __syncthreads();
+            if (tid == 0) s_w.gone[n_gone] = tok;
+            ++n_gone;
+            __syncthreads();
         } else {
-            w.c += w.W;
+            c += W;
         }
+        bool more = false;
+        for (int x = n + 1; x < count; ++x) more |= s_parent[x] == cur;
+        if (!more) continue;
+        // the residual's mass.  What is left of certain proposals follows by subtraction as
+        // long as that keeps all but four bits.
+        if (certain && W - left > 0.0625f) {
+            W -= left;
+            continue;
+        }
+        const Residual<E> res = {target + cur * a.t_row, certain ? nullptr : draft + cur * a.d_row, s_law[0][cur],
+                                 certain ? Law{} : s_law[1][cur], c};
+        constexpr int N = Vec<E>::n;
         float sum = 0.f;
-        for (int v = tid; v < a.V; v += kWalkThreads) sum += w.residual(v);
+        const int whole = a.V / N * N;
+        for (int v = tid * N; v < whole; v += kWalkThreads * N) {
+            float x[N];
+            Vec<E>::load(x, res.t + v);
+            res.of(x, v, s_w, n_gone);
+#pragma unroll
+            for (int i = 0; i < N; ++i) sum += x[i];
+        }
+        if (whole + tid < a.V) {
+            float x[1] = {to_f(res.t[whole + tid])};
+            res.of(x, whole + tid, s_w, n_gone);
+            sum += x[0];
+        }
         for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
         if (lane == 0) s_sum[wave] = sum;
         __syncthreads();
-        sum = 0.f;
-        for (int i = 0; i < kWalkThreads / 64; ++i) sum += s_sum[i];
+        W = 0.f;
+        for (int i = 0; i < kWalkThreads / 64; ++i) W += s_sum[i];
         __syncthreads();
-        w.W = sum;
-    }
-    // the race, for the residual and (where that is zero everywhere) for p itself
-    const float *noise = a.noise + r * a.noise_stride;
-    float best[2] = {0.f, 0.f};
-    int at[2] = {-1, -1};
-    if (w.p.ok) {
-        for (int v = tid; v < a.V; v += kWalkThreads) {
-            const float e = noise[v], x = w.residual(v) / e, y = w.p.at(load_logit(w.t + v), v) / e;
-            if (x > best[0]) { best[0] = x; at[0] = v; }
-            if (y > best[1]) { best[1] = y; at[1] = v; }
-        }
-    }
-    for (int i = 0; i < 2; ++i) {
-        for (int o = 32; o; o >>= 1) {
-            const float x = __shfl_xor(best[i], o);
-            const int y = __shfl_xor(at[i], o);
-            if (x > best[i] || (x == best[i] && (unsigned)y < (unsigned)at[i])) { best[i] = x; at[i] = y; }
-        }
-        if (lane == 0) { s_best[i][wave] = best[i]; s_at[i][wave] = at[i]; }
     }
     for (int n = tid; n < a.N; n += kWalkThreads)
         if (n > steps) path[n] = -1;
-    __syncthreads();
+    if (tid < n_gone) out->gone[tid] = s_w.gone[tid];
+    // (an integer comparison of the law's bits: from the one of floats hipcc 7.2 makes a select
+    // on a condition that it has not set)
+    const bool lawful = __builtin_amdgcn_readfirstlane(__float_as_int(s_law[0][cur].inv)) > 0;
     if (tid == 0) {
-        for (int i = 0; i < 2; ++i)
-            for (int j = 1; j < kWalkThreads / 64; ++j)
-                if (s_best[i][j] > best[i] || (s_best[i][j] == best[i] && (unsigned)s_at[i][j] < (unsigned)at[i])) {
-                    best[i] = s_best[i][j];
-                    at[i] = s_at[i][j];
-                }
         path[0] = 0;
         a.n_accept[r] = steps;
         if (a.n_path) a.n_path[r] = steps + 1;
-        a.next[r] = at[0] >= 0 ? at[0] : at[1];
+        out->p = s_law[0][cur];
+        if (c > 0.f) out->q = s_law[1][cur];
+        out->c = c;
+        out->node = lawful ? cur : -1;
+        out->n_gone = n_gone;
+        out->done = 0;
+        if (!lawful) a.next[r] = -1;
     }
 }
+
+struct Best {
+    float score;
+    int at;
+    __device__ __forceinline__ void take(float x, int v)
+    {
+        if (x > score || (x == score && (unsigned)v < (unsigned)at)) {
+            score = x;
+            at = v;
+        }
+    }
+};
+
+__device__ __forceinline__ Best best_of_block(Best b, Best *lds)
+{
+#pragma unroll
+    for (int o = 32; o; o >>= 1) b.take(__shfl_xor(b.score, o), __shfl_xor(b.at, o));
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = b;
+    __syncthreads();
+    b = lds[0];
+    for (int w = 1; w < kRaceThreads / 64; ++w) b.take(lds[w].score, lds[w].at);
+    __syncthreads();
+    return b;
+}
+
+// argmax over [v0, v1) of law / noise, -1 where nothing is above zero.
+template <typename E> __device__ __forceinline__ Best race(const Residual<E> &res, const Walked &w, int n_gone,
+                                                           const float *noise, int v0, int v1)
+{
+    constexpr int N = Vec<E>::n;
+    Best b = {0.f, -1};
+    int v = v0 + threadIdx.x * N;
+    for (; v + N <= v1; v += kRaceThreads * N) {
+        float x[N], e[N];
+        Vec<E>::load(x, res.t + v);
+#pragma unroll
+        for (int i = 0; i < N; i += 4) Vec<float>::load(reinterpret_cast<float(&)[4]>(e[i]), noise + v + i);
+        res.of(x, v, w, n_gone);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float y = x[i] / e[i];
+            if (y > b.score) b = Best{y, v + i};
+        }
+    }
+    for (; v < v1; ++v) {   // the one thread whose vector ends past v1
+        float x[1] = {to_f(res.t[v])};
+        res.of(x, v, w, n_gone);
+        const float y = x[0] / noise[v];
+        if (y > b.score) b = Best{y, v};
+    }
+    return b;
+}
+
+template <typename E> __global__ void __launch_bounds__(kRaceThreads) bdgdn_verify_race_kernel(VerifyArgs a)
+{
+    __shared__ Best lds[kRaceThreads / 64];
+    __shared__ bool s_last;
+    const int r = blockIdx.y, tid = threadIdx.x;
+    Walked *w = static_cast<Walked *>(a.walked) + r;
+    const int node = w->node;
+    if (node < 0) return;   // no law
+    const float *noise = a.noise + r * a.noise_stride;
+    Residual<E> res = {static_cast<const E *>(a.target) + r * a.t_req + node * a.t_row,
+                       static_cast<const E *>(a.draft) + r * a.d_req + node * a.d_row, w->p, w->q, w->c};
+    const int n_gone = w->n_gone;
+    const int v0 = blockIdx.x * a.race_part, v1 = min(v0 + a.race_part, a.V);
+    Best b = best_of_block(race(res, *w, n_gone, noise, v0, v1), lds);
+    Best *parts = static_cast<Best *>(a.best) + (long)r * a.race_splits;
+    if (tid == 0) {
+        __hip_atomic_store(&parts[blockIdx.x].score, b.score, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(&parts[blockIdx.x].at, b.at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        s_last = __hip_atomic_fetch_add(&w->done, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)a.race_splits - 1;
+    }
+    __syncthreads();
+    if (!s_last) return;
+    b = Best{0.f, -1};
+    for (int i = tid; i < a.race_splits; i += kRaceThreads)
+        b.take(__hip_atomic_load(&parts[i].score, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT),
+               __hip_atomic_load(&parts[i].at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+    b = best_of_block(b, lds);
+    if (b.at < 0) {   // nothing is left of the law: p itself
+        res.c = 0.f;
+        b = best_of_block(race(res, *w, 0, noise, 0, a.V), lds);
+    }
+    if (tid == 0) a.next[r] = b.at;
+}
+
+template <typename E> void launch(const VerifyArgs &a, hipStream_t s)
+{
+    bdgdn_verify_stats_kernel<E><<<(a.draft ? 2 : 1) * a.R * a.N * a.splits, kStatThreads, 0, s>>>(a);
+    bdgdn_verify_walk_kernel<E><<<a.R, kWalkThreads, 0, s>>>(a);
+    bdgdn_verify_race_kernel<E><<<dim3(a.race_splits, a.R), kRaceThreads, 0, s>>>(a);
+}
+
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 }  // namespace
 
-// Parts of the vocabulary: enough workgroups for the chip, of 4096 logits at least.
-int verify_splits(int R, int N, int V)
+// Parts of a row: enough workgroups for the chip (2048 hold all its threads), at least 4096
+// logits each and at most 64 of them, a part to a lane of the wave that joins them.
+VerifyPlan verify_plan(int R, int N, int V)
 {
-    const long rows = 2L * R * N;
-    long s = (2048 + rows - 1) / rows;
-    const long most = (V + 4095) / 4096;
-    return (int)(s < 1 ? 1 : s > most ? most : s);
+    const auto cut = [V](long rows, long wanted, int &parts, int &part) {
+        long n = (wanted + rows - 1) / rows;
+        const long most = (V + 4095) / 4096;
+        n = n > most ? most : n;
+        n = n > 64 ? 64 : n < 1 ? 1 : n;
+        part = (int)(((V + n - 1) / n + 7) / 8 * 8);
+        parts = (V + part - 1) / part;
+    };
+    VerifyPlan p;
+    cut(2L * R * N, 2048, p.splits, p.part);
+    cut(R, 1024, p.race_splits, p.race_part);
+    p.walked_at = align256(2 * (size_t)R * N * p.splits * 16);
+    p.best_at = p.walked_at + align256((size_t)R * sizeof(Walked));
+    p.bytes = p.best_at + align256((size_t)R * p.race_splits * sizeof(Best));
+    return p;
 }
 
-hipError_t launch_verify(bool bf16, const VerifyArgs &a, hipStream_t s)
+hipError_t launch_verify(bool bf16, VerifyArgs &a, const VerifyPlan &p, void *workspace, hipStream_t s)
 {
-    const dim3 grid((a.draft ? 2 : 1) * a.R * a.N, a.splits);
-    if (bf16) {
-        bdgdn_verify_stats_kernel<__bf16><<<grid, kStatThreads, 0, s>>>(a);
-        bdgdn_verify_walk_kernel<__bf16><<<a.R, kWalkThreads, 0, s>>>(a);
-    } else {
-        bdgdn_verify_stats_kernel<float><<<grid, kStatThreads, 0, s>>>(a);
-        bdgdn_verify_walk_kernel<float><<<a.R, kWalkThreads, 0, s>>>(a);
-    }
+    char *ws = static_cast<char *>(workspace);
+    a.stats = reinterpret_cast<float *>(ws);
+    a.walked = ws + p.walked_at;
+    a.best = ws + p.best_at;
+    a.splits = p.splits; a.part = p.part;
+    a.race_splits = p.race_splits; a.race_part = p.race_part;
+    if (bf16) launch<__bf16>(a, s);
+    else launch<float>(a, s);
     return hipGetLastError();
 }
 
