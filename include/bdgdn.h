@@ -515,7 +515,8 @@ typedef struct {
     int32_t max_pages;      /* columns of page_table; max_pages * page < 2^31             */
     int32_t h_kv, d;        /* heads and head dimension of the pools                      */
     int32_t dtype;          /* bdgdn_dtype_t of the pools                                 */
-    int64_t page_stride, token_stride, head_stride;   /* elements, multiples of 16 bytes */
+    int64_t page_stride, token_stride, head_stride;   /* elements, multiples of 16 bytes;
+                               a token's at most 2^26 bytes                               */
 } bdgdn_cache_desc_t;
 
 typedef enum {

@@ -29,7 +29,8 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-I" + INCLUDE, 
 # ordinary VGPRs (the compiler's default AGPR form copies every accumulator that VALU code
 # touches in and out of the accumulation registers).
 EXTRA = {"chunked_kernels.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
-         "bwd_scan.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+         "bwd_scan.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+         "attn_kernels.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 
 def _compile(src: str, objdir: str) -> str:

@@ -15,7 +15,8 @@ struct AttnArgs {
     const uint64_t *mask;
     void *o;
     float *lse;
-    float *part_o, *part_ml;   // partial results of the splits: [wave][rows][d], [wave][rows][2]
+    int32_t *info;             // [R][2]: a request's first (request, split) pair and its splits
+    float *part_o, *part_ml;   // the splits' results: [pair][h_kv][rows_padded][d], [..][2]
     int R, N, h_q, h_kv, G;    // G = h_q / h_kv query heads to a key head
     int page, max_pages, n_slots, n_pages;
     int mask_kind;             // bdgdn_mask_t
@@ -24,18 +25,18 @@ struct AttnArgs {
     uint32_t page16, token16;            // strides of a pool in units of 16 bytes
     float c;                   // |scale| log2(e), or 1 for scale 0
     uint32_t q_and, q_xor;     // applied to the words of q: the scale's sign, or zero
-    int RG;                    // groups of rows (of one key head) that different waves take
+    int RW, RG;                // waves of a workgroup, and workgroups, with other rows of a key head
+    int rows_padded;           // rows of a key head, filled up to those of RW x RG waves
     int items;                 // (request, split) pairs that the call aims at
-    int grid;                  // workgroups
 };
 
-// How a call is cut: rows of one wave, row groups, (request, split) pairs at most.
+// How a call is cut: 16-row groups of a wave, the above, workgroups, and the workspace.
 struct AttnPlan {
-    int mt, RG, items, items_max;
-    size_t part_bytes;
+    int mt, RW, RG, rows_padded, items, grid;
+    size_t ml_at, o_at, bytes;
 };
 AttnPlan attn_plan(bool bf16, int d, int R, int N, int h_q, int h_kv);
-hipError_t launch_tree_attn(bool bf16, bool f32_out, int d, const AttnPlan &p, AttnArgs &a, hipStream_t s);
+hipError_t launch_tree_attn(bool bf16, bool f32_out, int d, const AttnPlan &p, AttnArgs &a, void *workspace, hipStream_t s);
 hipError_t launch_tree_mask(int R, int N, const int32_t *parent, uint64_t *mask, int32_t *depth, hipStream_t s);
 
 // ------------------------------------------------------------------ verification (verify_kernels.hip)

@@ -34,7 +34,8 @@ int check_pools(const bdgdn_cache_desc_t *c)
     const int64_t unit = 16 / size_of(c->dtype);
     if (c->page_stride <= 0 || c->token_stride < c->d || c->head_stride < c->d) return BDGDN_ERR_INVALID_ARG;
     if (c->page_stride % unit || c->token_stride % unit || c->head_stride % unit) return BDGDN_ERR_INVALID_ARG;
-    // offsets within a pool count 16-byte units in 32 bits
+    // offsets within a tile of 32 tokens are 32-bit bytes, those within a pool 32-bit 16-byte units
+    if (c->token_stride * size_of(c->dtype) > (1L << 26)) return BDGDN_ERR_UNSUPPORTED;
     const double bytes = ((double)c->n_pages * (double)c->page_stride + (double)c->page * (double)c->token_stride +
                           (double)c->h_kv * (double)c->head_stride) * size_of(c->dtype);
     if (bytes > 68719476736.0) return BDGDN_ERR_UNSUPPORTED;
@@ -136,7 +137,7 @@ extern "C" {
 size_t bdgdn_tree_attn_workspace(const bdgdn_attn_desc_t *desc, const bdgdn_cache_desc_t *cache)
 {
     if (check_attn(desc, cache) != BDGDN_OK || desc->num_req == 0) return 0;
-    return attn_plan(desc->dtype == BDGDN_BF16, desc->d, desc->num_req, desc->nodes, desc->h_q, desc->h_kv).part_bytes;
+    return attn_plan(desc->dtype == BDGDN_BF16, desc->d, desc->num_req, desc->nodes, desc->h_q, desc->h_kv).bytes;
 }
 
 int bdgdn_tree_attn(const bdgdn_attn_desc_t *desc, const bdgdn_cache_desc_t *cache, const void *q,
@@ -157,15 +158,12 @@ int bdgdn_tree_attn(const bdgdn_attn_desc_t *desc, const bdgdn_cache_desc_t *cac
     const bool bf16 = desc->dtype == BDGDN_BF16;
     const AttnPlan p = attn_plan(bf16, desc->d, desc->num_req, desc->nodes, desc->h_q, desc->h_kv);
     if (!aligned(workspace, 256)) return BDGDN_ERR_INVALID_ARG;
-    if (workspace_bytes < p.part_bytes || (p.part_bytes && !workspace)) return BDGDN_ERR_WORKSPACE;
+    if (workspace_bytes < p.bytes || !workspace) return BDGDN_ERR_WORKSPACE;
     const long size = size_of(desc->dtype);
     AttnArgs a = {};
     a.q = q; a.k = k; a.v = v; a.kp = k_pages; a.vp = v_pages;
     a.table = page_table; a.len = seq_len; a.slot = slot; a.count = count; a.mask = mask;
     a.o = o; a.lse = lse;
-    a.part_ml = static_cast<float *>(workspace);
-    const size_t ml = (size_t)p.items_max * desc->h_kv * p.RG * 16 * p.mt * 8;
-    a.part_o = reinterpret_cast<float *>(static_cast<char *>(workspace) + ((ml + 255) & ~(size_t)255));
     a.R = desc->num_req; a.N = desc->nodes; a.h_q = desc->h_q; a.h_kv = desc->h_kv; a.G = desc->h_q / desc->h_kv;
     a.page = cache->page; a.max_pages = cache->max_pages; a.n_slots = cache->n_slots; a.n_pages = cache->n_pages;
     a.mask_kind = desc->mask;
@@ -180,7 +178,8 @@ int bdgdn_tree_attn(const bdgdn_attn_desc_t *desc, const bdgdn_cache_desc_t *cac
     a.c = desc->scale == 0.f ? 1.f : fabsf(desc->scale) * 1.4426950408889634f;
     a.q_and = desc->scale == 0.f ? 0u : ~0u;
     a.q_xor = desc->scale < 0.f ? (bf16 ? 0x80008000u : 0x80000000u) : 0u;
-    return status_of(launch_tree_attn(bf16, desc->out_dtype == BDGDN_F32, desc->d, p, a, static_cast<hipStream_t>(stream)));
+    return status_of(launch_tree_attn(bf16, desc->out_dtype == BDGDN_F32, desc->d, p, a, workspace,
+                                      static_cast<hipStream_t>(stream)));
 }
 
 int bdgdn_tree_mask(int32_t num_req, int32_t nodes, const int32_t *parent, uint64_t *mask, int32_t *depth, void *stream)
