@@ -17,7 +17,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libbdgdn.so")
 SOURCES = ["api.hip", "fwd_kernels.hip", "fwd_scan_kernels.hip", "fused_kernels.hip", "serve_kernels.hip",
            "split_kernels.hip", "conv_kernels.hip", "bwd_kernels.hip", "chunked_kernels.hip",
-           "bwd_generic.hip", "bwd_steps.hip", "bwd_scan.hip", "attn_kernels.hip", "verify_kernels.hip",
+           "bwd_generic.hip", "bwd_steps.hip", "bwd_scan.hip", "attn_kernels.hip", "attn_wide_kernels.hip",
+           "verify_kernels.hip",
            "cache_kernels.hip", "round_api.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-I" + INCLUDE, "-I" + CSRC,
@@ -25,12 +26,13 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-I" + INCLUDE, 
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 
 
-# Per-source extra flags.  The chunk-parallel and the backward scan kernels keep their MFMA accumulators in
+# Per-source extra flags.  The chunk-parallel, the backward scan and the attention kernels keep their MFMA accumulators in
 # ordinary VGPRs (the compiler's default AGPR form copies every accumulator that VALU code
 # touches in and out of the accumulation registers).
 EXTRA = {"chunked_kernels.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
          "bwd_scan.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
-         "attn_kernels.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+         "attn_kernels.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+         "attn_wide_kernels.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 
 def _compile(src: str, objdir: str) -> str:

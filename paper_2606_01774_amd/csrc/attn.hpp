@@ -1,0 +1,546 @@
+// attn.hpp -- attention of a block of nodes over a paged cache: the parts that its kernels share.
+//
+// The rows that share a key head (N nodes x G query heads, M in all) are taken together: 16 MT
+// of them by one wave, 32 keys at a time.  Both
+// products are formed transposed, S^T = K Q^T and O^T = V^T P^T, so that a lane holds one row's
+// scores (row = lane & 15) and the accumulators of the first product are the operand of the
+// second as they stand; the transposed values are made from 16-byte loads by byte permutes.
+#pragma once
+
+#include "common.hpp"
+#include "round.hpp"
+
+namespace bdgdn {
+
+namespace {
+
+constexpr int kTile = 32;          // keys of a step
+constexpr int kMinTiles = 4;       // of a split, at least
+typedef unsigned int u32x2v __attribute__((ext_vector_type(2)));
+
+template <typename T, int D> struct Geo {
+    static constexpr int kRow = D * sizeof(T);          // bytes of a row
+    static constexpr int NK = kRow / 64;                // 16-byte chunks of a key row in a lane
+    static constexpr int VB = kRow < 256 ? 8 : 16;      // bytes of a chunk of a value row in a lane
+    static constexpr int NV = kRow / (16 * VB);         // such chunks
+    static constexpr int EV = VB / sizeof(T);           // elements of such a chunk
+    static constexpr int NT = D / 16;                   // accumulator tiles of a row group
+};
+
+// Tables that a kernel reads at addresses common to a wave, through the scalar cache: such a
+// read is not counted among the vector loads, so waiting for it leaves those in flight.
+typedef __attribute__((address_space(4))) const int32_t *TablePtr;
+
+__device__ __forceinline__ TablePtr table_of(const AttnArgs &a, int r)
+{
+    const int slot = a.slot ? ((TablePtr)(uintptr_t)a.slot)[r] : r;
+    return (TablePtr)(uintptr_t)(a.table + (long)slot * a.max_pages);
+}
+
+__device__ __forceinline__ float max_over_groups(float x)
+{
+    x = fmaxf(x, __shfl_xor(x, 16));
+    return fmaxf(x, __shfl_xor(x, 32));
+}
+
+// What a workgroup works on: a request and one split of its tiles.
+struct Item {
+    int r, split, splits, base;    // base: the request's first (request, split) pair
+    int len, tiles;                // cached tokens and tiles
+    bool valid;
+};
+
+__device__ __forceinline__ int length_of(const AttnArgs &a, int r)
+{
+    const int slot = a.slot ? a.slot[r] : r;
+    if ((unsigned)slot >= (unsigned)a.n_slots) return 0;
+    return min(max(a.len[slot], 0), a.max_pages * a.page);
+}
+
+// The (request, split) pair number `pair`.  A split has the tiles that spread all requests'
+// over the pairs that the call aims at.
+__device__ __forceinline__ Item find_item(const AttnArgs &a, int pair, int lane)
+{
+    const int len0 = lane < a.R ? length_of(a, lane) : 0;
+    int sum = (len0 + kTile - 1) / kTile;
+    for (int r = lane + 64; r < a.R; r += 64) sum += (length_of(a, r) + kTile - 1) / kTile;
+#pragma unroll
+    for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
+    const int per = max(kMinTiles, (sum + a.items - 1) / a.items);
+    Item it = {};
+    int before = 0;
+    for (int r0 = 0; r0 < a.R; r0 += 64) {
+        const int r = r0 + lane;
+        const int len = r0 == 0 ? len0 : r < a.R ? length_of(a, r) : 0;
+        const int tiles = (len + kTile - 1) / kTile;
+        const int n = r < a.R ? max(1, (tiles + per - 1) / per) : 0;
+        int inc = n;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int y = __shfl_up(inc, o);
+            if (lane >= o) inc += y;
+        }
+        const int start = before + inc - n;
+        const unsigned long long hit = __ballot(pair >= start && pair < start + n);
+        if (hit) {
+            const int src = __ffsll(hit) - 1;
+            it.r = r0 + src;
+            it.base = __builtin_amdgcn_readlane(start, src);
+            it.splits = __builtin_amdgcn_readlane(n, src);
+            it.len = __builtin_amdgcn_readlane(len, src);
+            it.tiles = __builtin_amdgcn_readlane(tiles, src);
+            it.split = pair - it.base;
+            it.valid = true;
+            return it;
+        }
+        before += __builtin_amdgcn_readlane(inc, 63);
+    }
+    return it;
+}
+
+// One step of 32 keys for MT groups of 16 rows.
+template <typename T, int D, int MT, bool SPLITP> struct Wave {
+    typedef Geo<T, D> G;
+    u32x4 q[MT][G::NK];
+    f32x4 o[MT][G::NT];
+    float l[MT];           // this lane's share of the weights' sum
+    float m[MT];           // in units of the scaled scores' base-2 exponents
+    float c;
+
+    __device__ __forceinline__ void init(float scale)
+    {
+        c = scale;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            m[i] = -INFINITY;
+            l[i] = 0.f;
+#pragma unroll
+            for (int t = 0; t < G::NT; ++t) o[i][t] = f32x4{0, 0, 0, 0};
+        }
+    }
+
+    // s[mt][half] of lane (g, r): keys 16 half + 4 g + i against row r
+    __device__ __forceinline__ void scores(f32x4 (&s)[MT][2], const u32x4 (&k)[2][G::NK])
+    {
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                f32x4 x = {0, 0, 0, 0};
+#pragma unroll
+                for (int j = 0; j < G::NK; ++j) {
+                    if constexpr (sizeof(T) == 2) {
+                        x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[h][j]),
+                                                                    __builtin_bit_cast(bf16x8, q[mt][j]), x, 0, 0, 0);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            x = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[h][j][i]),
+                                                                     __uint_as_float(q[mt][j][i]), x, 0, 0, 0);
+                    }
+                }
+                s[mt][h] = x;
+            }
+    }
+
+    // keys that are not there: their scores and values
+    __device__ __forceinline__ void hide(f32x4 (&s)[MT][2], u32x4 (&v)[8][G::NV], uint32_t seen, int g)
+    {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (!(seen >> (16 * (e >> 2) + 4 * g + (e & 3)) & 1)) {
+#pragma unroll
+                for (int j = 0; j < G::NV; ++j) v[e][j] = u32x4{0, 0, 0, 0};
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) s[mt][e >> 2][e & 3] = -INFINITY;
+            }
+    }
+
+    // s -> weights exp2(c s - m); the running maximum grows only when a score passes it by
+    // more than 2^8, so that the accumulators are seldom rescaled.
+    __device__ __forceinline__ void weigh(f32x4 (&s)[MT][2])
+    {
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            float top = s[mt][0][0];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) top = fmaxf(top, s[mt][h][i]);
+            top = c * max_over_groups(top);
+            if (__any(top > m[mt] + 8.f)) {
+                const float now = fmaxf(m[mt], top);
+                const float f = m[mt] == -INFINITY ? 0.f : fexp2(m[mt] - now);
+                m[mt] = now;
+                l[mt] *= f;
+#pragma unroll
+                for (int t = 0; t < G::NT; ++t) o[mt][t] *= f;
+            }
+            const float base = m[mt] == -INFINITY ? 0.f : m[mt];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    s[mt][h][i] = fexp2(fmaf(s[mt][h][i], c, -base));
+                    l[mt] += s[mt][h][i];
+                }
+        }
+    }
+
+    // o += V^T P^T; v[e] is the lane's part of value row
+    // 16 (e / 4) + 4 g + e % 4.
+    __device__ __forceinline__ void values(const f32x4 (&p)[MT][2], const u32x4 (&v)[8][G::NV])
+    {
+        if constexpr (sizeof(T) == 2) {
+            bf16x8 hi[MT], lo[MT];
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float x = p[mt][e >> 2][e & 3];
+                    hi[mt][e] = (__bf16)x;
+                    if (SPLITP) lo[mt][e] = (__bf16)(x - (float)hi[mt][e]);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < G::NV; ++j)
+#pragma unroll
+                for (int w = 0; w < G::VB / 4; ++w) {
+                    u32x4 even, odd;
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        even[x] = __builtin_amdgcn_perm(v[2 * x + 1][j][w], v[2 * x][j][w], 0x05040100u);
+                        odd[x] = __builtin_amdgcn_perm(v[2 * x + 1][j][w], v[2 * x][j][w], 0x07060302u);
+                    }
+                    const bf16x8 a0 = __builtin_bit_cast(bf16x8, even), a1 = __builtin_bit_cast(bf16x8, odd);
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) {
+                        f32x4 &o0 = o[mt][j * G::EV + 2 * w], &o1 = o[mt][j * G::EV + 2 * w + 1];
+                        o0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a0, hi[mt], o0, 0, 0, 0);
+                        o1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a1, hi[mt], o1, 0, 0, 0);
+                        if (SPLITP) {
+                            o0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a0, lo[mt], o0, 0, 0, 0);
+                            o1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a1, lo[mt], o1, 0, 0, 0);
+                        }
+                    }
+                }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    const float x = p[mt][e >> 2][e & 3];
+#pragma unroll
+                    for (int j = 0; j < G::NV; ++j)
+#pragma unroll
+                        for (int w = 0; w < 4; ++w)
+                            o[mt][j * 4 + w] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[e][j][w]), x,
+                                                                                    o[mt][j * 4 + w], 0, 0, 0);
+                }
+        }
+    }
+};
+
+template <int NK> __device__ __forceinline__ void load_key(u32x4 (&k)[NK], const unsigned char *row, int g)
+{
+#pragma unroll
+    for (int j = 0; j < NK; ++j) k[j] = *reinterpret_cast<const u32x4 *>(row + 64 * j + 16 * g);
+}
+
+template <int VB, int NV> __device__ __forceinline__ void load_value(u32x4 (&v)[NV], const unsigned char *row, int r)
+{
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        if constexpr (VB == 16) {
+            v[j] = *reinterpret_cast<const u32x4 *>(row + 256 * j + 16 * r);
+        } else {
+            const u32x2v x = *reinterpret_cast<const u32x2v *>(row + 128 * j + 8 * r);
+            v[j] = u32x4{x[0], x[1], 0, 0};
+        }
+    }
+}
+
+template <int N> __device__ __forceinline__ void zero(u32x4 (&x)[N])
+{
+#pragma unroll
+    for (int j = 0; j < N; ++j) x[j] = u32x4{0, 0, 0, 0};
+}
+
+// tok / page.
+__device__ __forceinline__ int column(const AttnArgs &a, int tok)
+{
+    return a.page_mul ? (int)(__umulhi((unsigned)tok, a.page_mul) >> a.page_shift) : tok;
+}
+
+// Where the keys of a tile of cached tokens lie.  HALVES: a page holds whole runs of 16
+// tokens, so a tile is two base addresses; otherwise lane x finds key x & 31 and the others
+// ask it.  A key that is not there reads the pool's first tokens instead and is left out by
+// `seen`.
+template <bool HALVES> struct Tiles {
+    const AttnArgs &a;
+    TablePtr table;
+    const unsigned char *kp, *vp;
+    int len, lane;
+    uint32_t at[2];       // HALVES: of the halves' first tokens, else of this lane's, in 16 bytes
+    uint32_t seen;        // keys that are there
+    int pages[2];         // the next tile's, ahead of its use
+
+    __device__ __forceinline__ Tiles(const AttnArgs &args, int r, int kvh, int len_, int lane_) : a(args), len(len_), lane(lane_)
+    {
+        table = table_of(a, r);
+        kp = static_cast<const unsigned char *>(a.kp) + (long)kvh * a.head_stride;
+        vp = static_cast<const unsigned char *>(a.vp) + (long)kvh * a.head_stride;
+    }
+    __device__ __forceinline__ void look_up(int t)
+    {
+        if (HALVES) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) pages[h] = t * kTile + 16 * h < len ? table[column(a, t * kTile + 16 * h)] : -1;
+        } else {
+            const int tok = t * kTile + (lane & 31);
+            pages[0] = tok < len ? ((const int32_t *)(uintptr_t)table)[column(a, tok)] : -1;
+        }
+    }
+    __device__ __forceinline__ bool place(int tok, int page, uint32_t &where) const
+    {
+        const bool there = (unsigned)page < (unsigned)a.n_pages;
+        where = there ? page * a.page16 + (uint32_t)(tok - column(a, tok) * a.page) * a.token16 : 0;
+        return there;
+    }
+    // on to the tile that was looked up
+    __device__ __forceinline__ void go(int t)
+    {
+        if (HALVES) {
+            seen = 0;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int tok = t * kTile + 16 * h, left = len - tok;
+                if (place(tok, pages[h], at[h])) seen |= (left >= 16 ? 0xffffu : (1u << left) - 1) << (16 * h);
+            }
+        } else {
+            seen = (uint32_t)__ballot(place(t * kTile + (lane & 31), pages[0], at[0]));
+        }
+    }
+    __device__ __forceinline__ const unsigned char *row(const unsigned char *p, int h, int i, int lane_key) const
+    {
+        // key 16 h + i + lane_key, of which 16 h + i is the same for all lanes
+        if (HALVES) return p + (long)at[h] * 16 + (long)(i * a.token16) * 16 + (uint32_t)(lane_key * a.token16 * 16);
+        return p + (long)__shfl(at[0], 16 * h + i + lane_key) * 16;
+    }
+    template <int NK> __device__ __forceinline__ void keys(u32x4 (&k)[2][NK], int g, int rr) const
+    {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) load_key(k[h], row(kp, h, 0, rr), g);
+    }
+    template <int VB, int NV> __device__ __forceinline__ void values(u32x4 (&v)[8][NV], int g, int rr) const
+    {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) load_value<VB>(v[e], row(vp, e >> 2, e & 3, 4 * g), rr);
+    }
+};
+
+__device__ __forceinline__ bool finite_words(u32x4 x, bool wide)
+{
+    bool ok = true;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        ok &= wide ? (x[i] & 0x7f800000u) != 0x7f800000u
+                   : (x[i] & 0x7f80u) != 0x7f80u && (x[i] & 0x7f800000u) != 0x7f800000u;
+    return ok;
+}
+
+// Infinities and NaNs of a word of values set to zero.
+__device__ __forceinline__ uint32_t finite_part(uint32_t x, bool wide)
+{
+    if (wide) return (x & 0x7f800000u) == 0x7f800000u ? 0u : x;
+    const uint32_t lo = (x & 0x7f80u) == 0x7f80u ? 0u : x & 0xffffu;
+    return lo | ((x & 0x7f800000u) == 0x7f800000u ? 0u : x & 0xffff0000u);
+}
+
+// The queries of a wave's 16 MT rows from row0 on, and the nodes that they belong to.
+template <typename T, int D, int MT, bool SPLITP>
+__device__ __forceinline__ void load_rows(Wave<T, D, MT, SPLITP> &w, const AttnArgs &a, int r, int kvh, int row0, int (&node)[MT],
+                                          int g, int rr)
+{
+    typedef Geo<T, D> G;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+        const int row = min(row0 + mt * 16 + rr, a.N * a.G - 1);
+        node[mt] = row / a.G;
+        load_key(w.q[mt], static_cast<const unsigned char *>(a.q) + ((long)r * a.N + node[mt]) * a.q_stride +
+                              (long)(kvh * a.G + row - node[mt] * a.G) * G::kRow, g);
+    }
+}
+
+template <typename T, int D, int MT, bool SPLITP> __device__ __forceinline__ void sign_rows(Wave<T, D, MT, SPLITP> &w, const AttnArgs &a)
+{
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int j = 0; j < Geo<T, D>::NK; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w.q[mt][j][i] = (w.q[mt][j][i] & a.q_and) ^ a.q_xor;
+}
+
+// The nodes themselves as keys and values, for the rows of one wave.
+template <typename T, int D, int MT, bool SPLITP>
+__device__ __forceinline__ void attend_nodes(Wave<T, D, MT, SPLITP> &w, const AttnArgs &a, int r, int kvh, int count,
+                                             const int (&node)[MT], int g, int rr)
+{
+    typedef Geo<T, D> G;
+    u32x4 k[2][G::NK], v[8][G::NV];
+    const unsigned char *kn = static_cast<const unsigned char *>(a.k) + (long)r * a.N * a.k_stride + (long)kvh * G::kRow;
+    const unsigned char *vn = static_cast<const unsigned char *>(a.v) + (long)r * a.N * a.v_stride + (long)kvh * G::kRow;
+    const uint64_t live = count >= 64 ? ~0ull : (1ull << count) - 1;
+    uint64_t sees[MT];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+        sees[mt] = live;
+        if (a.mask_kind == 1) sees[mt] &= node[mt] == 63 ? ~0ull : (1ull << (node[mt] + 1)) - 1;
+        if (a.mask_kind == 2) sees[mt] &= a.mask[(long)r * a.N + node[mt]];
+    }
+    for (int n0 = 0; n0 < count; n0 += kTile) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) load_key(k[h], kn + min(n0 + 16 * h + rr, count - 1) * a.k_stride, g);
+        bool fine = true;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int key = n0 + 16 * (e >> 2) + 4 * g + (e & 3);
+            if (key < count) load_value<G::VB>(v[e], vn + key * a.v_stride, rr);
+            else zero(v[e]);
+#pragma unroll
+            for (int j = 0; j < G::NV; ++j) fine &= finite_words(v[e][j], sizeof(T) == 4);
+        }
+        f32x4 s[MT][2];
+        w.scores(s, k);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (!(sees[mt] >> (n0 + 16 * (e >> 2) + 4 * g + (e & 3)) & 1)) s[mt][e >> 2][e & 3] = -INFINITY;
+        w.weigh(s);
+        if (__any(!fine)) {
+            // Values that are not finite: a weight of zero does not take them out of a
+            // product, so they are left out of it and added where they are seen.
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+#pragma unroll
+                for (int j = 0; j < G::NV; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[e][j][i] = finite_part(v[e][j][i], sizeof(T) == 4);
+        }
+        w.values(s, v);
+        if (__any(!fine)) {
+            for (int x = 0; x < kTile && n0 + x < count; ++x) {
+                const T *row = reinterpret_cast<const T *>(vn + (n0 + x) * a.v_stride);
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    // (every weight of a lane is asked for, so that none is held by a varying index)
+                    const int from = ((x & 15) >> 2) * 16 + rr;
+                    float p = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float pe = __shfl(s[mt][e >> 2][e & 3], from);
+                        if (e == (x >> 4) * 4 + (x & 3)) p = pe;
+                    }
+                    if (sees[mt] >> (n0 + x) & 1) {
+#pragma unroll
+                        for (int j = 0; j < G::NV; ++j)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                                for (int e = 0; e < G::EV; ++e) {
+                                    const float y = to_f(row[j * 16 * G::EV + (4 * g + i) * G::EV + e]);
+                                    if (!(fabsf(y) < INFINITY)) w.o[mt][j * G::EV + e][i] += p * y;
+                                }
+                    }
+                }
+            }
+        }
+    }
+}
+
+// Waves with the same rows (RW apart, KW of them) joined two by two; the first of them holds
+// the result.  s_o and s_ml have room for KW / 2 * RW waves.
+template <typename T, int D, int MT, bool SPLITP>
+__device__ __forceinline__ void join_waves(Wave<T, D, MT, SPLITP> &w, f32x4 (*s_o)[Geo<T, D>::NT][64], float (*s_ml)[2][64],
+                                           int kw, int rw, int KW, int RW, int lane)
+{
+    typedef Geo<T, D> G;
+    for (int step = KW >> 1; step; step >>= 1) {
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            const int at = (kw & (step - 1)) * RW + rw;
+            if (kw >= step && kw < 2 * step) {
+                s_ml[at][0][lane] = w.m[mt];
+                s_ml[at][1][lane] = w.l[mt];
+#pragma unroll
+                for (int t = 0; t < G::NT; ++t) s_o[at][t][lane] = w.o[mt][t];
+            }
+            __syncthreads();
+            if (kw < step) {
+                const float m = s_ml[at][0][lane], top = fmaxf(w.m[mt], m), base = top == -INFINITY ? 0.f : top;
+                const float f0 = fexp2(w.m[mt] - base), f1 = fexp2(m - base);
+                w.m[mt] = top;
+                w.l[mt] = w.l[mt] * f0 + s_ml[at][1][lane] * f1;
+#pragma unroll
+                for (int t = 0; t < G::NT; ++t) w.o[mt][t] = w.o[mt][t] * f0 + s_o[at][t][lane] * f1;
+            }
+            __syncthreads();
+        }
+    }
+}
+
+// The rows of one wave: the result where the request has one split, else the split's part.
+template <typename Out, typename T, int D, int MT, bool SPLITP>
+__device__ __forceinline__ void write_rows(const Wave<T, D, MT, SPLITP> &w, const AttnArgs &a, const Item &it, int pair, int kvh,
+                                           int count, int row0, const int (&node)[MT], int g, int rr)
+{
+    typedef Geo<T, D> G;
+    const int r = it.r, M = a.N * a.G;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+        const int row = row0 + mt * 16 + rr;
+        float sum = w.l[mt];
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        if (row >= M) continue;
+        if (it.splits == 1) {   // the result
+            const bool none = node[mt] >= count || sum == 0.f;
+            const float inv = none ? 0.f : 1.f / sum;
+            const long at = ((long)r * a.N + node[mt]) * a.h_q + kvh * a.G + row - node[mt] * a.G;
+            Out *out = static_cast<Out *>(a.o) + at * D;
+#pragma unroll
+            for (int j = 0; j < G::NV; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    Out *p = out + j * 16 * G::EV + (4 * g + i) * G::EV;
+                    float y[G::EV];
+#pragma unroll
+                    for (int e = 0; e < G::EV; ++e) y[e] = none ? 0.f : w.o[mt][j * G::EV + e][i] * inv;
+#pragma unroll
+                    for (int e = 0; e < G::EV; e += 4) st4(p + e, y[e], y[e + 1], y[e + 2], y[e + 3]);
+                }
+            if (a.lse && g == 0) a.lse[at] = none ? -INFINITY : (w.m[mt] + __log2f(sum)) * 0.6931471805599453f;
+        } else {                // the split's part: rows of [d] and (maximum, sum)
+            const long at = ((long)pair * a.h_kv + kvh) * a.rows_padded + row;
+            float *po = a.part_o + at * D;
+            if (g == 0) {
+                a.part_ml[2 * at] = w.m[mt];
+                a.part_ml[2 * at + 1] = sum;
+            }
+#pragma unroll
+            for (int j = 0; j < G::NV; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int e = 0; e < G::EV; e += 4)
+                        st4(po + j * 16 * G::EV + (4 * g + i) * G::EV + e, w.o[mt][j * G::EV + e][i], w.o[mt][j * G::EV + e + 1][i],
+                            w.o[mt][j * G::EV + e + 2][i], w.o[mt][j * G::EV + e + 3][i]);
+        }
+    }
+}
+
+}  // namespace
+
+}  // namespace bdgdn

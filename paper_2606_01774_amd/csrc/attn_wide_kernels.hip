@@ -1,0 +1,205 @@
+// attn_wide_kernels.hip -- attention of a block of nodes over a paged cache: the kernel for many
+// rows to a key head (bf16, pages of whole runs of 16 tokens).
+//
+// Eight waves (four with heads of 256) are a workgroup of RW x KW: RW waves have 32 rows each and
+// read the same tiles, KW take different tiles.  Tiles go from memory to LDS without passing
+// through registers, S stages deep, one barrier a stage; a stage is KW tiles of 32 keys and
+// values.  A row of D elements is D / 8 chunks of 16 bytes; chunk c of key x lies at place
+// c ^ (x & 15) of its row (c ^ (x / 2 & 7) in rows of 8 chunks), so that the 16 lanes that read one chunk of
+// 16 keys, and those that read 16 chunks of one key, meet different banks.
+#include <mutex>
+#include <type_traits>
+
+#include "attn.hpp"
+
+namespace bdgdn {
+
+namespace {
+
+typedef __attribute__((address_space(1))) const void *GlobalPtr;
+typedef __attribute__((address_space(3))) void *LdsPtr;
+
+constexpr int waves_of(int d) { return d == 256 ? 4 : 8; }   // of a workgroup
+
+template <int D, int RW> struct Wide {
+    static constexpr int CH = D / 8;                    // chunks of a row
+    static constexpr int W = waves_of(D);
+    static constexpr int KW = W / RW;
+    static constexpr int STAGE = KW * 64 * CH;          // chunks of a stage: KW x (keys, values) x 32 rows
+    static constexpr int LOADS = CH / RW;               // of a wave for a stage, 64 chunks each
+    static constexpr int S = STAGE * 16 >= 65536 ? 2 : STAGE * 16 >= 32768 ? 4 : 6;
+    static constexpr int JOIN = (KW / 2) * RW * (D / 16 * 1024 + 512);
+    static constexpr int LDS = S * STAGE * 16 > JOIN ? S * STAGE * 16 : JOIN;
+    static __device__ __forceinline__ int place(int c, int key) { return c ^ (CH == 8 ? (key >> 1) & 7 : key & 15); }
+};
+
+template <int N> __device__ __forceinline__ void wait_loads_barrier()
+{
+    // the memory clobber keeps reads and writes of LDS on their side of the barrier
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+template <int D, int RW, bool SPLITP, typename Out>
+__global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) bdgdn_tree_attn_wide_kernel(AttnArgs a)
+{
+    typedef __bf16 T;
+    typedef Geo<T, D> G;
+    typedef Wide<D, RW> X;
+    constexpr int CH = X::CH, KW = X::KW, S = X::S, LOADS = X::LOADS, ROWS = 64 / CH;   // rows of one load
+    extern __shared__ u32x4 lds[];
+    __shared__ uint32_t s_seen[S][KW][2];
+    const int lane = threadIdx.x & 63, g = lane >> 4, rr = lane & 15;
+    const int wave = wave_id(), kw = wave / RW, rw = wave % RW;
+    // workgroups with the same keys and other rows are neighbours on one XCD (their numbers
+    // are equal modulo 8)
+    const int x = blockIdx.x & 7, y = blockIdx.x >> 3;
+    const int unit = y / a.RG * 8 + x, rg = y % a.RG;
+    const int pair = unit / a.h_kv, kvh = unit - pair * a.h_kv;
+    const Item it = find_item(a, pair, lane);
+    if (!it.valid) return;
+    const int r = it.r;
+    const int count = a.count ? min(max(a.count[r], 0), a.N) : a.N;
+    if (it.split == 0 && kvh == 0 && rg == 0 && threadIdx.x == 0) {
+        a.info[2 * r] = it.base;
+        a.info[2 * r + 1] = it.splits;
+    }
+    const int t0 = (int)((long)it.tiles * it.split / it.splits), t1 = (int)((long)it.tiles * (it.split + 1) / it.splits);
+    const int n = (t1 - t0 + KW - 1) / KW;   // stages
+
+    // this wave's share of a stage: rows [first, first + LOADS ROWS) of the keys or the values of one tile
+    const int block = wave * LOADS, lkw = block / CH, first = block % (CH / 2) * ROWS;
+    const bool is_value = block / (CH / 2) & 1;
+    const TablePtr table = table_of(a, r);
+    const unsigned char *pool = static_cast<const unsigned char *>(is_value ? a.vp : a.kp) + (long)kvh * a.head_stride;
+    uint32_t off[LOADS];
+#pragma unroll
+    for (int l = 0; l < LOADS; ++l) {
+        const int key = first + l * ROWS + lane / CH;
+        off[l] = (key & 15) * a.token16 * 16 + X::place(lane % CH, key) * 16;
+    }
+    int pages[2];
+    const auto look_up = [&](int i) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int t = t0 + i * KW + lkw, tok = t * kTile + 16 * h;
+            pages[h] = t < t1 && tok < it.len ? table[column(a, tok)] : -1;
+        }
+    };
+    const auto request = [&](int i) {
+        const int tok0 = (t0 + i * KW + lkw) * kTile;
+        const int buf = i % S;
+        const unsigned char *at[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int tok = tok0 + 16 * h;
+            const bool there = (unsigned)pages[h] < (unsigned)a.n_pages;
+            const uint32_t where = there ? pages[h] * a.page16 + (uint32_t)(tok - column(a, tok) * a.page) * a.token16 : 0;
+            at[h] = pool + (long)where * 16;
+            if (!is_value && lane == 0)
+                s_seen[buf][lkw][h] = !there ? 0u : it.len - tok >= 16 ? 0xffffu : (1u << (it.len - tok)) - 1;
+        }
+#pragma unroll
+        for (int l = 0; l < LOADS; ++l) {
+            const unsigned char *p = at[(first + l * ROWS) >> 4] + off[l];
+            __builtin_amdgcn_global_load_lds((GlobalPtr)p, (LdsPtr)&lds[buf * X::STAGE + (block + l) * 64], 16, 0, 0);
+        }
+    };
+    if (n > 0) look_up(0);
+    Wave<T, D, 2, SPLITP> w;
+    w.init(a.c);
+    const int row0 = (rg * RW + rw) * 32;   // of this wave's rows
+    int node[2];
+    load_rows(w, a, r, kvh, row0, node, g, rr);
+    sign_rows(w, a);
+#pragma unroll
+    for (int i = 0; i < S - 1; ++i)
+        if (i < n) {
+            request(i);
+            if (i + 1 < n) look_up(i + 1);
+        }
+
+    // where this lane's chunks of keys and values lie in a tile
+    int ko[G::NK], vo[4];
+#pragma unroll
+    for (int j = 0; j < G::NK; ++j) ko[j] = rr * CH + X::place(4 * j + g, rr);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) vo[i] = CH == 8 ? ((4 * g + i) * CH + X::place(rr >> 1, 4 * g + i)) * 16 + (rr & 1) * 8
+                                                : ((4 * g + i) * CH + X::place(rr, 4 * g + i)) * 16;
+    int buf = 0;
+    for (int i = 0; i < n; ++i) {
+        if (n - 1 - i >= S - 2) wait_loads_barrier<(S - 2) * LOADS>();
+        else wait_loads_barrier<0>();
+        if (i + S - 1 < n) {
+            request(i + S - 1);
+            if (i + S < n) look_up(i + S);
+        }
+        const uint32_t seen = __builtin_amdgcn_readfirstlane(s_seen[buf][kw][0] | s_seen[buf][kw][1] << 16);
+        const u32x4 *kt = lds + buf * X::STAGE + kw * 64 * CH;
+        const unsigned char *vt = reinterpret_cast<const unsigned char *>(kt + 32 * CH);
+        buf = buf + 1 == S ? 0 : buf + 1;
+        if (!seen) continue;
+        u32x4 k[2][G::NK], v[8][G::NV];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < G::NK; ++j) k[h][j] = kt[16 * h * CH + ko[j]];
+        f32x4 s[2][2];
+        w.scores(s, k);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+            for (int j = 0; j < G::NV; ++j) {
+                const unsigned char *p = vt + (e >> 2) * 16 * CH * 16 + vo[e & 3] + 256 * j;
+                if constexpr (CH == 8) {
+                    const u32x2v z = *reinterpret_cast<const u32x2v *>(p);
+                    v[e][j] = u32x4{z[0], z[1], 0, 0};
+                } else {
+                    v[e][j] = *reinterpret_cast<const u32x4 *>(p);
+                }
+            }
+        if (seen != ~0u) w.hide(s, v, seen, g);
+        w.weigh(s);
+        w.values(s, v);
+    }
+    if (it.split == it.splits - 1 && kw == KW - 1) attend_nodes(w, a, r, kvh, count, node, g, rr);
+    if constexpr (KW > 1) {
+        __syncthreads();   // the stages are read: their memory is free
+        f32x4(*s_o)[G::NT][64] = reinterpret_cast<f32x4(*)[G::NT][64]>(lds);
+        float(*s_ml)[2][64] = reinterpret_cast<float(*)[2][64]>(lds + (KW / 2) * RW * G::NT * 64);
+        join_waves(w, s_o, s_ml, kw, rw, KW, RW, lane);
+    }
+    if (kw == 0) write_rows<Out>(w, a, it, pair, kvh, count, row0, node, g, rr);
+}
+
+template <int D, int RW, bool SPLITP, typename Out> hipError_t launch(int grid, const AttnArgs &a, hipStream_t s)
+{
+    typedef Wide<D, RW> X;
+    static std::once_flag once;
+    static hipError_t err;
+    const auto kernel = bdgdn_tree_attn_wide_kernel<D, RW, SPLITP, Out>;
+    std::call_once(once, [&] {
+        err = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, X::LDS);
+    });
+    if (err != hipSuccess) return err;
+    kernel<<<grid, 64 * X::W, X::LDS, s>>>(a);
+    return hipGetLastError();
+}
+
+template <int D, bool SPLITP, typename Out> hipError_t launch_rw(int grid, const AttnArgs &a, hipStream_t s)
+{
+    if (a.RW == 2) return launch<D, 2, SPLITP, Out>(grid, a, s);
+    if constexpr (D < 256)
+        if (a.RW == 8) return launch<D, 8, SPLITP, Out>(grid, a, s);
+    return launch<D, 4, SPLITP, Out>(grid, a, s);
+}
+
+}  // namespace
+
+hipError_t launch_tree_attn_wide(bool f32_out, int d, int grid, const AttnArgs &a, hipStream_t s)
+{
+#define BDGDN_WIDE(D) (f32_out ? launch_rw<D, true, float>(grid, a, s) : launch_rw<D, false, __bf16>(grid, a, s))
+    return d == 64 ? BDGDN_WIDE(64) : d == 128 ? BDGDN_WIDE(128) : BDGDN_WIDE(256);
+#undef BDGDN_WIDE
+}
+
+}  // namespace bdgdn

@@ -19,6 +19,8 @@ struct AttnArgs {
     float *part_o, *part_ml;   // the splits' results: [pair][h_kv][rows_padded][d], [..][2]
     int R, N, h_q, h_kv, G;    // G = h_q / h_kv query heads to a key head
     int page, max_pages, n_slots, n_pages;
+    uint32_t page_mul;         // tok / page = mulhi(tok, page_mul) >> page_shift, or tok for 0 (pages of one)
+    int page_shift;
     int mask_kind;             // bdgdn_mask_t
     long q_stride, k_stride, v_stride;   // bytes between nodes' rows
     long head_stride;                    // bytes between a pool's heads
@@ -32,11 +34,13 @@ struct AttnArgs {
 
 // How a call is cut: 16-row groups of a wave, the above, workgroups, and the workspace.
 struct AttnPlan {
+    bool wide;                 // the kernel that stages tiles in LDS
     int mt, RW, RG, rows_padded, items, grid;
     size_t ml_at, o_at, bytes;
 };
-AttnPlan attn_plan(bool bf16, int d, int R, int N, int h_q, int h_kv);
+AttnPlan attn_plan(bool bf16, int d, int page, int R, int N, int h_q, int h_kv);
 hipError_t launch_tree_attn(bool bf16, bool f32_out, int d, const AttnPlan &p, AttnArgs &a, void *workspace, hipStream_t s);
+hipError_t launch_tree_attn_wide(bool f32_out, int d, int grid, const AttnArgs &a, hipStream_t s);
 hipError_t launch_tree_mask(int R, int N, const int32_t *parent, uint64_t *mask, int32_t *depth, hipStream_t s);
 
 // ------------------------------------------------------------------ verification (verify_kernels.hip)

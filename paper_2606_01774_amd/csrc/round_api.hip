@@ -137,7 +137,7 @@ extern "C" {
 size_t bdgdn_tree_attn_workspace(const bdgdn_attn_desc_t *desc, const bdgdn_cache_desc_t *cache)
 {
     if (check_attn(desc, cache) != BDGDN_OK || desc->num_req == 0) return 0;
-    return attn_plan(desc->dtype == BDGDN_BF16, desc->d, desc->num_req, desc->nodes, desc->h_q, desc->h_kv).bytes;
+    return attn_plan(desc->dtype == BDGDN_BF16, desc->d, cache->page, desc->num_req, desc->nodes, desc->h_q, desc->h_kv).bytes;
 }
 
 int bdgdn_tree_attn(const bdgdn_attn_desc_t *desc, const bdgdn_cache_desc_t *cache, const void *q,
@@ -156,7 +156,7 @@ int bdgdn_tree_attn(const bdgdn_attn_desc_t *desc, const bdgdn_cache_desc_t *cac
         !aligned(o, 16) || !aligned(mask, 8))
         return BDGDN_ERR_INVALID_ARG;
     const bool bf16 = desc->dtype == BDGDN_BF16;
-    const AttnPlan p = attn_plan(bf16, desc->d, desc->num_req, desc->nodes, desc->h_q, desc->h_kv);
+    const AttnPlan p = attn_plan(bf16, desc->d, cache->page, desc->num_req, desc->nodes, desc->h_q, desc->h_kv);
     if (!aligned(workspace, 256)) return BDGDN_ERR_INVALID_ARG;
     if (workspace_bytes < p.bytes || !workspace) return BDGDN_ERR_WORKSPACE;
     const long size = size_of(desc->dtype);
@@ -166,6 +166,14 @@ int bdgdn_tree_attn(const bdgdn_attn_desc_t *desc, const bdgdn_cache_desc_t *cac
     a.o = o; a.lse = lse;
     a.R = desc->num_req; a.N = desc->nodes; a.h_q = desc->h_q; a.h_kv = desc->h_kv; a.G = desc->h_q / desc->h_kv;
     a.page = cache->page; a.max_pages = cache->max_pages; a.n_slots = cache->n_slots; a.n_pages = cache->n_pages;
+    // tok / page for tok < 2^31: with 2^(l-1) < page <= 2^l, m = ceil(2^(31+l) / page) < 2^32 and
+    // tok m >> (31 + l) is exact (m page - 2^(31+l) < 2^l)
+    if (cache->page > 1) {
+        int l = 1;
+        while ((1 << l) < cache->page) ++l;
+        a.page_mul = (uint32_t)(((1ull << (31 + l)) + cache->page - 1) / cache->page);
+        a.page_shift = l - 1;
+    }
     a.mask_kind = desc->mask;
     a.q_stride = (desc->q_stride ? desc->q_stride : (int64_t)desc->h_q * desc->d) * size;
     a.k_stride = (desc->k_stride ? desc->k_stride : (int64_t)desc->h_kv * desc->d) * size;

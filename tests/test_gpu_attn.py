@@ -122,6 +122,17 @@ def _compare(c, out, mask, scale, dtype, out_dtype, count=None):
     (1, 40, 2, 2, 64, 5, [44], "f32", "f32", "full", False),
     (5, 2, 32, 8, 128, 64, [64, 63, 65, 2000, 1], "bf16", "bf16", "causal", False),
     (70, 1, 2, 1, 64, 16, [(37 * i) % 90 for i in range(70)], "bf16", "bf16", "full", False),
+    # many rows to a key head: each number of row waves and head size, one tile to many stages
+    (2, 12, 8, 2, 64, 16, [5, 300], "bf16", "bf16", "tree", False),
+    (2, 25, 8, 2, 64, 48, [1100, 16], "bf16", "f32", "causal", True),
+    (1, 50, 4, 1, 64, 64, [777], "bf16", "bf16", "full", False),
+    (3, 10, 6, 1, 128, 32, [0, 31, 1500], "bf16", "f32", "tree", True),
+    (2, 32, 8, 2, 128, 64, [2049, 95], "bf16", "bf16", "full", False),
+    (1, 64, 16, 2, 128, 16, [1000], "bf16", "bf16", "causal", False),
+    (2, 9, 4, 1, 256, 32, [40, 650], "bf16", "f32", "full", False),
+    (2, 30, 8, 2, 256, 64, [129, 512], "bf16", "bf16", "causal", True),
+    (1, 64, 6, 1, 256, 16, [333], "bf16", "bf16", "tree", False),
+    (1, 37, 3, 1, 128, 128, [4000], "bf16", "f32", "full", False),
 ])
 def test_against_the_definition(R, N, h_q, h_kv, d, page, lens, dtype, out, mask, htd):
     c = _case(R, N, h_q, h_kv, d, page, lens, dtype, htd=htd, seed=R + N + d, slots=list(range(R, 0, -1)))
@@ -154,11 +165,11 @@ def test_scores_that_grow_and_scores_far_apart():
     _compare(c, got, "full", 1 / math.sqrt(128), "bf16", "f32")
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("page", [16, 32])
-def test_nothing_unseen_enters(dtype, page):
+@pytest.mark.parametrize("dtype,h_q", [("bf16", 4), ("f32", 4), ("bf16", 16)])
+@pytest.mark.parametrize("page", [16, 32, 20])
+def test_nothing_unseen_enters(dtype, h_q, page):
     """Stale places, pages that are not there, refused nodes: NaN and infinities in all of them."""
-    c = _case(3, 6, 4, 2, 64, page, [5 * page + 3, 0, 2 * page], dtype, seed=9, max_pages=7)
+    c = _case(3, 6, h_q, 2, 64, page, [5 * page + 3, 0, 2 * page], dtype, seed=9, max_pages=7)
     t = c["table"]
     for pool in (c["kp"], c["vp"]):
         used = torch.zeros(pool.shape[:2], dtype=torch.bool, device="cuda")
@@ -182,10 +193,10 @@ def test_nothing_unseen_enters(dtype, page):
     assert torch.isinf(got[1][1, 0]).all() and torch.isinf(got[1][1, 4]).all()   # rows that see nothing
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_what_is_seen_is_not_hidden(dtype):
+@pytest.mark.parametrize("dtype,page", [("bf16", 32), ("f32", 32), ("bf16", 20)])
+def test_what_is_seen_is_not_hidden(dtype, page):
     """A node's NaN reaches the rows that see it, in its element alone, and no other row."""
-    c = _case(1, 40, 2, 1, 128, 32, [45], dtype, seed=2)
+    c = _case(1, 40, 2, 1, 128, page, [45], dtype, seed=2)
     c["v"][0, 3, 0, 17] = float("nan")
     c["v"][0, 35, 0, 99] = float("inf")
     o, lse = bd.bdgdn_tree_attn(c["q"], c["k"], c["v"], c["kp"], c["vp"], c["table"], c["seq"], mask="causal",
