@@ -15,7 +15,6 @@ namespace bdgdn {
 namespace {
 
 constexpr int kTile = 32;          // keys of a step
-constexpr int kMinTiles = 4;       // of a split, at least
 typedef unsigned int u32x2v __attribute__((ext_vector_type(2)));
 
 template <typename T, int D> struct Geo {
@@ -26,6 +25,25 @@ template <typename T, int D> struct Geo {
     static constexpr int EV = VB / sizeof(T);           // elements of such a chunk
     static constexpr int NT = D / 16;                   // accumulator tiles of a row group
 };
+
+// The lane's number, as new to the compiler: what follows from it is worked out again in each
+// turn of a loop, not once before it and kept in registers that the loop needs.
+__device__ __forceinline__ int lane_anew()
+{
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    return lane;
+}
+
+// Registers without a value that nothing has to be kept for (a variable that is set under a
+// condition in a loop would otherwise hold the last turn's).
+template <int M, int N> __device__ __forceinline__ void undefine(u32x4 (&x)[M][N])
+{
+#pragma unroll
+    for (int i = 0; i < M; ++i)
+#pragma unroll
+        for (int j = 0; j < N; ++j) asm volatile("" : "=v"(x[i][j]));
+}
 
 // Tables that a kernel reads at addresses common to a wave, through the scalar cache: such a
 // read is not counted among the vector loads, so waiting for it leaves those in flight.
@@ -39,15 +57,21 @@ __device__ __forceinline__ TablePtr table_of(const AttnArgs &a, int r)
 
 __device__ __forceinline__ float max_over_groups(float x)
 {
-    x = fmaxf(x, __shfl_xor(x, 16));
-    return fmaxf(x, __shfl_xor(x, 32));
+    // the swaps leave a value and its partner's in the two results
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
-// What a workgroup works on: a request and one split of its tiles.
-struct Item {
-    int r, split, splits, base;    // base: the request's first (request, split) pair
-    int len, tiles;                // cached tokens and tiles
-    bool valid;
+// The keys of all requests in one row, a request's cached tiles followed by its nodes (which
+// count as one tile), are cut into equal ranges, one to a workgroup (of each key head and row
+// group), whatever the requests' lengths.  A range holds the end of one request, whole ones and
+// the beginning of another.
+struct Range {
+    int pos, end;              // what is left of the range
+    int size;                  // of every range
+    int r, off, len, tiles;    // the request at pos, its tile there, its cached tokens and tiles
 };
 
 __device__ __forceinline__ int length_of(const AttnArgs &a, int r)
@@ -57,23 +81,28 @@ __device__ __forceinline__ int length_of(const AttnArgs &a, int r)
     return min(max(a.len[slot], 0), a.max_pages * a.page);
 }
 
-// The (request, split) pair number `pair`.  A split has the tiles that spread all requests'
-// over the pairs that the call aims at.
-__device__ __forceinline__ Item find_item(const AttnArgs &a, int pair, int lane)
+__device__ __forceinline__ int tiles_of(int len) { return (len + kTile - 1) / kTile; }
+
+__device__ __forceinline__ Range find_range(const AttnArgs &a, int w, int lane)
 {
     const int len0 = lane < a.R ? length_of(a, lane) : 0;
-    int sum = (len0 + kTile - 1) / kTile;
-    for (int r = lane + 64; r < a.R; r += 64) sum += (length_of(a, r) + kTile - 1) / kTile;
+    int sum = lane < a.R ? tiles_of(len0) + 1 : 0;
+    for (int r = lane + 64; r < a.R; r += 64) sum += tiles_of(length_of(a, r)) + 1;
 #pragma unroll
     for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
-    const int per = max(kMinTiles, (sum + a.items - 1) / a.items);
-    Item it = {};
+    sum = __builtin_amdgcn_readfirstlane(sum);
+    Range g = {};
+    g.size = max(a.least, (sum + a.ranges - 1) / a.ranges);
+    // (in 64 bits: ranges past the end may lie beyond 2^31)
+    const long pos = (long)w * g.size;
+    if (pos >= sum) return g;
+    g.pos = (int)pos;
+    g.end = (int)min(pos + g.size, (long)sum);
     int before = 0;
     for (int r0 = 0; r0 < a.R; r0 += 64) {
         const int r = r0 + lane;
         const int len = r0 == 0 ? len0 : r < a.R ? length_of(a, r) : 0;
-        const int tiles = (len + kTile - 1) / kTile;
-        const int n = r < a.R ? max(1, (tiles + per - 1) / per) : 0;
+        const int n = r < a.R ? tiles_of(len) + 1 : 0;
         int inc = n;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
@@ -81,21 +110,57 @@ __device__ __forceinline__ Item find_item(const AttnArgs &a, int pair, int lane)
             if (lane >= o) inc += y;
         }
         const int start = before + inc - n;
-        const unsigned long long hit = __ballot(pair >= start && pair < start + n);
+        const unsigned long long hit = __ballot(g.pos >= start && g.pos < start + n);
         if (hit) {
             const int src = __ffsll(hit) - 1;
-            it.r = r0 + src;
-            it.base = __builtin_amdgcn_readlane(start, src);
-            it.splits = __builtin_amdgcn_readlane(n, src);
-            it.len = __builtin_amdgcn_readlane(len, src);
-            it.tiles = __builtin_amdgcn_readlane(tiles, src);
-            it.split = pair - it.base;
-            it.valid = true;
-            return it;
+            g.r = r0 + src;
+            g.off = g.pos - __builtin_amdgcn_readlane(start, src);
+            g.len = __builtin_amdgcn_readlane(len, src);
+            g.tiles = tiles_of(g.len);
+            return g;
         }
         before += __builtin_amdgcn_readlane(inc, 63);
     }
-    return it;
+    return g;
+}
+
+// What a workgroup does with one request: tiles t0 .. t1 - 1, the nodes where `nodes`.
+struct Piece {
+    int r, len, t0, t1;
+    bool nodes, whole;         // whole: the request's only piece
+    int part;                  // else its place among the parts: 2 w for a range's first piece, 2 w + 1
+};
+
+__device__ __forceinline__ Piece piece_of(const Range &g, int w)
+{
+    Piece p;
+    const int n = min(g.tiles + 1 - g.off, g.end - g.pos);
+    p.r = g.r;
+    p.len = g.len;
+    p.t0 = g.off;
+    p.nodes = g.off + n == g.tiles + 1;
+    p.t1 = p.nodes ? g.tiles : g.off + n;
+    p.whole = p.nodes && g.off == 0;
+    p.part = 2 * w + (g.pos != (long)w * g.size);
+    return p;
+}
+
+__device__ __forceinline__ void next_piece(const AttnArgs &a, Range &g)
+{
+    g.pos += min(g.tiles + 1 - g.off, g.end - g.pos);
+    if (g.pos >= g.end) return;
+    ++g.r;
+    g.off = 0;
+    g.len = __builtin_amdgcn_readfirstlane(length_of(a, g.r));
+    g.tiles = tiles_of(g.len);
+}
+
+// What the joining kernel needs to know of a request that a range begins.
+__device__ __forceinline__ void note_request(const AttnArgs &a, const Range &g)
+{
+    a.info[1 + 2 * g.r] = g.pos;
+    a.info[2 + 2 * g.r] = g.tiles + 1;
+    if (g.pos == 0) a.info[0] = g.size;
 }
 
 // One step of 32 keys for MT groups of 16 rows.
@@ -260,12 +325,6 @@ template <int VB, int NV> __device__ __forceinline__ void load_value(u32x4 (&v)[
     }
 }
 
-template <int N> __device__ __forceinline__ void zero(u32x4 (&x)[N])
-{
-#pragma unroll
-    for (int j = 0; j < N; ++j) x[j] = u32x4{0, 0, 0, 0};
-}
-
 // tok / page.
 __device__ __forceinline__ int column(const AttnArgs &a, int tok)
 {
@@ -406,10 +465,13 @@ __device__ __forceinline__ void attend_nodes(Wave<T, D, MT, SPLITP> &w, const At
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const int key = n0 + 16 * (e >> 2) + 4 * g + (e & 3);
-            if (key < count) load_value<G::VB>(v[e], vn + key * a.v_stride, rr);
-            else zero(v[e]);
+            load_value<G::VB>(v[e], vn + min(key, count - 1) * a.v_stride, rr);
+            const uint32_t live_bits = key < count ? ~0u : 0u;
 #pragma unroll
-            for (int j = 0; j < G::NV; ++j) fine &= finite_words(v[e][j], sizeof(T) == 4);
+            for (int j = 0; j < G::NV; ++j) {
+                v[e][j] &= live_bits;
+                fine &= finite_words(v[e][j], sizeof(T) == 4);
+            }
         }
         f32x4 s[MT][2];
         w.scores(s, k);
@@ -491,9 +553,9 @@ __device__ __forceinline__ void join_waves(Wave<T, D, MT, SPLITP> &w, f32x4 (*s_
     }
 }
 
-// The rows of one wave: the result where the request has one split, else the split's part.
+// The rows of one wave: the result where the request is one piece, else the piece's part.
 template <typename Out, typename T, int D, int MT, bool SPLITP>
-__device__ __forceinline__ void write_rows(const Wave<T, D, MT, SPLITP> &w, const AttnArgs &a, const Item &it, int pair, int kvh,
+__device__ __forceinline__ void write_rows(const Wave<T, D, MT, SPLITP> &w, const AttnArgs &a, const Piece &it, int kvh,
                                            int count, int row0, const int (&node)[MT], int g, int rr)
 {
     typedef Geo<T, D> G;
@@ -505,7 +567,7 @@ __device__ __forceinline__ void write_rows(const Wave<T, D, MT, SPLITP> &w, cons
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
         if (row >= M) continue;
-        if (it.splits == 1) {   // the result
+        if (it.whole) {          // the result
             const bool none = node[mt] >= count || sum == 0.f;
             const float inv = none ? 0.f : 1.f / sum;
             const long at = ((long)r * a.N + node[mt]) * a.h_q + kvh * a.G + row - node[mt] * a.G;
@@ -522,8 +584,8 @@ __device__ __forceinline__ void write_rows(const Wave<T, D, MT, SPLITP> &w, cons
                     for (int e = 0; e < G::EV; e += 4) st4(p + e, y[e], y[e + 1], y[e + 2], y[e + 3]);
                 }
             if (a.lse && g == 0) a.lse[at] = none ? -INFINITY : (w.m[mt] + __log2f(sum)) * 0.6931471805599453f;
-        } else {                // the split's part: rows of [d] and (maximum, sum)
-            const long at = ((long)pair * a.h_kv + kvh) * a.rows_padded + row;
+        } else {                // rows of [d] and (maximum, sum)
+            const long at = ((long)it.part * a.h_kv + kvh) * a.rows_padded + row;
             float *po = a.part_o + at * D;
             if (g == 0) {
                 a.part_ml[2 * at] = w.m[mt];

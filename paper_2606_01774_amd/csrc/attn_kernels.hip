@@ -4,9 +4,9 @@
 // One wave streams its tiles from memory to registers, the next keys requested when the scores
 // are done with these and the next values when the output is.  Four waves are a workgroup:
 // those with different rows take the same keys, those with the same rows every KW-th tile,
-// and are joined through LDS.  The keys of a request are cut into as many splits as fill the
-// chip, balanced over requests of different lengths; where a request has more than one, a
-// second kernel joins the splits' (maximum, sum, output).
+// and are joined through LDS.  The keys of all requests are cut into equal ranges, as many as
+// the chip holds workgroups (attn.hpp), so that it is busy to the end whatever the requests'
+// lengths; a second kernel joins (maximum, sum, output) of requests in several ranges.
 #include <type_traits>
 
 #include "attn.hpp"
@@ -17,80 +17,85 @@ namespace {
 
 constexpr int kWaves = 4;          // of a workgroup
 
+// Waves of a SIMD that a kernel's registers allow (two of up to 256, one of more).
+constexpr int waves_per_simd(bool bf16, int d, int mt) { return bf16 ? (mt * d <= 256 && d < 256 ? 2 : 1) : d == 64 ? 2 : 1; }
+
 template <typename T, int D, int MT, bool SPLITP, bool HALVES, typename Out>
-__global__ void __launch_bounds__(64 * kWaves) bdgdn_tree_attn_kernel(AttnArgs a)
+__global__ void __launch_bounds__(64 * kWaves, waves_per_simd(sizeof(T) == 2, D, MT)) bdgdn_tree_attn_kernel(AttnArgs a)
 {
     typedef Geo<T, D> G;
     __shared__ f32x4 s_o[2][G::NT][64];
     __shared__ float s_ml[2][2][64];
-    const int lane = threadIdx.x & 63, g = lane >> 4, rr = lane & 15;
     const int wave = wave_id(), kw = wave / a.RW, rw = wave - kw * a.RW, KW = kWaves / a.RW;
     // workgroups with the same keys and other rows are neighbours on one XCD (their numbers
     // are equal modulo 8)
     const int x = blockIdx.x & 7, y = blockIdx.x >> 3;
     const int unit = y / a.RG * 8 + x, rg = y % a.RG;
-    const int pair = unit / a.h_kv, kvh = unit - pair * a.h_kv;
-    const Item it = find_item(a, pair, lane);
-    if (!it.valid) return;
-    const int r = it.r;
-    const int count = a.count ? min(max(a.count[r], 0), a.N) : a.N;
-    if (it.split == 0 && kvh == 0 && rg == 0 && threadIdx.x == 0) {
-        a.info[2 * r] = it.base;
-        a.info[2 * r + 1] = it.splits;
-    }
-
+    const int range = unit / a.h_kv, kvh = unit - range * a.h_kv;
+    Range span = find_range(a, range, threadIdx.x & 63);
     Wave<T, D, MT, SPLITP> w;
-    w.init(a.c);
     const int row0 = (rg * a.RW + rw) * 16 * MT;   // of this wave's rows
-    int node[MT];
-    load_rows(w, a, r, kvh, row0, node, g, rr);
+    for (; span.pos < span.end; next_piece(a, span)) {
+        const int lane = lane_anew(), g = lane >> 4, rr = lane & 15;
+        const Piece it = piece_of(span, range);
+        const int count = a.count ? min(max(a.count[it.r], 0), a.N) : a.N;
+        if (span.off == 0 && kvh == 0 && rg == 0 && threadIdx.x == 0) note_request(a, span);
+        w.init(a.c);
+        int node[MT];
+        load_rows(w, a, it.r, kvh, row0, node, g, rr);
 
-    // the split's share of the request's tiles, every KW-th for this wave
-    const int t0 = (int)((long)it.tiles * it.split / it.splits) + kw, t1 = (int)((long)it.tiles * (it.split + 1) / it.splits);
-    Tiles<HALVES> tl(a, r, kvh, it.len, lane);
-    u32x4 k[2][G::NK], v[8][G::NV];
-    if (t0 < t1) {
-        tl.look_up(t0);
-        tl.go(t0);
-        tl.keys(k, g, rr);
-        tl.template values<G::VB>(v, g, rr);
-        if (t0 + KW < t1) tl.look_up(t0 + KW);
-    }
-    sign_rows(w, a);
-    for (int t = t0; t < t1; t += KW) {
-        f32x4 s[MT][2];
-        w.scores(s, k);
-        const uint32_t seen = tl.seen;
-        const bool more = t + KW < t1;
-        if (more) {
-            tl.go(t + KW);
+        // every KW-th tile for this wave
+        const int t0 = it.t0 + kw, t1 = it.t1;
+        Tiles<HALVES> tl(a, it.r, kvh, it.len, lane);
+        u32x4 k[2][G::NK], v[8][G::NV];
+        undefine(k);
+        undefine(v);
+        if (t0 < t1) {
+            tl.look_up(t0);
+            tl.go(t0);
             tl.keys(k, g, rr);
-            if (t + 2 * KW < t1) tl.look_up(t + 2 * KW);
+            tl.template values<G::VB>(v, g, rr);
+            if (t0 + KW < t1) tl.look_up(t0 + KW);
         }
-        if (seen != ~0u) w.hide(s, v, seen, g);
-        w.weigh(s);
-        w.values(s, v);
-        if (more) tl.template values<G::VB>(v, g, rr);
+        sign_rows(w, a);
+        for (int t = t0; t < t1; t += KW) {
+            f32x4 s[MT][2];
+            w.scores(s, k);
+            const uint32_t seen = tl.seen;
+            const bool more = t + KW < t1;
+            if (more) {
+                tl.go(t + KW);
+                tl.keys(k, g, rr);
+                if (t + 2 * KW < t1) tl.look_up(t + 2 * KW);
+            }
+            if (seen != ~0u) w.hide(s, v, seen, g);
+            w.weigh(s);
+            w.values(s, v);
+            if (more) tl.template values<G::VB>(v, g, rr);
+        }
+        if (it.nodes && kw == KW - 1) attend_nodes(w, a, it.r, kvh, count, node, g, rr);
+        join_waves(w, s_o, s_ml, kw, rw, KW, a.RW, lane);
+        if (kw == 0) write_rows<Out>(w, a, it, kvh, count, row0, node, g, rr);
     }
-    if (it.split == it.splits - 1 && kw == KW - 1) attend_nodes(w, a, r, kvh, count, node, g, rr);
-    join_waves(w, s_o, s_ml, kw, rw, KW, a.RW, lane);
-    if (kw == 0) write_rows<Out>(w, a, it, pair, kvh, count, row0, node, g, rr);
 }
 
 // One workgroup per (request, key head, 16 rows), 16 lanes to a row:
-// o = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.
+// o = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s over the pieces s of a request.
 template <typename Out, int D> __global__ void __launch_bounds__(256) bdgdn_tree_attn_join_kernel(AttnArgs a, int row_tiles)
 {
     constexpr int C = D / 64;   // float4s of a lane
     const int tile = blockIdx.x % row_tiles, rest = blockIdx.x / row_tiles, kvh = rest % a.h_kv, r = rest / a.h_kv;
-    const int base = a.info[2 * r], splits = a.info[2 * r + 1];
-    if (splits == 1) return;   // written by its one split
+    const int size = a.info[0], pos = a.info[1 + 2 * r], w0 = pos / size, splits = (pos + a.info[2 + 2 * r] - 1) / size - w0 + 1;
+    if (splits == 1) return;   // one piece, whose workgroup wrote the result
     const int c = threadIdx.x & 15, lane = threadIdx.x & 63, row = tile * 16 + (threadIdx.x >> 4);
     if (row >= a.N * a.G) return;
-    const long stride = (long)a.h_kv * a.rows_padded;   // rows from one split to the next
-    const long at0 = ((long)base * a.h_kv + kvh) * a.rows_padded + row;
+    // the first piece ends its range unless it begins there too, the others begin theirs
+    const int second = pos % size != 0;
+    const auto place = [&](int s) {
+        return ((long)(2 * (w0 + s) + (s == 0 ? second : 0)) * a.h_kv + kvh) * a.rows_padded + row;
+    };
     float top = -INFINITY;
-    for (int s = c; s < splits; s += 16) top = fmaxf(top, a.part_ml[2 * (at0 + s * stride)]);
+    for (int s = c; s < splits; s += 16) top = fmaxf(top, a.part_ml[2 * place(s)]);
 #pragma unroll
     for (int o = 8; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
     const float ref = top == -INFINITY ? 0.f : top;
@@ -99,7 +104,7 @@ template <typename Out, int D> __global__ void __launch_bounds__(256) bdgdn_tree
     for (int s0 = 0; s0 < splits; s0 += 16) {
         float f = 0.f;
         if (s0 + c < splits) {
-            const long at = at0 + (s0 + c) * stride;
+            const long at = place(s0 + c);
             f = fexp2(a.part_ml[2 * at] - ref);
             l += f * a.part_ml[2 * at + 1];
         }
@@ -107,7 +112,7 @@ template <typename Out, int D> __global__ void __launch_bounds__(256) bdgdn_tree
 #pragma unroll 8
         for (int i = 0; i < n; ++i) {
             const float fi = __shfl(f, (lane & 48) + i);
-            const f32x4 *po = reinterpret_cast<const f32x4 *>(a.part_o + (at0 + (s0 + i) * stride) * D) + c;
+            const f32x4 *po = reinterpret_cast<const f32x4 *>(a.part_o + place(s0 + i) * D) + c;
 #pragma unroll
             for (int x = 0; x < C; ++x) o[x] += fi * po[16 * x];
         }
@@ -148,7 +153,7 @@ __global__ void __launch_bounds__(64) bdgdn_tree_mask_kernel(int N, const int32_
 
 // 16-row groups of a wave at most (bf16 calls with more rows take the wide kernel where the
 // pages allow it): what its registers hold, 512 a lane.
-constexpr int most_mt(bool bf16, int d) { return bf16 ? (d == 256 ? 2 : 4) : (d == 256 ? 1 : 2); }
+constexpr int most_mt(bool bf16, int d) { return d == 256 ? 1 : bf16 ? 4 : 2; }
 
 template <typename T, int D, int MT, bool F32OUT> hipError_t launch_m(const AttnPlan &p, const AttnArgs &a, hipStream_t s)
 {
@@ -164,7 +169,7 @@ template <typename T, int D, bool F32OUT> hipError_t launch_d(const AttnPlan &p,
     constexpr int most = most_mt(sizeof(T) == 2, D);
     hipError_t e = p.wide ? launch_tree_attn_wide(F32OUT, D, p.grid, a, s)
                    : p.mt == 1 ? launch_m<T, D, 1, F32OUT>(p, a, s)
-                   : p.mt == 2 ? launch_m<T, D, (most < 2 ? 1 : 2), F32OUT>(p, a, s)
+                   : p.mt == 2 ? launch_m<T, D, (most < 2 ? most : 2), F32OUT>(p, a, s)
                                : launch_m<T, D, most, F32OUT>(p, a, s);
     if (e != hipSuccess) return e;
     const int row_tiles = (a.N * a.G + 15) / 16;
@@ -179,20 +184,20 @@ AttnPlan attn_plan(bool bf16, int d, int page, int R, int N, int h_q, int h_kv)
 {
     AttnPlan p;
     const int M = N * (h_q / h_kv);
-    p.wide = bf16 && page % 16 == 0 && M > 32;
+    p.wide = bf16 && page % 16 == 0 && M > (d == 256 ? 16 : 32);
     const int groups = M <= 16 ? 1 : M <= 32 ? 2 : 4, most = p.wide ? 2 : most_mt(bf16, d);
     p.mt = groups < most ? groups : most;
     const int waves = (M + 16 * p.mt - 1) / (16 * p.mt);
     p.RW = waves <= 1 ? 1 : waves <= 2 ? 2 : waves <= 4 || !p.wide || d == 256 ? 4 : 8;
     p.RG = (waves + p.RW - 1) / p.RW;
     p.rows_padded = p.RG * p.RW * 16 * p.mt;
-    const long heads = (long)h_kv * p.RG;
-    const long items = (p.mt == 4 ? 512 : 768) / heads;
-    p.items = (int)(items < 1 ? 1 : items);
-    const long units = ((long)p.items + R) * h_kv;   // (request, split, key head) triples at most
-    p.grid = (int)((units + 7) / 8 * 8 * p.RG);
-    const size_t rows = (size_t)units * p.rows_padded;
-    p.ml_at = ((size_t)R * 8 + 255) & ~(size_t)255;
+    // one range for every workgroup that the chip holds at once (one or two to a compute unit)
+    const long heads = (long)h_kv * p.RG, ranges = 256 * (p.wide ? 1 : waves_per_simd(bf16, d, p.mt)) / heads;
+    p.ranges = (int)(ranges < 1 ? 1 : ranges);
+    p.least = 4;   // tiles of a range, one to a wave
+    p.grid = (int)(((long)p.ranges * h_kv + 7) / 8 * 8 * p.RG);
+    const size_t rows = 2 * (size_t)p.ranges * h_kv * p.rows_padded;
+    p.ml_at = ((size_t)(1 + 2 * (size_t)R) * 4 + 255) & ~(size_t)255;
     p.o_at = p.ml_at + ((rows * 8 + 255) & ~(size_t)255);
     p.bytes = p.o_at + rows * d * 4;
     return p;
@@ -202,7 +207,8 @@ hipError_t launch_tree_attn(bool bf16, bool f32_out, int d, const AttnPlan &p, A
 {
     a.RW = p.RW;
     a.RG = p.RG;
-    a.items = p.items;
+    a.ranges = p.ranges;
+    a.least = p.least;
     a.rows_padded = p.rows_padded;
     char *ws = static_cast<char *>(workspace);
     a.info = reinterpret_cast<int32_t *>(ws);

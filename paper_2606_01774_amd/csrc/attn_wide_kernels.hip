@@ -48,127 +48,126 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) bdgdn_tree_
     constexpr int CH = X::CH, KW = X::KW, S = X::S, LOADS = X::LOADS, ROWS = 64 / CH;   // rows of one load
     extern __shared__ u32x4 lds[];
     __shared__ uint32_t s_seen[S][KW][2];
-    const int lane = threadIdx.x & 63, g = lane >> 4, rr = lane & 15;
     const int wave = wave_id(), kw = wave / RW, rw = wave % RW;
     // workgroups with the same keys and other rows are neighbours on one XCD (their numbers
     // are equal modulo 8)
     const int x = blockIdx.x & 7, y = blockIdx.x >> 3;
     const int unit = y / a.RG * 8 + x, rg = y % a.RG;
-    const int pair = unit / a.h_kv, kvh = unit - pair * a.h_kv;
-    const Item it = find_item(a, pair, lane);
-    if (!it.valid) return;
-    const int r = it.r;
-    const int count = a.count ? min(max(a.count[r], 0), a.N) : a.N;
-    if (it.split == 0 && kvh == 0 && rg == 0 && threadIdx.x == 0) {
-        a.info[2 * r] = it.base;
-        a.info[2 * r + 1] = it.splits;
-    }
-    const int t0 = (int)((long)it.tiles * it.split / it.splits), t1 = (int)((long)it.tiles * (it.split + 1) / it.splits);
-    const int n = (t1 - t0 + KW - 1) / KW;   // stages
+    const int range = unit / a.h_kv, kvh = unit - range * a.h_kv;
+    Range span = find_range(a, range, threadIdx.x & 63);
+    Wave<T, D, 2, SPLITP> w;
+    const int row0 = (rg * RW + rw) * 32;   // of this wave's rows
 
     // this wave's share of a stage: rows [first, first + LOADS ROWS) of the keys or the values of one tile
     const int block = wave * LOADS, lkw = block / CH, first = block % (CH / 2) * ROWS;
     const bool is_value = block / (CH / 2) & 1;
-    const TablePtr table = table_of(a, r);
     const unsigned char *pool = static_cast<const unsigned char *>(is_value ? a.vp : a.kp) + (long)kvh * a.head_stride;
-    uint32_t off[LOADS];
-#pragma unroll
-    for (int l = 0; l < LOADS; ++l) {
-        const int key = first + l * ROWS + lane / CH;
-        off[l] = (key & 15) * a.token16 * 16 + X::place(lane % CH, key) * 16;
-    }
-    int pages[2];
-    const auto look_up = [&](int i) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int t = t0 + i * KW + lkw, tok = t * kTile + 16 * h;
-            pages[h] = t < t1 && tok < it.len ? table[column(a, tok)] : -1;
-        }
-    };
-    const auto request = [&](int i) {
-        const int tok0 = (t0 + i * KW + lkw) * kTile;
-        const int buf = i % S;
-        const unsigned char *at[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int tok = tok0 + 16 * h;
-            const bool there = (unsigned)pages[h] < (unsigned)a.n_pages;
-            const uint32_t where = there ? pages[h] * a.page16 + (uint32_t)(tok - column(a, tok) * a.page) * a.token16 : 0;
-            at[h] = pool + (long)where * 16;
-            if (!is_value && lane == 0)
-                s_seen[buf][lkw][h] = !there ? 0u : it.len - tok >= 16 ? 0xffffu : (1u << (it.len - tok)) - 1;
-        }
+    for (; span.pos < span.end; next_piece(a, span)) {
+        const int lane = lane_anew(), g = lane >> 4, rr = lane & 15;
+        uint32_t off[LOADS];
 #pragma unroll
         for (int l = 0; l < LOADS; ++l) {
-            const unsigned char *p = at[(first + l * ROWS) >> 4] + off[l];
-            __builtin_amdgcn_global_load_lds((GlobalPtr)p, (LdsPtr)&lds[buf * X::STAGE + (block + l) * 64], 16, 0, 0);
+            const int key = first + l * ROWS + lane / CH;
+            off[l] = (key & 15) * a.token16 * 16 + X::place(lane % CH, key) * 16;
         }
-    };
-    if (n > 0) look_up(0);
-    Wave<T, D, 2, SPLITP> w;
-    w.init(a.c);
-    const int row0 = (rg * RW + rw) * 32;   // of this wave's rows
-    int node[2];
-    load_rows(w, a, r, kvh, row0, node, g, rr);
-    sign_rows(w, a);
+        // where this lane's chunks of keys and values lie in a tile
+        int ko[G::NK], vo[4];
 #pragma unroll
-    for (int i = 0; i < S - 1; ++i)
-        if (i < n) {
-            request(i);
-            if (i + 1 < n) look_up(i + 1);
-        }
-
-    // where this lane's chunks of keys and values lie in a tile
-    int ko[G::NK], vo[4];
+        for (int j = 0; j < G::NK; ++j) ko[j] = rr * CH + X::place(4 * j + g, rr);
 #pragma unroll
-    for (int j = 0; j < G::NK; ++j) ko[j] = rr * CH + X::place(4 * j + g, rr);
+        for (int i = 0; i < 4; ++i) vo[i] = CH == 8 ? ((4 * g + i) * CH + X::place(rr >> 1, 4 * g + i)) * 16 + (rr & 1) * 8
+                                                    : ((4 * g + i) * CH + X::place(rr, 4 * g + i)) * 16;
+        const Piece it = piece_of(span, range);
+        const int count = a.count ? min(max(a.count[it.r], 0), a.N) : a.N;
+        if (span.off == 0 && kvh == 0 && rg == 0 && threadIdx.x == 0) note_request(a, span);
+        const TablePtr table = table_of(a, it.r);
+        const int n = (it.t1 - it.t0 + KW - 1) / KW;   // stages
+        int pages[2];
+        const auto look_up = [&](int i) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) vo[i] = CH == 8 ? ((4 * g + i) * CH + X::place(rr >> 1, 4 * g + i)) * 16 + (rr & 1) * 8
-                                                : ((4 * g + i) * CH + X::place(rr, 4 * g + i)) * 16;
-    int buf = 0;
-    for (int i = 0; i < n; ++i) {
-        if (n - 1 - i >= S - 2) wait_loads_barrier<(S - 2) * LOADS>();
-        else wait_loads_barrier<0>();
-        if (i + S - 1 < n) {
-            request(i + S - 1);
-            if (i + S < n) look_up(i + S);
-        }
-        const uint32_t seen = __builtin_amdgcn_readfirstlane(s_seen[buf][kw][0] | s_seen[buf][kw][1] << 16);
-        const u32x4 *kt = lds + buf * X::STAGE + kw * 64 * CH;
-        const unsigned char *vt = reinterpret_cast<const unsigned char *>(kt + 32 * CH);
-        buf = buf + 1 == S ? 0 : buf + 1;
-        if (!seen) continue;
-        u32x4 k[2][G::NK], v[8][G::NV];
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int j = 0; j < G::NK; ++j) k[h][j] = kt[16 * h * CH + ko[j]];
-        f32x4 s[2][2];
-        w.scores(s, k);
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-#pragma unroll
-            for (int j = 0; j < G::NV; ++j) {
-                const unsigned char *p = vt + (e >> 2) * 16 * CH * 16 + vo[e & 3] + 256 * j;
-                if constexpr (CH == 8) {
-                    const u32x2v z = *reinterpret_cast<const u32x2v *>(p);
-                    v[e][j] = u32x4{z[0], z[1], 0, 0};
-                } else {
-                    v[e][j] = *reinterpret_cast<const u32x4 *>(p);
-                }
+            for (int h = 0; h < 2; ++h) {
+                const int t = it.t0 + i * KW + lkw, tok = t * kTile + 16 * h;
+                pages[h] = t < it.t1 && tok < it.len ? table[column(a, tok)] : -1;
             }
-        if (seen != ~0u) w.hide(s, v, seen, g);
-        w.weigh(s);
-        w.values(s, v);
-    }
-    if (it.split == it.splits - 1 && kw == KW - 1) attend_nodes(w, a, r, kvh, count, node, g, rr);
-    if constexpr (KW > 1) {
+        };
+        const auto request = [&](int i) {
+            const int tok0 = (it.t0 + i * KW + lkw) * kTile;
+            const int buf = i % S;
+            const unsigned char *at[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int tok = tok0 + 16 * h;
+                const bool there = (unsigned)pages[h] < (unsigned)a.n_pages;
+                const uint32_t where = there ? pages[h] * a.page16 + (uint32_t)(tok - column(a, tok) * a.page) * a.token16 : 0;
+                at[h] = pool + (long)where * 16;
+                if (!is_value && lane == 0)
+                    s_seen[buf][lkw][h] = !there ? 0u : it.len - tok >= 16 ? 0xffffu : (1u << (it.len - tok)) - 1;
+            }
+#pragma unroll
+            for (int l = 0; l < LOADS; ++l) {
+                // (held as 32 bits, so that the address is a scalar base and a lane's offset)
+                uint32_t lane_off = off[l];
+                asm("" : "+v"(lane_off));
+                const unsigned char *p = at[(first + l * ROWS) >> 4] + lane_off;
+                __builtin_amdgcn_global_load_lds((GlobalPtr)p, (LdsPtr)&lds[buf * X::STAGE + (block + l) * 64], 16, 0, 0);
+            }
+        };
+        if (n > 0) look_up(0);
+        w.init(a.c);
+        int node[2];
+        load_rows(w, a, it.r, kvh, row0, node, g, rr);
+        sign_rows(w, a);
+#pragma unroll
+        for (int i = 0; i < S - 1; ++i)
+            if (i < n) {
+                request(i);
+                if (i + 1 < n) look_up(i + 1);
+            }
+        int buf = 0;
+        for (int i = 0; i < n; ++i) {
+            if (n - 1 - i >= S - 2) wait_loads_barrier<(S - 2) * LOADS>();
+            else wait_loads_barrier<0>();
+            if (i + S - 1 < n) {
+                request(i + S - 1);
+                if (i + S < n) look_up(i + S);
+            }
+            const uint32_t seen = __builtin_amdgcn_readfirstlane(s_seen[buf][kw][0] | s_seen[buf][kw][1] << 16);
+            const u32x4 *kt = lds + buf * X::STAGE + kw * 64 * CH;
+            const unsigned char *vt = reinterpret_cast<const unsigned char *>(kt + 32 * CH);
+            buf = buf + 1 == S ? 0 : buf + 1;
+            if (!seen) continue;
+            u32x4 k[2][G::NK], v[8][G::NV];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int j = 0; j < G::NK; ++j) k[h][j] = kt[16 * h * CH + ko[j]];
+            f32x4 s[2][2];
+            w.scores(s, k);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+#pragma unroll
+                for (int j = 0; j < G::NV; ++j) {
+                    const unsigned char *p = vt + (e >> 2) * 16 * CH * 16 + vo[e & 3] + 256 * j;
+                    if constexpr (CH == 8) {
+                        const u32x2v z = *reinterpret_cast<const u32x2v *>(p);
+                        v[e][j] = u32x4{z[0], z[1], 0, 0};
+                    } else {
+                        v[e][j] = *reinterpret_cast<const u32x4 *>(p);
+                    }
+                }
+            if (seen != ~0u) w.hide(s, v, seen, g);
+            w.weigh(s);
+            w.values(s, v);
+        }
+        if (it.nodes && kw == KW - 1) attend_nodes(w, a, it.r, kvh, count, node, g, rr);
         __syncthreads();   // the stages are read: their memory is free
-        f32x4(*s_o)[G::NT][64] = reinterpret_cast<f32x4(*)[G::NT][64]>(lds);
-        float(*s_ml)[2][64] = reinterpret_cast<float(*)[2][64]>(lds + (KW / 2) * RW * G::NT * 64);
-        join_waves(w, s_o, s_ml, kw, rw, KW, RW, lane);
+        if constexpr (KW > 1) {
+            f32x4(*s_o)[G::NT][64] = reinterpret_cast<f32x4(*)[G::NT][64]>(lds);
+            float(*s_ml)[2][64] = reinterpret_cast<float(*)[2][64]>(lds + (KW / 2) * RW * G::NT * 64);
+            join_waves(w, s_o, s_ml, kw, rw, KW, RW, lane);
+        }
+        if (kw == 0) write_rows<Out>(w, a, it, kvh, count, row0, node, g, rr);
     }
-    if (kw == 0) write_rows<Out>(w, a, it, pair, kvh, count, row0, node, g, rr);
 }
 
 template <int D, int RW, bool SPLITP, typename Out> hipError_t launch(int grid, const AttnArgs &a, hipStream_t s)

@@ -15,8 +15,8 @@ struct AttnArgs {
     const uint64_t *mask;
     void *o;
     float *lse;
-    int32_t *info;             // [R][2]: a request's first (request, split) pair and its splits
-    float *part_o, *part_ml;   // the splits' results: [pair][h_kv][rows_padded][d], [..][2]
+    int32_t *info;             // tiles of a range; [R][2]: a request's first tile among all, its tiles
+    float *part_o, *part_ml;   // the pieces' results: [range][2][h_kv][rows_padded][d], [..][2]
     int R, N, h_q, h_kv, G;    // G = h_q / h_kv query heads to a key head
     int page, max_pages, n_slots, n_pages;
     uint32_t page_mul;         // tok / page = mulhi(tok, page_mul) >> page_shift, or tok for 0 (pages of one)
@@ -29,13 +29,13 @@ struct AttnArgs {
     uint32_t q_and, q_xor;     // applied to the words of q: the scale's sign, or zero
     int RW, RG;                // waves of a workgroup, and workgroups, with other rows of a key head
     int rows_padded;           // rows of a key head, filled up to those of RW x RG waves
-    int items;                 // (request, split) pairs that the call aims at
+    int ranges, least;         // ranges that the keys are cut into, at most, and their tiles, at least
 };
 
 // How a call is cut: 16-row groups of a wave, the above, workgroups, and the workspace.
 struct AttnPlan {
     bool wide;                 // the kernel that stages tiles in LDS
-    int mt, RW, RG, rows_padded, items, grid;
+    int mt, RW, RG, rows_padded, ranges, least, grid;
     size_t ml_at, o_at, bytes;
 };
 AttnPlan attn_plan(bool bf16, int d, int page, int R, int N, int h_q, int h_kv);
