@@ -188,11 +188,11 @@ AttnPlan attn_plan(bool bf16, int d, int page, int R, int N, int h_q, int h_kv)
     const int groups = M <= 16 ? 1 : M <= 32 ? 2 : 4, most = p.wide ? 2 : most_mt(bf16, d);
     p.mt = groups < most ? groups : most;
     const int waves = (M + 16 * p.mt - 1) / (16 * p.mt);
-    p.RW = waves <= 1 ? 1 : waves <= 2 ? 2 : waves <= 4 || !p.wide || d == 256 ? 4 : 8;
+    p.RW = waves <= 1 && !p.wide ? 1 : waves <= 2 ? 2 : 4;
     p.RG = (waves + p.RW - 1) / p.RW;
     p.rows_padded = p.RG * p.RW * 16 * p.mt;
     // one range for every workgroup that the chip holds at once (one or two to a compute unit)
-    const long heads = (long)h_kv * p.RG, ranges = 256 * (p.wide ? 1 : waves_per_simd(bf16, d, p.mt)) / heads;
+    const long heads = (long)h_kv * p.RG, ranges = 256 * (p.wide ? (d == 256 ? 1 : 2) : waves_per_simd(bf16, d, p.mt)) / heads;
     p.ranges = (int)(ranges < 1 ? 1 : ranges);
     p.least = 4;   // tiles of a range, one to a wave
     p.grid = (int)(((long)p.ranges * h_kv + 7) / 8 * 8 * p.RG);

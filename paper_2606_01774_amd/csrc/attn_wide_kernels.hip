@@ -19,15 +19,13 @@ namespace {
 typedef __attribute__((address_space(1))) const void *GlobalPtr;
 typedef __attribute__((address_space(3))) void *LdsPtr;
 
-constexpr int waves_of(int d) { return d == 256 ? 4 : 8; }   // of a workgroup
-
 template <int D, int RW> struct Wide {
     static constexpr int CH = D / 8;                    // chunks of a row
-    static constexpr int W = waves_of(D);
+    static constexpr int W = 4;                         // waves
     static constexpr int KW = W / RW;
     static constexpr int STAGE = KW * 64 * CH;          // chunks of a stage: KW x (keys, values) x 32 rows
     static constexpr int LOADS = CH / RW;               // of a wave for a stage, 64 chunks each
-    static constexpr int S = STAGE * 16 >= 65536 ? 2 : STAGE * 16 >= 32768 ? 4 : 6;
+    static constexpr int S = D == 256 ? (RW == 4 ? 4 : 2) : 65536 / (STAGE * 16) > 6 ? 6 : 65536 / (STAGE * 16);
     static constexpr int JOIN = (KW / 2) * RW * (D / 16 * 1024 + 512);
     static constexpr int LDS = S * STAGE * 16 > JOIN ? S * STAGE * 16 : JOIN;
     static __device__ __forceinline__ int place(int c, int key) { return c ^ (CH == 8 ? (key >> 1) & 7 : key & 15); }
@@ -40,7 +38,7 @@ template <int N> __device__ __forceinline__ void wait_loads_barrier()
 }
 
 template <int D, int RW, bool SPLITP, typename Out>
-__global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) bdgdn_tree_attn_wide_kernel(AttnArgs a)
+__global__ void __launch_bounds__(256, D == 256 ? 1 : 2) bdgdn_tree_attn_wide_kernel(AttnArgs a)
 {
     typedef __bf16 T;
     typedef Geo<T, D> G;
@@ -186,10 +184,7 @@ template <int D, int RW, bool SPLITP, typename Out> hipError_t launch(int grid, 
 
 template <int D, bool SPLITP, typename Out> hipError_t launch_rw(int grid, const AttnArgs &a, hipStream_t s)
 {
-    if (a.RW == 2) return launch<D, 2, SPLITP, Out>(grid, a, s);
-    if constexpr (D < 256)
-        if (a.RW == 8) return launch<D, 8, SPLITP, Out>(grid, a, s);
-    return launch<D, 4, SPLITP, Out>(grid, a, s);
+    return a.RW == 2 ? launch<D, 2, SPLITP, Out>(grid, a, s) : launch<D, 4, SPLITP, Out>(grid, a, s);
 }
 
 }  // namespace
