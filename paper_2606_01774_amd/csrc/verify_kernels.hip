@@ -1,13 +1,16 @@
 // verify_kernels.hip -- verification of drafted tokens against the target's logits from given
-// random numbers, in three launches.
+// random numbers, in four launches.
 //
 //   stats  (row, part of the vocabulary): reads every row of logits that a walk may need once
 //          and leaves the part's maximum and sum of exponentials, or (greedy requests) the
 //          index of its maximum.  This is where the bytes are.
 //   walk   (request): the rows' laws and every child's odds at once, then the walk itself in
 //          LDS.  Only a refusal with a sibling left reads a row again, for the residual's mass.
-//   race   (request, part): argmax of law(t) / noise(t) over one row; a request's workgroup
-//          that ends last joins the parts.
+//   race   (request, part): argmax of law(t) / noise(t) over a part of one row.
+//   pick   (request): the best of the parts.
+// One workgroup to a request for walk and race together takes three times as long (36 us for
+// a row of 131072 with its draft and noise, 64 requests), and joining the parts by the last of
+// a request's workgroups twice (each has to write back its caches first).
 #include "common.hpp"
 #include "round.hpp"
 
@@ -186,10 +189,8 @@ struct Law {
     float max, inv, k;
     int arg;
     __device__ __forceinline__ bool ok() const { return inv > 0.f; }
-    __device__ __forceinline__ float at(float x, int v) const
-    {
-        return k == 0.f ? (v == arg ? inv : 0.f) : fexp2((x - max) * k) * inv;
-    }
+    __device__ __forceinline__ float of(float x) const { return fexp2((x - max) * k) * inv; }
+    __device__ __forceinline__ float at(float x, int v) const { return k == 0.f ? (v == arg ? inv : 0.f) : of(x); }
 };
 
 // Joined by one wave, a part to a lane.
@@ -209,40 +210,72 @@ __device__ __forceinline__ Law law_of(const VerifyArgs &a, long row, float k, bo
     return Law{st.max, !ok ? 0.f : greedy ? 1.f : 1.f / st.sum, greedy ? 0.f : k, st.arg};
 }
 
-// What the walk leaves for the race.
-struct Walked {
-    Law p, q;
-    float c;          // law = (p - c q)+; c 0: q is not looked at
-    int node, n_gone; // node whose row is raced for, refused tokens that are out of the law
-    unsigned done;    // parts of the race that have ended
-    int gone[kMaxNodes];
-};
-
+// The law that is left of a row (of a request that is not greedy) from its logits.
 template <typename E> struct Residual {
     const E *t, *d;
     Law p, q;
     float c;
-    // law of the tokens v .. v + N - 1 from their logits
-    template <int N> __device__ __forceinline__ void of(float (&x)[N], int v, const Walked &w, int n_gone) const
+    const int *gone;   // refused tokens that are out of the law
+    int n_gone;
+    __device__ __forceinline__ bool out(int v) const
+    {
+        bool found = false;
+        for (int i = 0; i < n_gone; ++i) found |= gone[i] == v;
+        return found;
+    }
+    // x: the target's logits, then what is left of the law but for what `out` says; y: the
+    // draft's logits where c > 0
+    template <int N> __device__ __forceinline__ void of(float (&x)[N], const float (&y)[N]) const
     {
         if (c > 0.f) {
-            float y[N];
-            if constexpr (N > 1) Vec<E>::load(y, d + v);
-            else y[0] = to_f(d[v]);
 #pragma unroll
-            for (int i = 0; i < N; ++i) x[i] = fmaxf(p.at(x[i], v + i) - c * q.at(y[i], v + i), 0.f);
+            for (int i = 0; i < N; ++i) x[i] = fmaxf(p.of(x[i]) - c * q.of(y[i]), 0.f);
         } else {
 #pragma unroll
-            for (int i = 0; i < N; ++i) x[i] = p.at(x[i], v + i);
-            for (int j = 0; j < n_gone; ++j) {
-                const unsigned at = (unsigned)(w.gone[j] - v);
-#pragma unroll
-                for (int i = 0; i < N; ++i)
-                    if (at == (unsigned)i) x[i] = 0.f;
-            }
+            for (int i = 0; i < N; ++i) x[i] = p.of(x[i]);
+        }
+    }
+    __device__ __forceinline__ float one(int v) const
+    {
+        float x[1] = {to_f(t[v])}, y[1] = {0.f};
+        if (c > 0.f) y[0] = to_f(d[v]);
+        of(x, y);
+        return x[0];
+    }
+};
+
+struct Best {
+    float score;
+    int at;
+    __device__ __forceinline__ void take(float x, int v)
+    {
+        if (x > score || (x == score && (unsigned)v < (unsigned)at)) {
+            score = x;
+            at = v;
         }
     }
 };
+
+// What the walk leaves for the race.
+struct Walked {
+    Law p, q;
+    float c;           // law = (p - c q)+; c 0: q is not looked at
+    int node, n_gone;  // the node whose row is raced for, or -1; refused tokens out of the law
+    int next;          // of a request without a race
+    int gone[kMaxNodes];
+};
+
+template <int THREADS> __device__ __forceinline__ Best best_of_block(Best b, Best *lds)
+{
+#pragma unroll
+    for (int o = 32; o; o >>= 1) b.take(__shfl_xor(b.score, o), __shfl_xor(b.at, o));
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = b;
+    __syncthreads();
+    b = lds[0];
+    for (int w = 1; w < THREADS / 64; ++w) b.take(lds[w].score, lds[w].at);
+    __syncthreads();
+    return b;
+}
 
 template <typename E> __global__ void __launch_bounds__(kWalkThreads) bdgdn_verify_walk_kernel(VerifyArgs a)
 {
@@ -250,18 +283,17 @@ template <typename E> __global__ void __launch_bounds__(kWalkThreads) bdgdn_veri
     __shared__ float s_p[kMaxNodes], s_q[kMaxNodes], s_u[kMaxNodes];
     __shared__ int s_parent[kMaxNodes], s_token[kMaxNodes];
     __shared__ float s_sum[kWalkThreads / 64];
-    __shared__ Walked s_w;
+    __shared__ int s_gone[kMaxNodes];
     const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int count = nodes_of(a, r);
-    int32_t *path = a.path + (long)r * a.N;
     Walked *out = static_cast<Walked *>(a.walked) + r;
+    int32_t *path = a.path + (long)r * a.N;
     if (count < 1) {
         for (int n = tid; n < a.N; n += kWalkThreads) path[n] = -1;
         if (tid == 0) {
             a.n_accept[r] = 0;
             if (a.n_path) a.n_path[r] = 0;
-            a.next[r] = -1;
-            out->node = -1;
+            out->node = out->next = -1;
         }
         return;
     }
@@ -302,7 +334,7 @@ template <typename E> __global__ void __launch_bounds__(kWalkThreads) bdgdn_veri
         const int tok = s_token[n];
         if (tok < 0 || !s_law[0][cur].ok() || (!certain && !s_law[1][cur].ok())) continue;
         bool out_already = false;
-        for (int i = 0; i < n_gone; ++i) out_already |= s_w.gone[i] == tok;
+        for (int i = 0; i < n_gone; ++i) out_already |= s_gone[i] == tok;
         const float left = certain ? (out_already ? 0.f : s_p[n]) : fmaxf(s_p[n] - c * s_q[n], 0.f);
         if (s_u[n] * W * s_q[n] < left) {
             cur = n;
@@ -316,7 +348,7 @@ template <typename E> __global__ void __launch_bounds__(kWalkThreads) bdgdn_veri
         if (certain) {
             if (out_already) continue;
             __syncthreads();
-            if (tid == 0) s_w.gone[n_gone] = tok;
+            if (tid == 0) s_gone[n_gone] = tok;
             ++n_gone;
             __syncthreads();
         } else {
@@ -332,22 +364,20 @@ template <typename E> __global__ void __launch_bounds__(kWalkThreads) bdgdn_veri
             continue;
         }
         const Residual<E> res = {target + cur * a.t_row, certain ? nullptr : draft + cur * a.d_row, s_law[0][cur],
-                                 certain ? Law{} : s_law[1][cur], c};
+                                 certain ? Law{} : s_law[1][cur], c, s_gone, n_gone};
         constexpr int N = Vec<E>::n;
         float sum = 0.f;
         const int whole = a.V / N * N;
+#pragma unroll 2
         for (int v = tid * N; v < whole; v += kWalkThreads * N) {
-            float x[N];
+            float x[N], y[N];
             Vec<E>::load(x, res.t + v);
-            res.of(x, v, s_w, n_gone);
+            if (c > 0.f) Vec<E>::load(y, res.d + v);
+            res.of(x, y);
 #pragma unroll
-            for (int i = 0; i < N; ++i) sum += x[i];
+            for (int i = 0; i < N; ++i) sum += certain && res.out(v + i) ? 0.f : x[i];
         }
-        if (whole + tid < a.V) {
-            float x[1] = {to_f(res.t[whole + tid])};
-            res.of(x, whole + tid, s_w, n_gone);
-            sum += x[0];
-        }
+        if (whole + tid < a.V && !(certain && res.out(whole + tid))) sum += res.one(whole + tid);
         for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
         if (lane == 0) s_sum[wave] = sum;
         __syncthreads();
@@ -357,108 +387,112 @@ template <typename E> __global__ void __launch_bounds__(kWalkThreads) bdgdn_veri
     }
     for (int n = tid; n < a.N; n += kWalkThreads)
         if (n > steps) path[n] = -1;
-    if (tid < n_gone) out->gone[tid] = s_w.gone[tid];
-    // (an integer comparison of the law's bits: from the one of floats hipcc 7.2 makes a select
-    // on a condition that it has not set)
-    const bool lawful = __builtin_amdgcn_readfirstlane(__float_as_int(s_law[0][cur].inv)) > 0;
     if (tid == 0) {
         path[0] = 0;
         a.n_accept[r] = steps;
         if (a.n_path) a.n_path[r] = steps + 1;
+    }
+    if (tid < n_gone) out->gone[tid] = s_gone[tid];
+    // (an integer comparison of the law's bits: from one of floats hipcc 7.2 has made a select
+    // on a condition that it had not set)
+    const bool lawful = __builtin_amdgcn_readfirstlane(__float_as_int(s_law[0][cur].inv)) > 0;
+    if (tid == 0) {
         out->p = s_law[0][cur];
         if (c > 0.f) out->q = s_law[1][cur];
         out->c = c;
-        out->node = lawful ? cur : -1;
+        out->node = lawful && !greedy ? cur : -1;
         out->n_gone = n_gone;
-        out->done = 0;
-        if (!lawful) a.next[r] = -1;
+        // a greedy law is all on one token, and that was not refused
+        out->next = lawful ? s_law[0][cur].arg : -1;
     }
 }
 
-struct Best {
-    float score;
-    int at;
-    __device__ __forceinline__ void take(float x, int v)
-    {
-        if (x > score || (x == score && (unsigned)v < (unsigned)at)) {
-            score = x;
-            at = v;
-        }
-    }
-};
-
-__device__ __forceinline__ Best best_of_block(Best b, Best *lds)
-{
-#pragma unroll
-    for (int o = 32; o; o >>= 1) b.take(__shfl_xor(b.score, o), __shfl_xor(b.at, o));
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = b;
-    __syncthreads();
-    b = lds[0];
-    for (int w = 1; w < kRaceThreads / 64; ++w) b.take(lds[w].score, lds[w].at);
-    __syncthreads();
-    return b;
-}
-
-// argmax over [v0, v1) of law / noise, -1 where nothing is above zero.
-template <typename E> __device__ __forceinline__ Best race(const Residual<E> &res, const Walked &w, int n_gone,
-                                                           const float *noise, int v0, int v1)
+// argmax over [v0, v1) of law / noise, -1 where nothing is above zero.  Every thread of the
+// workgroup gets it.  The quotient is formed only where a product says that it may pass the
+// best one of the wave (x >= best e, less what the rounding of either can hide).
+template <typename E> __device__ __forceinline__ Best race(const Residual<E> &res, const float *noise, int v0, int v1, Best *lds)
 {
     constexpr int N = Vec<E>::n;
     Best b = {0.f, -1};
-    int v = v0 + threadIdx.x * N;
-    for (; v + N <= v1; v += kRaceThreads * N) {
-        float x[N], e[N];
-        Vec<E>::load(x, res.t + v);
+    float bar = 0.f;
+    const auto consider = [&](const float x, const float e, int at) {
+        const float y = x / e;
+        if (y > b.score && !res.out(at)) b = Best{y, at};
+    };
+    const int whole = v0 + (v1 - v0) / N * N;
+#pragma unroll 2
+    for (int v = v0; v < whole; v += kRaceThreads * N) {
+        const int at = v + threadIdx.x * N;
+        const bool in = at < whole;
+        float x[N], y[N], e[N];
+        bool pass = false;
+        if (in) {
+            Vec<E>::load(x, res.t + at);
+            if (res.c > 0.f) Vec<E>::load(y, res.d + at);
 #pragma unroll
-        for (int i = 0; i < N; i += 4) Vec<float>::load(reinterpret_cast<float(&)[4]>(e[i]), noise + v + i);
-        res.of(x, v, w, n_gone);
+            for (int i = 0; i < N; i += 4) Vec<float>::load(reinterpret_cast<float(&)[4]>(e[i]), noise + at + i);
+            res.of(x, y);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const float y = x[i] / e[i];
-            if (y > b.score) b = Best{y, v + i};
+            for (int i = 0; i < N; ++i) pass |= x[i] >= bar * e[i];
         }
+        if (!__any(pass)) continue;
+        if (pass) {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (x[i] >= bar * e[i]) consider(x[i], e[i], at + i);
+        }
+        float top = b.score;
+#pragma unroll
+        for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+        bar = top * 0.999999f;
     }
-    for (; v < v1; ++v) {   // the one thread whose vector ends past v1
-        float x[1] = {to_f(res.t[v])};
-        res.of(x, v, w, n_gone);
-        const float y = x[0] / noise[v];
-        if (y > b.score) b = Best{y, v};
+    if (whole + (int)threadIdx.x < v1) {
+        const int at = whole + threadIdx.x;
+        consider(res.one(at), noise[at], at);
     }
-    return b;
+    return best_of_block<kRaceThreads>(b, lds);
+}
+
+template <typename E> __device__ __forceinline__ Residual<E> left_of(const VerifyArgs &a, const Walked &w, int r)
+{
+    return Residual<E>{static_cast<const E *>(a.target) + r * a.t_req + w.node * a.t_row,
+                       w.c > 0.f ? static_cast<const E *>(a.draft) + r * a.d_req + w.node * a.d_row : nullptr, w.p, w.q, w.c,
+                       w.gone, w.n_gone};
 }
 
 template <typename E> __global__ void __launch_bounds__(kRaceThreads) bdgdn_verify_race_kernel(VerifyArgs a)
 {
     __shared__ Best lds[kRaceThreads / 64];
-    __shared__ bool s_last;
-    const int r = blockIdx.y, tid = threadIdx.x;
-    Walked *w = static_cast<Walked *>(a.walked) + r;
-    const int node = w->node;
-    if (node < 0) return;   // no law
-    const float *noise = a.noise + r * a.noise_stride;
-    Residual<E> res = {static_cast<const E *>(a.target) + r * a.t_req + node * a.t_row,
-                       static_cast<const E *>(a.draft) + r * a.d_req + node * a.d_row, w->p, w->q, w->c};
-    const int n_gone = w->n_gone;
+    const int r = blockIdx.y;
+    const Walked &w = static_cast<const Walked *>(a.walked)[r];
+    if (w.node < 0) return;
     const int v0 = blockIdx.x * a.race_part, v1 = min(v0 + a.race_part, a.V);
-    Best b = best_of_block(race(res, *w, n_gone, noise, v0, v1), lds);
-    Best *parts = static_cast<Best *>(a.best) + (long)r * a.race_splits;
-    if (tid == 0) {
-        __hip_atomic_store(&parts[blockIdx.x].score, b.score, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        __hip_atomic_store(&parts[blockIdx.x].at, b.at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        s_last = __hip_atomic_fetch_add(&w->done, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)a.race_splits - 1;
+    const Best b = race(left_of<E>(a, w, r), a.noise + r * a.noise_stride, v0, v1, lds);
+    if (threadIdx.x == 0) static_cast<Best *>(a.best)[(long)r * a.race_splits + blockIdx.x] = b;
+}
+
+template <typename E> __global__ void __launch_bounds__(kRaceThreads) bdgdn_verify_pick_kernel(VerifyArgs a)
+{
+    __shared__ Best lds[kRaceThreads / 64];
+    const int r = blockIdx.x;
+    const Walked &w = static_cast<const Walked *>(a.walked)[r];
+    if (w.node < 0) {
+        if (threadIdx.x == 0) a.next[r] = w.next;
+        return;
     }
-    __syncthreads();
-    if (!s_last) return;
-    b = Best{0.f, -1};
-    for (int i = tid; i < a.race_splits; i += kRaceThreads)
-        b.take(__hip_atomic_load(&parts[i].score, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT),
-               __hip_atomic_load(&parts[i].at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
-    b = best_of_block(b, lds);
+    Best b = {0.f, -1};
+    for (int i = threadIdx.x; i < a.race_splits; i += kRaceThreads) {
+        const Best x = static_cast<const Best *>(a.best)[(long)r * a.race_splits + i];
+        b.take(x.score, x.at);
+    }
+    b = best_of_block<kRaceThreads>(b, lds);
     if (b.at < 0) {   // nothing is left of the law: p itself
+        Residual<E> res = left_of<E>(a, w, r);
         res.c = 0.f;
-        b = best_of_block(race(res, *w, 0, noise, 0, a.V), lds);
+        res.n_gone = 0;
+        b = race(res, a.noise + r * a.noise_stride, 0, a.V, lds);
     }
-    if (tid == 0) a.next[r] = b.at;
+    if (threadIdx.x == 0) a.next[r] = b.at;
 }
 
 template <typename E> void launch(const VerifyArgs &a, hipStream_t s)
@@ -466,27 +500,29 @@ template <typename E> void launch(const VerifyArgs &a, hipStream_t s)
     bdgdn_verify_stats_kernel<E><<<(a.draft ? 2 : 1) * a.R * a.N * a.splits, kStatThreads, 0, s>>>(a);
     bdgdn_verify_walk_kernel<E><<<a.R, kWalkThreads, 0, s>>>(a);
     bdgdn_verify_race_kernel<E><<<dim3(a.race_splits, a.R), kRaceThreads, 0, s>>>(a);
+    bdgdn_verify_pick_kernel<E><<<a.R, kRaceThreads, 0, s>>>(a);
 }
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 }  // namespace
 
-// Parts of a row: enough workgroups for the chip (2048 hold all its threads), at least 4096
-// logits each and at most 64 of them, a part to a lane of the wave that joins them.
+// Parts of a row: enough workgroups for the chip (2048 hold all its threads), of two steps of
+// a workgroup's loads at least; of a row's statistics at most 64, one to a lane of the wave
+// that joins them.
 VerifyPlan verify_plan(int R, int N, int V)
 {
-    const auto cut = [V](long rows, long wanted, int &parts, int &part) {
-        long n = (wanted + rows - 1) / rows;
+    const auto cut = [V](long rows, long limit, int &parts, int &part) {
         const long most = (V + 4095) / 4096;
+        long n = (2048 + rows - 1) / rows;
         n = n > most ? most : n;
-        n = n > 64 ? 64 : n < 1 ? 1 : n;
+        n = n > limit ? limit : n;
         part = (int)(((V + n - 1) / n + 7) / 8 * 8);
         parts = (V + part - 1) / part;
     };
     VerifyPlan p;
-    cut(2L * R * N, 2048, p.splits, p.part);
-    cut(R, 1024, p.race_splits, p.race_part);
+    cut(2L * R * N, 64, p.splits, p.part);
+    cut(R, 2048, p.race_splits, p.race_part);
     p.walked_at = align256(2 * (size_t)R * N * p.splits * 16);
     p.best_at = p.walked_at + align256((size_t)R * sizeof(Walked));
     p.bytes = p.best_at + align256((size_t)R * p.race_splits * sizeof(Best));

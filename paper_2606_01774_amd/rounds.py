@@ -15,7 +15,7 @@ from typing import NamedTuple
 
 import torch
 
-from . import _DT, _F32, _I32, _check, _dev, _p, _stream, load_library
+from . import _DT, _F32, _I32, _Tensor, _check, _p, _stream, load_library
 
 BDGDN_MASK_FULL = 0
 BDGDN_MASK_CAUSAL = 1
@@ -90,10 +90,13 @@ def bind(lib):
 
 
 # ------------------------------------------------------------------ marshalling
+# A serving round makes these calls once a layer, so they cost what their marshalling does: what
+# follows from shapes, strides and types alone is worked out once for each set of them, and a
+# call reads its tensors' attributes and passes plain integers.
 @functools.lru_cache(maxsize=512)
 def _cache_desc(n_slots, max_pages, shape, strides, dtype):
     n_pages, page, h_kv, d = shape
-    return CacheDesc(n_pages, page, n_slots, max_pages, h_kv, d, _DT.get(dtype, -1), *strides)
+    return CacheDesc(n_pages, page, n_slots, max_pages, h_kv, d, _DT.get(dtype, -1), *strides[:3])
 
 
 @functools.lru_cache(maxsize=512)
@@ -101,30 +104,43 @@ def _table_desc(n_slots, max_pages, n_pages, page):
     return CacheDesc(n_pages, page, n_slots, max_pages)
 
 
-def _pool(t, name):
-    """A pool's geometry, (shape, strides without the last), after its checks."""
-    if not isinstance(t, torch.Tensor) or t.device.type != "cuda" or t.dim() != 4:
-        raise ValueError(f"{name} must be a device tensor [n_pages, page, h_kv, d]")
-    strides = t.stride()
+def _check_pool(shape, strides, name):
+    if len(shape) != 4:
+        raise ValueError(f"{name} must be [n_pages, page, h_kv, d]")
     if strides[3] != 1:
         raise ValueError(f"the elements of a head of {name} must be contiguous")
-    return tuple(t.shape), strides[:3]
 
 
-def _rows(t, name, dtype):
-    """The stride between the nodes' rows of [R, N, h, d], which may be a part of longer rows."""
-    if not isinstance(t, torch.Tensor) or t.device.type != "cuda" or t.dim() != 4:
-        raise ValueError(f"{name} must be a device tensor [R, N, heads, d]")
-    if t.dtype != dtype:
-        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.is_contiguous():
+def _row_stride(shape, strides, name):
+    """Elements between the nodes' rows of [R, N, h, d], which may be a part of longer rows; 0
+    for contiguous ones."""
+    if len(shape) != 4:
+        raise ValueError(f"{name} must be [R, N, heads, d]")
+    R, N, h, d = shape
+    if R * N == 0:
         return 0
-    R, N, h, d = t.shape
-    s = t.stride()
-    row = s[1] if N > 1 else s[0]
-    if s[3] != 1 or (h > 1 and s[2] != d) or (R > 1 and s[0] != N * row):
+    row = strides[1] if N > 1 else strides[0] if R > 1 else h * d
+    if (d > 1 and strides[3] != 1) or (h > 1 and strides[2] != d) or (R > 1 and N > 1 and strides[0] != N * row):
         raise ValueError(f"{name} must have contiguous heads and one stride between its rows")
-    return row if R * N > 1 else 0
+    return 0 if row == h * d else row
+
+
+def _device(t, name):
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+
+
+def _alike(ts, name):
+    """The addresses of device tensors of one shape, stride and type."""
+    first = ts[0]
+    _device(first, f"{name}[0]")
+    shape, strides, dt = first.shape, first.stride(), first.dtype
+    for i, t in enumerate(ts):
+        if not (type(t) is _Tensor and t.is_cuda and t.dtype is dt and t.shape == shape and t.stride() == strides):
+            _device(t, f"{name}[{i}]")
+            if t.dtype is not dt or t.shape != shape or t.stride() != strides:
+                raise ValueError(f"{name}[{i}] must be like {name}[0]")
+    return (ctypes.c_void_p * len(ts))(*[t.data_ptr() for t in ts])
 
 
 def _tables(tables):
@@ -137,24 +153,41 @@ def _tables(tables):
 
 
 def _vector(t, name, n, dtype=_I32):
-    if t is not None and t.numel() != n:
+    if t is None:
+        return None
+    if t.numel() != n:
         raise ValueError(f"{name} must have {n} elements")
     return _p(t, name, dtype)
 
 
-def _workspace(workspace, need, device):
-    """(workspace, its address, its size), allocated where none is given."""
+def _scratch(workspace, need, device):
+    """(workspace, its size), allocated where none is given."""
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=device)
-    return workspace, _p(workspace, "workspace"), workspace.numel() * workspace.element_size()
+        return torch.empty(need, dtype=torch.uint8, device=device), need
+    _p(workspace, "workspace")
+    return workspace, workspace.numel() * workspace.element_size()
 
 
 # ------------------------------------------------------------------ attention
 @functools.lru_cache(maxsize=512)
-def _attn_plan(R, N, h_q, h_kv, d, scale, dtype, out_dtype, mask, strides, cache):
-    desc = AttnDesc(R, N, h_q, h_kv, d, scale, _DT.get(dtype, -1), _DT.get(out_dtype, -1), mask, *strides)
-    c = _cache_desc(*cache)
-    return desc, c, int(load_library().bdgdn_tree_attn_workspace(ctypes.byref(desc), ctypes.byref(c)))
+def _attn_plan(q, sq, k, sk, v, sv, kp, skp, vp, svp, table, slots, scale, dtype, out_dtype, mask):
+    """Everything that follows from shapes, strides and types: both descriptors and the bytes of
+    workspace."""
+    rows = [_row_stride(*x) for x in ((q, sq, "q"), (k, sk, "k"), (v, sv, "v"))]
+    (R, N, h_q, d), h_kv = q, k[2]
+    if tuple(k) != (R, N, h_kv, d) or v != k:
+        raise ValueError("k and v must be [R, N, h_kv, d] for q's R, N and d")
+    _check_pool(kp, skp, "k_pages")
+    if vp != kp or svp != skp:
+        raise ValueError("k_pages and v_pages must be alike")
+    if len(table) != 2 or slots != table[0]:
+        raise ValueError("page_table must be [n_slots, max_pages] and seq_len [n_slots]")
+    if mask is None:
+        raise ValueError("unknown mask")
+    desc = AttnDesc(R, N, h_q, h_kv, d, 1.0 / math.sqrt(d) if scale is None else scale, _DT.get(dtype, -1),
+                    _DT.get(out_dtype, -1), mask, *rows)
+    cache = _cache_desc(table[0], table[1], tuple(kp), skp, dtype)
+    return desc, cache, int(load_library().bdgdn_tree_attn_workspace(ctypes.byref(desc), ctypes.byref(cache)))
 
 
 def bdgdn_tree_attn_workspace(desc: AttnDesc, cache: CacheDesc) -> int:
@@ -168,34 +201,36 @@ def bdgdn_tree_attn(q, k, v, k_pages, v_pages, page_table, seq_len, *, mask="ful
     "causal", or int64 words [R, N] (bit j of word n: node n sees node j; bdgdn_tree_mask makes
     a tree's).  scale is 1/sqrt(d) unless given, out_dtype q's.  Returns (o, lse or None)."""
     lib = load_library()
+    for t, name in ((q, "q"), (k, "k"), (v, "v"), (k_pages, "k_pages"), (v_pages, "v_pages")):
+        if not (type(t) is _Tensor and t.is_cuda):
+            _device(t, name)
     dt = q.dtype
-    strides = (_rows(q, "q", dt), _rows(k, "k", dt), _rows(v, "v", dt))
-    (R, N, h_q, d), h_kv = q.shape, k.shape[2]
-    if k.shape != (R, N, h_kv, d) or v.shape != k.shape:
-        raise ValueError("k and v must be [R, N, h_kv, d] for q's R, N and d")
-    shape, pool_strides = _pool(k_pages, "k_pages")
-    if _pool(v_pages, "v_pages") != (shape, pool_strides) or k_pages.dtype != dt or v_pages.dtype != dt:
-        raise ValueError("k_pages and v_pages must be alike and of q's type")
-    if page_table.dim() != 2 or seq_len.numel() != page_table.shape[0]:
-        raise ValueError("page_table must be [n_slots, max_pages] and seq_len [n_slots]")
-    kind = BDGDN_MASK_BITS if isinstance(mask, torch.Tensor) else _MASKS.get(mask)
-    if kind is None:
-        raise ValueError(f"unknown mask {mask!r}")
-    bits = _vector(mask, "mask", R * N, torch.int64) if kind == BDGDN_MASK_BITS else None
+    if k.dtype is not dt or v.dtype is not dt or k_pages.dtype is not dt or v_pages.dtype is not dt:
+        raise ValueError(f"k, v, k_pages and v_pages must be of q's type, {dt}")
+    shape = q.shape
+    words = isinstance(mask, _Tensor)
     out_dtype = o.dtype if o is not None else dt if out_dtype is None else out_dtype
-    desc, cache, need = _attn_plan(R, N, h_q, h_kv, d, 1.0 / math.sqrt(d) if scale is None else float(scale), dt,
-                                   out_dtype, kind, strides, (*page_table.shape, shape, pool_strides, dt))
+    desc, cache, need = _attn_plan(shape, q.stride(), k.shape, k.stride(), v.shape, v.stride(), k_pages.shape,
+                                   k_pages.stride(), v_pages.shape, v_pages.stride(), page_table.shape, seq_len.numel(),
+                                   None if scale is None else float(scale), dt, out_dtype,
+                                   BDGDN_MASK_BITS if words else _MASKS.get(mask))
+    R, N, h_q, _ = shape
+    device = q.device
     if o is None:
-        o = torch.empty(R, N, h_q, d, dtype=out_dtype, device=q.device)
-    elif o.shape != q.shape:
-        raise ValueError("o must have q's shape")
+        o = torch.empty(shape, dtype=out_dtype, device=device)
+        po = o.data_ptr()
+    else:
+        if o.shape != shape:
+            raise ValueError("o must have q's shape")
+        po = _p(o, "o", out_dtype)
     if lse is None and want_lse:
-        lse = torch.empty(R, N, h_q, dtype=_F32, device=q.device)
-    workspace, pw, size = _workspace(workspace, need, q.device)
+        lse = torch.empty((R, N, h_q), dtype=_F32, device=device)
+    workspace, size = _scratch(workspace, need, device)
     st = lib.bdgdn_tree_attn(desc, cache, q.data_ptr(), k.data_ptr(), v.data_ptr(), k_pages.data_ptr(),
                              v_pages.data_ptr(), _p(page_table, "page_table", _I32), _p(seq_len, "seq_len", _I32),
-                             _vector(slot, "slot", R), _vector(count, "count", R), bits, _p(o, "o", out_dtype),
-                             _vector(lse, "lse", R * N * h_q, _F32), pw, size, _stream(stream))
+                             _vector(slot, "slot", R), _vector(count, "count", R),
+                             _vector(mask, "mask", R * N, torch.int64) if words else None, po,
+                             _vector(lse, "lse", R * N * h_q, _F32), workspace.data_ptr(), size, _stream(stream))
     _check(st, "bdgdn_tree_attn")
     return o, lse
 
@@ -204,9 +239,9 @@ def bdgdn_tree_mask(parent, *, mask=None, depth=None, want_depth=False, stream=N
     """Mask words (int64 [R, N]) of drafted trees from parent [R, N] int32: a node sees itself
     and its ancestors.  With want_depth (or depth given) returns (mask, depth)."""
     lib = load_library()
+    pp = _p(parent, "parent", _I32)
     if parent.dim() != 2:
         raise ValueError("parent must be [R, N]")
-    pp = _p(parent, "parent", _I32)
     R, N = parent.shape
     if mask is None:
         mask = torch.empty(R, N, dtype=torch.int64, device=parent.device)
@@ -220,19 +255,21 @@ def bdgdn_tree_mask(parent, *, mask=None, depth=None, want_depth=False, stream=N
 
 # ------------------------------------------------------------------ verification
 @functools.lru_cache(maxsize=512)
-def _verify_plan(R, N, V, dtype, strides):
-    desc = VerifyDesc(R, N, V, _DT.get(dtype, -1), *strides)
+def _verify_plan(target, st, draft, sd, noise, sn, dtype):
+    for shape, strides, name in ((target, st, "target"), (draft, sd, "draft")):
+        if shape is not None and (len(shape) != 3 or (shape[2] > 1 and strides[2] != 1)):
+            raise ValueError(f"{name} must be [R, N, V] with contiguous rows")
+    R, N, V = target
+    if draft is not None and (draft[0] != R or draft[1] not in (N, N - 1) or draft[2] != V):
+        raise ValueError("draft must be [R, N or N - 1, V] for target's R, N and V")
+    if tuple(noise) != (R, V) or (V > 1 and sn[1] != 1):
+        raise ValueError("noise must be [R, V] with contiguous rows")
+    desc = VerifyDesc(R, N, V, _DT.get(dtype, -1), st[0], st[1], *((0, 0) if draft is None else sd[:2]), sn[0])
     return desc, int(load_library().bdgdn_verify_workspace(ctypes.byref(desc)))
 
 
 def bdgdn_verify_workspace(desc: VerifyDesc) -> int:
     return int(load_library().bdgdn_verify_workspace(ctypes.byref(desc)))
-
-
-def _logits(t, name):
-    if not isinstance(t, torch.Tensor) or t.device.type != "cuda" or t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
-        raise ValueError(f"{name} must be a device tensor [R, N, V] with contiguous rows")
-    return t.stride()[:2]
 
 
 def bdgdn_verify(target, token, u, noise, *, draft=None, parent=None, count=None, temperature=None, n_accept=None,
@@ -244,19 +281,20 @@ def bdgdn_verify(target, token, u, noise, *, draft=None, parent=None, count=None
     Returns (n_accept [R], path [R, N], next_token [R]), with want_n_path (or n_path given)
     (n_accept, path, next_token, n_path), all int32."""
     lib = load_library()
-    t_strides = _logits(target, "target")
-    R, N, V = target.shape
-    d_strides = (0, 0)
+    _device(target, "target")
+    _device(noise, "noise")
+    dt = target.dtype
+    if noise.dtype is not _F32:
+        raise ValueError(f"noise must be {_F32}, got {noise.dtype}")
     if draft is not None:
-        d_strides = _logits(draft, "draft")
-        if draft.dtype != target.dtype or draft.shape[0] != R or draft.shape[1] not in (N, N - 1) or draft.shape[2] != V:
-            raise ValueError("draft must be [R, N or N - 1, V] of the target's type")
-        if draft.shape[1] == 0:
-            draft = None
-    if noise.dim() != 2 or noise.shape != (R, V) or noise.dtype != _F32 or noise.device.type != "cuda" or (
-            V > 1 and noise.stride(1) != 1):
-        raise ValueError("noise must be a device tensor [R, V] of fp32 with contiguous rows")
-    desc, need = _verify_plan(R, N, V, target.dtype, (*t_strides, *d_strides, noise.stride(0)))
+        _device(draft, "draft")
+        if draft.dtype is not dt:
+            raise ValueError(f"draft must be of target's type, {dt}")
+    desc, need = _verify_plan(target.shape, target.stride(), None if draft is None else draft.shape,
+                              None if draft is None else draft.stride(), noise.shape, noise.stride(), dt)
+    R, N, V = target.shape
+    if draft is not None and draft.shape[1] == 0:
+        draft = None
     dev = target.device
     if n_accept is None:
         n_accept = torch.empty(R, dtype=_I32, device=dev)
@@ -266,12 +304,12 @@ def bdgdn_verify(target, token, u, noise, *, draft=None, parent=None, count=None
         next_token = torch.empty(R, dtype=_I32, device=dev)
     if n_path is None and want_n_path:
         n_path = torch.empty(R, dtype=_I32, device=dev)
-    workspace, pw, size = _workspace(workspace, need, dev)
+    workspace, size = _scratch(workspace, need, dev)
     st = lib.bdgdn_verify(desc, target.data_ptr(), None if draft is None else draft.data_ptr(),
                           _vector(token, "token", R * N), _vector(parent, "parent", R * N), _vector(count, "count", R),
                           _vector(temperature, "temperature", R, _F32), _vector(u, "u", R * N, _F32), noise.data_ptr(),
                           _vector(n_accept, "n_accept", R), _vector(n_path, "n_path", R), _vector(path, "path", R * N),
-                          _vector(next_token, "next_token", R), pw, size, _stream(stream))
+                          _vector(next_token, "next_token", R), workspace.data_ptr(), size, _stream(stream))
     _check(st, "bdgdn_verify")
     return (n_accept, path, next_token) if n_path is None else (n_accept, path, next_token, n_path)
 
@@ -282,23 +320,17 @@ def bdgdn_cache_workspace(cache: CacheDesc, num_req: int, rows_max: int) -> int:
 
 
 @functools.lru_cache(maxsize=512)
-def _cache_bytes(cache, num_req, rows_max):
-    return bdgdn_cache_workspace(_cache_desc(*cache), num_req, rows_max)
-
-
-def _pool_list(tables, pools):
-    """(descriptor's key, host array of the pools' addresses) of alike pools."""
-    if not pools:
-        raise ValueError("a cache has at least one pool")
-    first = _pool(pools[0], "pools[0]")
-    dt = pools[0].dtype
-    for i, t in enumerate(pools):
-        if _pool(t, f"pools[{i}]") != first or t.dtype != dt:
-            raise ValueError("the pools of a cache must be alike")
-    if first[0][0] != tables.refcount.numel():
+def _pools_plan(table, n_pages, shape, strides, dtype, R, M, rows, row_strides):
+    """(descriptor, bytes of workspace, stride between rows) of calls that move M rows at most
+    for each of R requests; rows are the new ones' shape (append)."""
+    _check_pool(shape, strides, "pools[0]")
+    if shape[0] != n_pages:
         raise ValueError("the pools must have as many pages as refcount")
-    return ((*tables.page_table.shape, *first, dt),
-            (ctypes.c_void_p * len(pools))(*[t.data_ptr() for t in pools]))
+    if rows is not None and tuple(rows[2:]) != tuple(shape[2:]):
+        raise ValueError("rows must be [R, N, h_kv, d] for the pools' h_kv and d")
+    stride = 0 if rows is None else _row_stride(rows, row_strides, "rows[0]")
+    desc = _cache_desc(table[0], table[1], tuple(shape), strides, dtype)
+    return desc, bdgdn_cache_workspace(desc, R, M), stride
 
 
 def bdgdn_cache_append(tables, pools, rows, slot, count, *, path=None, status=None, workspace=None, stream=None):
@@ -306,23 +338,22 @@ def bdgdn_cache_append(tables, pools, rows, slot, count, *, path=None, status=No
     slot[r].  rows: one [R, N, h_kv, d] per pool; path [R, N] int32 or None (rows in order).
     Returns status [R] (BDGDN_CACHE_DONE or why a sequence was left as it was)."""
     lib = load_library()
-    key, ptrs = _pool_list(tables, pools)
-    if len(rows) != len(pools):
-        raise ValueError("rows must hold one tensor per pool")
-    stride, shape = _rows(rows[0], "rows[0]", pools[0].dtype), rows[0].shape
-    for i, t in enumerate(rows):
-        if _rows(t, f"rows[{i}]", pools[0].dtype) != stride or t.shape != shape:
-            raise ValueError("the rows of all pools must be alike")
-    R, N = shape[:2]
-    if shape[2:] != pools[0].shape[2:]:
-        raise ValueError("rows must be [R, N, h_kv, d] for the pools' h_kv and d")
+    n = len(pools)
+    if n == 0 or len(rows) != n:
+        raise ValueError("a cache has at least one pool, and rows one tensor per pool")
+    pool_ptrs, row_ptrs, p0, r0 = _alike(pools, "pools"), _alike(rows, "rows"), pools[0], rows[0]
+    if r0.dtype is not p0.dtype or r0.dim() != 4:
+        raise ValueError("rows must be [R, N, h_kv, d] of the pools' type")
+    R, N = r0.shape[:2]
+    desc, need, stride = _pools_plan(tables[0].shape, tables[2].numel(), p0.shape, p0.stride(), p0.dtype, R, N, r0.shape,
+                                     r0.stride())
+    device = p0.device
     if status is None:
-        status = torch.empty(R, dtype=_I32, device=slot.device)
-    workspace, pw, size = _workspace(workspace, _cache_bytes(key, R, N), slot.device)
-    st = lib.bdgdn_cache_append(_cache_desc(*key), _tables(tables), ptrs,
-                                (ctypes.c_void_p * len(rows))(*[t.data_ptr() for t in rows]), len(pools), R, N, stride,
-                                _vector(slot, "slot", R), _vector(path, "path", R * N), _vector(count, "count", R),
-                                _vector(status, "status", R), pw, size, _stream(stream))
+        status = torch.empty(R, dtype=_I32, device=device)
+    workspace, size = _scratch(workspace, need, device)
+    st = lib.bdgdn_cache_append(desc, _tables(tables), pool_ptrs, row_ptrs, n, R, N, stride, _vector(slot, "slot", R),
+                                _vector(path, "path", R * N), _vector(count, "count", R), _vector(status, "status", R),
+                                workspace.data_ptr(), size, _stream(stream))
     _check(st, "bdgdn_cache_append")
     return status
 
@@ -342,16 +373,20 @@ def bdgdn_cache_fork(tables, src, dst, *, page, status=None, stream=None):
 def bdgdn_cache_compact(tables, pools, slot, keep, count, *, status=None, workspace=None, stream=None):
     """Keeps positions keep[r, :count[r]] (rising) of the sequences in slot[r].  Returns status."""
     lib = load_library()
-    key, ptrs = _pool_list(tables, pools)
+    if len(pools) == 0:
+        raise ValueError("a cache has at least one pool")
+    ptrs, p0 = _alike(pools, "pools"), pools[0]
+    pk = _p(keep, "keep", _I32)
     if keep.dim() != 2:
         raise ValueError("keep must be [R, M]")
     R, M = keep.shape
+    desc, need, _ = _pools_plan(tables[0].shape, tables[2].numel(), p0.shape, p0.stride(), p0.dtype, R, M, None, None)
     if status is None:
-        status = torch.empty(R, dtype=_I32, device=slot.device)
-    workspace, pw, size = _workspace(workspace, _cache_bytes(key, R, M), slot.device)
-    st = lib.bdgdn_cache_compact(_cache_desc(*key), _tables(tables), ptrs, len(pools), R, M, _vector(slot, "slot", R),
-                                 _p(keep, "keep", _I32), _vector(count, "count", R), _vector(status, "status", R), pw,
-                                 size, _stream(stream))
+        status = torch.empty(R, dtype=_I32, device=p0.device)
+    workspace, size = _scratch(workspace, need, p0.device)
+    st = lib.bdgdn_cache_compact(desc, _tables(tables), ptrs, len(pools), R, M, _vector(slot, "slot", R), pk,
+                                 _vector(count, "count", R), _vector(status, "status", R), workspace.data_ptr(), size,
+                                 _stream(stream))
     _check(st, "bdgdn_cache_compact")
     return status
 
