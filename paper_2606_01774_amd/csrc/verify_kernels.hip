@@ -329,8 +329,12 @@ template <typename E> __global__ void __launch_bounds__(kWalkThreads) bdgdn_veri
 
     int cur = 0, steps = 0, n_gone = 0;
     float c = 0.f, W = 1.f;
-    for (int n = 1; n < count; ++n) {
-        if (s_parent[n] != cur) continue;
+    const int my_parent = lane < count ? s_parent[lane] : -1;
+    // (a child's number is higher than its parent's, so the children come in index order)
+    unsigned long long children = __ballot(my_parent == cur);
+    while (children) {
+        const int n = __ffsll(children) - 1;
+        children &= children - 1;
         const int tok = s_token[n];
         if (tok < 0 || !s_law[0][cur].ok() || (!certain && !s_law[1][cur].ok())) continue;
         bool out_already = false;
@@ -343,6 +347,7 @@ template <typename E> __global__ void __launch_bounds__(kWalkThreads) bdgdn_veri
             c = 0.f;
             W = 1.f;
             n_gone = 0;
+            children = __ballot(my_parent == cur);
             continue;
         }
         if (certain) {
@@ -354,9 +359,7 @@ template <typename E> __global__ void __launch_bounds__(kWalkThreads) bdgdn_veri
         } else {
             c += W;
         }
-        bool more = false;
-        for (int x = n + 1; x < count; ++x) more |= s_parent[x] == cur;
-        if (!more) continue;
+        if (!children) continue;
         // the residual's mass.  What is left of certain proposals follows by subtraction as
         // long as that keeps all but four bits.
         if (certain && W - left > 0.0625f) {
