@@ -151,7 +151,8 @@ __device__ __forceinline__ void next_piece(const AttnArgs &a, Range &g)
     if (g.pos >= g.end) return;
     ++g.r;
     g.off = 0;
-    g.len = __builtin_amdgcn_readfirstlane(length_of(a, g.r));
+    const int slot = a.slot ? ((TablePtr)(uintptr_t)a.slot)[g.r] : g.r;
+    g.len = (unsigned)slot < (unsigned)a.n_slots ? min(max(((TablePtr)(uintptr_t)a.len)[slot], 0), a.max_pages * a.page) : 0;
     g.tiles = tiles_of(g.len);
 }
 
@@ -208,30 +209,38 @@ template <typename T, int D, int MT, bool SPLITP> struct Wave {
             }
     }
 
-    // keys that are not there: their scores and values
-    __device__ __forceinline__ void hide(f32x4 (&s)[MT][2], u32x4 (&v)[8][G::NV], uint32_t seen, int g)
+    // keys that are not there: their scores, their values
+    __device__ __forceinline__ void hide(f32x4 (&s)[MT][2], uint32_t seen, int g)
     {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-            if (!(seen >> (16 * (e >> 2) + 4 * g + (e & 3)) & 1)) {
-#pragma unroll
-                for (int j = 0; j < G::NV; ++j) v[e][j] = u32x4{0, 0, 0, 0};
+            if (!(seen >> (16 * (e >> 2) + 4 * g + (e & 3)) & 1))
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) s[mt][e >> 2][e & 3] = -INFINITY;
-            }
+    }
+    __device__ __forceinline__ void hide(u32x4 (&v)[8][G::NV], uint32_t seen, int g)
+    {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t there = seen >> (16 * (e >> 2) + 4 * g + (e & 3)) & 1 ? ~0u : 0u;
+#pragma unroll
+            for (int j = 0; j < G::NV; ++j) v[e][j] &= there;
+        }
     }
 
-    // s -> weights exp2(c s - m); the running maximum grows only when a score passes it by
-    // more than 2^8, so that the accumulators are seldom rescaled.
-    __device__ __forceinline__ void weigh(f32x4 (&s)[MT][2])
+    // s -> weights exp2(c s - m), for TP tiles at once; the running maximum grows only when a
+    // score passes it by more than 2^8, so that the accumulators are seldom rescaled.
+    template <int TP> __device__ __forceinline__ void weigh(f32x4 (&s)[TP][MT][2])
     {
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
-            float top = s[mt][0][0];
+            float top = s[0][mt][0][0];
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int t = 0; t < TP; ++t)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) top = fmaxf(top, s[mt][h][i]);
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][mt][h][i]);
             top = c * max_over_groups(top);
             if (__any(top > m[mt] + 8.f)) {
                 const float now = fmaxf(m[mt], top);
@@ -243,12 +252,14 @@ template <typename T, int D, int MT, bool SPLITP> struct Wave {
             }
             const float base = m[mt] == -INFINITY ? 0.f : m[mt];
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int t = 0; t < TP; ++t)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    s[mt][h][i] = fexp2(fmaf(s[mt][h][i], c, -base));
-                    l[mt] += s[mt][h][i];
-                }
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        s[t][mt][h][i] = fexp2(fmaf(s[t][mt][h][i], c, -base));
+                        l[mt] += s[t][mt][h][i];
+                    }
         }
     }
 
@@ -473,14 +484,15 @@ __device__ __forceinline__ void attend_nodes(Wave<T, D, MT, SPLITP> &w, const At
                 fine &= finite_words(v[e][j], sizeof(T) == 4);
             }
         }
-        f32x4 s[MT][2];
+        f32x4 st[1][MT][2];
+        f32x4(&s)[MT][2] = st[0];
         w.scores(s, k);
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 if (!(sees[mt] >> (n0 + 16 * (e >> 2) + 4 * g + (e & 3)) & 1)) s[mt][e >> 2][e & 3] = -INFINITY;
-        w.weigh(s);
+        w.weigh(st);
         if (__any(!fine)) {
             // Values that are not finite: a weight of zero does not take them out of a
             // product, so they are left out of it and added where they are seen.
@@ -539,7 +551,7 @@ __device__ __forceinline__ void join_waves(Wave<T, D, MT, SPLITP> &w, f32x4 (*s_
 #pragma unroll
                 for (int t = 0; t < G::NT; ++t) s_o[at][t][lane] = w.o[mt][t];
             }
-            __syncthreads();
+            lds_barrier();
             if (kw < step) {
                 const float m = s_ml[at][0][lane], top = fmaxf(w.m[mt], m), base = top == -INFINITY ? 0.f : top;
                 const float f0 = fexp2(w.m[mt] - base), f1 = fexp2(m - base);
@@ -548,7 +560,7 @@ __device__ __forceinline__ void join_waves(Wave<T, D, MT, SPLITP> &w, f32x4 (*s_
 #pragma unroll
                 for (int t = 0; t < G::NT; ++t) w.o[mt][t] = w.o[mt][t] * f0 + s_o[at][t][lane] * f1;
             }
-            __syncthreads();
+            lds_barrier();
         }
     }
 }

@@ -59,7 +59,8 @@ __global__ void __launch_bounds__(64 * kWaves, waves_per_simd(sizeof(T) == 2, D,
         }
         sign_rows(w, a);
         for (int t = t0; t < t1; t += KW) {
-            f32x4 s[MT][2];
+            f32x4 st[1][MT][2];
+            f32x4(&s)[MT][2] = st[0];
             w.scores(s, k);
             const uint32_t seen = tl.seen;
             const bool more = t + KW < t1;
@@ -68,8 +69,11 @@ __global__ void __launch_bounds__(64 * kWaves, waves_per_simd(sizeof(T) == 2, D,
                 tl.keys(k, g, rr);
                 if (t + 2 * KW < t1) tl.look_up(t + 2 * KW);
             }
-            if (seen != ~0u) w.hide(s, v, seen, g);
-            w.weigh(s);
+            if (seen != ~0u) {
+                w.hide(s, seen, g);
+                w.hide(v, seen, g);
+            }
+            w.weigh(st);
             w.values(s, v);
             if (more) tl.template values<G::VB>(v, g, rr);
         }

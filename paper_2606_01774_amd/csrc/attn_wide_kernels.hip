@@ -23,9 +23,11 @@ template <int D, int RW> struct Wide {
     static constexpr int CH = D / 8;                    // chunks of a row
     static constexpr int W = 4;                         // waves
     static constexpr int KW = W / RW;
-    static constexpr int STAGE = KW * 64 * CH;          // chunks of a stage: KW x (keys, values) x 32 rows
-    static constexpr int LOADS = CH / RW;               // of a wave for a stage, 64 chunks each
-    static constexpr int S = D == 256 ? (RW == 4 ? 4 : 2) : 65536 / (STAGE * 16) > 6 ? 6 : 65536 / (STAGE * 16);
+    static constexpr int TP = D == 256 ? 1 : 2 / KW;    // tiles that a wave takes at once
+    static constexpr int TILES = KW * TP;               // of a stage
+    static constexpr int STAGE = TILES * 64 * CH;       // chunks of a stage: tiles x (keys, values) x 32 rows
+    static constexpr int LOADS = TILES * CH / W;        // of a wave for a stage, 64 chunks each
+    static constexpr int S = (D == 256 ? 131072 : 65536) / (STAGE * 16);
     static constexpr int JOIN = (KW / 2) * RW * (D / 16 * 1024 + 512);
     static constexpr int LDS = S * STAGE * 16 > JOIN ? S * STAGE * 16 : JOIN;
     static __device__ __forceinline__ int place(int c, int key) { return c ^ (CH == 8 ? (key >> 1) & 7 : key & 15); }
@@ -43,9 +45,9 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) bdgdn_tree_attn_wide_ke
     typedef __bf16 T;
     typedef Geo<T, D> G;
     typedef Wide<D, RW> X;
-    constexpr int CH = X::CH, KW = X::KW, S = X::S, LOADS = X::LOADS, ROWS = 64 / CH;   // rows of one load
+    constexpr int CH = X::CH, KW = X::KW, TP = X::TP, S = X::S, LOADS = X::LOADS, ROWS = 64 / CH;   // rows of one load
     extern __shared__ u32x4 lds[];
-    __shared__ uint32_t s_seen[S][KW][2];
+    __shared__ uint32_t s_seen[S][X::TILES][2];
     const int wave = wave_id(), kw = wave / RW, rw = wave % RW;
     // workgroups with the same keys and other rows are neighbours on one XCD (their numbers
     // are equal modulo 8)
@@ -57,7 +59,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) bdgdn_tree_attn_wide_ke
     const int row0 = (rg * RW + rw) * 32;   // of this wave's rows
 
     // this wave's share of a stage: rows [first, first + LOADS ROWS) of the keys or the values of one tile
-    const int block = wave * LOADS, lkw = block / CH, first = block % (CH / 2) * ROWS;
+    const int block = wave * LOADS, ltile = block / CH, first = block % (CH / 2) * ROWS;
     const bool is_value = block / (CH / 2) & 1;
     const unsigned char *pool = static_cast<const unsigned char *>(is_value ? a.vp : a.kp) + (long)kvh * a.head_stride;
     for (; span.pos < span.end; next_piece(a, span)) {
@@ -79,17 +81,17 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) bdgdn_tree_attn_wide_ke
         const int count = a.count ? min(max(a.count[it.r], 0), a.N) : a.N;
         if (span.off == 0 && kvh == 0 && rg == 0 && threadIdx.x == 0) note_request(a, span);
         const TablePtr table = table_of(a, it.r);
-        const int n = (it.t1 - it.t0 + KW - 1) / KW;   // stages
+        const int n = (it.t1 - it.t0 + X::TILES - 1) / X::TILES;   // stages
         int pages[2];
         const auto look_up = [&](int i) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int t = it.t0 + i * KW + lkw, tok = t * kTile + 16 * h;
+                const int t = it.t0 + i * X::TILES + ltile, tok = t * kTile + 16 * h;
                 pages[h] = t < it.t1 && tok < it.len ? table[column(a, tok)] : -1;
             }
         };
         const auto request = [&](int i) {
-            const int tok0 = (it.t0 + i * KW + lkw) * kTile;
+            const int tok0 = (it.t0 + i * X::TILES + ltile) * kTile;
             const int buf = i % S;
             const unsigned char *at[2];
 #pragma unroll
@@ -99,7 +101,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) bdgdn_tree_attn_wide_ke
                 const uint32_t where = there ? pages[h] * a.page16 + (uint32_t)(tok - column(a, tok) * a.page) * a.token16 : 0;
                 at[h] = pool + (long)where * 16;
                 if (!is_value && lane == 0)
-                    s_seen[buf][lkw][h] = !there ? 0u : it.len - tok >= 16 ? 0xffffu : (1u << (it.len - tok)) - 1;
+                    s_seen[buf][ltile][h] = !there ? 0u : it.len - tok >= 16 ? 0xffffu : (1u << (it.len - tok)) - 1;
             }
 #pragma unroll
             for (int l = 0; l < LOADS; ++l) {
@@ -129,33 +131,47 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) bdgdn_tree_attn_wide_ke
                 request(i + S - 1);
                 if (i + S < n) look_up(i + S);
             }
-            const uint32_t seen = __builtin_amdgcn_readfirstlane(s_seen[buf][kw][0] | s_seen[buf][kw][1] << 16);
-            const u32x4 *kt = lds + buf * X::STAGE + kw * 64 * CH;
-            const unsigned char *vt = reinterpret_cast<const unsigned char *>(kt + 32 * CH);
+            uint32_t seen[TP], any = 0;
+#pragma unroll
+            for (int tp = 0; tp < TP; ++tp) {
+                const int tile = kw + tp * KW;
+                seen[tp] = __builtin_amdgcn_readfirstlane(s_seen[buf][tile][0] | s_seen[buf][tile][1] << 16);
+                any |= seen[tp];
+            }
+            const u32x4 *stage = lds + buf * X::STAGE + kw * 64 * CH;
             buf = buf + 1 == S ? 0 : buf + 1;
-            if (!seen) continue;
-            u32x4 k[2][G::NK], v[8][G::NV];
+            if (!any) continue;
+            f32x4 s[TP][2][2];
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int tp = 0; tp < TP; ++tp) {
+                u32x4 k[2][G::NK];
 #pragma unroll
-                for (int j = 0; j < G::NK; ++j) k[h][j] = kt[16 * h * CH + ko[j]];
-            f32x4 s[2][2];
-            w.scores(s, k);
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-#pragma unroll
-                for (int j = 0; j < G::NV; ++j) {
-                    const unsigned char *p = vt + (e >> 2) * 16 * CH * 16 + vo[e & 3] + 256 * j;
-                    if constexpr (CH == 8) {
-                        const u32x2v z = *reinterpret_cast<const u32x2v *>(p);
-                        v[e][j] = u32x4{z[0], z[1], 0, 0};
-                    } else {
-                        v[e][j] = *reinterpret_cast<const u32x4 *>(p);
-                    }
-                }
-            if (seen != ~0u) w.hide(s, v, seen, g);
+                    for (int j = 0; j < G::NK; ++j) k[h][j] = stage[tp * KW * 64 * CH + 16 * h * CH + ko[j]];
+                w.scores(s[tp], k);
+                if (seen[tp] != ~0u) w.hide(s[tp], seen[tp], g);
+            }
             w.weigh(s);
-            w.values(s, v);
+#pragma unroll
+            for (int tp = 0; tp < TP; ++tp) {
+                u32x4 v[8][G::NV];
+                const unsigned char *vt = reinterpret_cast<const unsigned char *>(stage + tp * KW * 64 * CH + 32 * CH);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+#pragma unroll
+                    for (int j = 0; j < G::NV; ++j) {
+                        const unsigned char *p = vt + (e >> 2) * 16 * CH * 16 + vo[e & 3] + 256 * j;
+                        if constexpr (CH == 8) {
+                            const u32x2v z = *reinterpret_cast<const u32x2v *>(p);
+                            v[e][j] = u32x4{z[0], z[1], 0, 0};
+                        } else {
+                            v[e][j] = *reinterpret_cast<const u32x4 *>(p);
+                        }
+                    }
+                if (seen[tp] != ~0u) w.hide(v, seen[tp], g);
+                w.values(s[tp], v);
+            }
         }
         if (it.nodes && kw == KW - 1) attend_nodes(w, a, it.r, kvh, count, node, g, rr);
         __syncthreads();   // the stages are read: their memory is free
