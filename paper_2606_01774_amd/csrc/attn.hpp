@@ -64,10 +64,11 @@ __device__ __forceinline__ float max_over_groups(float x)
     return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
-// The keys of all requests in one row, a request's cached tiles followed by its nodes (which
-// count as one tile), are cut into equal ranges, one to a workgroup (of each key head and row
-// group), whatever the requests' lengths.  A range holds the end of one request, whole ones and
-// the beginning of another.
+// The work of all requests in one row, a request's cached tiles followed by its nodes, is cut
+// into equal ranges, one to a workgroup (of each key head and row group), whatever the requests'
+// lengths.  A range holds the end of one request, whole ones and the beginning of another.  The
+// nodes, with the queries and the output, count as a.node_units tiles: what a request costs
+// whatever its length.
 struct Range {
     int pos, end;              // what is left of the range
     int size;                  // of every range
@@ -86,8 +87,8 @@ __device__ __forceinline__ int tiles_of(int len) { return (len + kTile - 1) / kT
 __device__ __forceinline__ Range find_range(const AttnArgs &a, int w, int lane)
 {
     const int len0 = lane < a.R ? length_of(a, lane) : 0;
-    int sum = lane < a.R ? tiles_of(len0) + 1 : 0;
-    for (int r = lane + 64; r < a.R; r += 64) sum += tiles_of(length_of(a, r)) + 1;
+    int sum = lane < a.R ? tiles_of(len0) + a.node_units : 0;
+    for (int r = lane + 64; r < a.R; r += 64) sum += tiles_of(length_of(a, r)) + a.node_units;
 #pragma unroll
     for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
     sum = __builtin_amdgcn_readfirstlane(sum);
@@ -102,7 +103,7 @@ __device__ __forceinline__ Range find_range(const AttnArgs &a, int w, int lane)
     for (int r0 = 0; r0 < a.R; r0 += 64) {
         const int r = r0 + lane;
         const int len = r0 == 0 ? len0 : r < a.R ? length_of(a, r) : 0;
-        const int n = r < a.R ? tiles_of(len) + 1 : 0;
+        const int n = r < a.R ? tiles_of(len) + a.node_units : 0;
         int inc = n;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
@@ -124,22 +125,24 @@ __device__ __forceinline__ Range find_range(const AttnArgs &a, int w, int lane)
     return g;
 }
 
-// What a workgroup does with one request: tiles t0 .. t1 - 1, the nodes where `nodes`.
+// What a workgroup does with one request: tiles t0 .. t1 - 1, the nodes where `nodes` (they are
+// done where the first of their units lies); nothing where only later units are left.
 struct Piece {
     int r, len, t0, t1;
-    bool nodes, whole;         // whole: the request's only piece
+    bool nodes, none, whole;   // whole: the request's only piece
     int part;                  // else its place among the parts: 2 w for a range's first piece, 2 w + 1
 };
 
-__device__ __forceinline__ Piece piece_of(const Range &g, int w)
+__device__ __forceinline__ Piece piece_of(const AttnArgs &a, const Range &g, int w)
 {
     Piece p;
-    const int n = min(g.tiles + 1 - g.off, g.end - g.pos);
+    const int end = g.off + min(g.tiles + a.node_units - g.off, g.end - g.pos);
     p.r = g.r;
     p.len = g.len;
-    p.t0 = g.off;
-    p.nodes = g.off + n == g.tiles + 1;
-    p.t1 = p.nodes ? g.tiles : g.off + n;
+    p.t0 = min(g.off, g.tiles);
+    p.t1 = min(end, g.tiles);
+    p.none = g.off > g.tiles;
+    p.nodes = !p.none && end > g.tiles;
     p.whole = p.nodes && g.off == 0;
     p.part = 2 * w + (g.pos != (long)w * g.size);
     return p;
@@ -147,7 +150,7 @@ __device__ __forceinline__ Piece piece_of(const Range &g, int w)
 
 __device__ __forceinline__ void next_piece(const AttnArgs &a, Range &g)
 {
-    g.pos += min(g.tiles + 1 - g.off, g.end - g.pos);
+    g.pos += min(g.tiles + a.node_units - g.off, g.end - g.pos);
     if (g.pos >= g.end) return;
     ++g.r;
     g.off = 0;

@@ -37,7 +37,8 @@ __global__ void __launch_bounds__(64 * kWaves, waves_per_simd(sizeof(T) == 2, D,
     const int row0 = (rg * a.RW + rw) * 16 * MT;   // of this wave's rows
     for (; span.pos < span.end; next_piece(a, span)) {
         const int lane = lane_anew(), g = lane >> 4, rr = lane & 15;
-        const Piece it = piece_of(span, range);
+        const Piece it = piece_of(a, span, range);
+        if (it.none) continue;
         const int count = a.count ? min(max(a.count[it.r], 0), a.N) : a.N;
         if (span.off == 0 && kvh == 0 && rg == 0 && threadIdx.x == 0) note_request(a, span);
         w.init(a.c);
@@ -213,6 +214,7 @@ hipError_t launch_tree_attn(bool bf16, bool f32_out, int d, const AttnPlan &p, A
     a.RG = p.RG;
     a.ranges = p.ranges;
     a.least = p.least;
+    a.node_units = 4 + p.RW * p.mt / 2;
     a.rows_padded = p.rows_padded;
     char *ws = static_cast<char *>(workspace);
     a.info = reinterpret_cast<int32_t *>(ws);

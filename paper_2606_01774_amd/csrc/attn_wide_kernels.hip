@@ -77,7 +77,8 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) bdgdn_tree_attn_wide_ke
 #pragma unroll
         for (int i = 0; i < 4; ++i) vo[i] = CH == 8 ? ((4 * g + i) * CH + X::place(rr >> 1, 4 * g + i)) * 16 + (rr & 1) * 8
                                                     : ((4 * g + i) * CH + X::place(rr, 4 * g + i)) * 16;
-        const Piece it = piece_of(span, range);
+        const Piece it = piece_of(a, span, range);
+        if (it.none) continue;
         const int count = a.count ? min(max(a.count[it.r], 0), a.N) : a.N;
         if (span.off == 0 && kvh == 0 && rg == 0 && threadIdx.x == 0) note_request(a, span);
         const TablePtr table = table_of(a, it.r);
@@ -115,14 +116,14 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) bdgdn_tree_attn_wide_ke
         if (n > 0) look_up(0);
         w.init(a.c);
         int node[2];
-        load_rows(w, a, it.r, kvh, row0, node, g, rr);
-        sign_rows(w, a);
 #pragma unroll
         for (int i = 0; i < S - 1; ++i)
             if (i < n) {
                 request(i);
                 if (i + 1 < n) look_up(i + 1);
             }
+        load_rows(w, a, it.r, kvh, row0, node, g, rr);
+        sign_rows(w, a);
         int buf = 0;
         for (int i = 0; i < n; ++i) {
             if (n - 1 - i >= S - 2) wait_loads_barrier<(S - 2) * LOADS>();

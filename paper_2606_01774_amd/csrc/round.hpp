@@ -29,6 +29,7 @@ struct AttnArgs {
     uint32_t q_and, q_xor;     // applied to the words of q: the scale's sign, or zero
     int RW, RG;                // waves of a workgroup, and workgroups, with other rows of a key head
     int rows_padded;           // rows of a key head, filled up to those of RW x RG waves
+    int node_units;            // tiles that a request's nodes, queries and output count as
     int ranges, least;         // ranges that the keys are cut into, at most, and their tiles, at least
 };
 
