@@ -17,7 +17,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libbdgdn.so")
 SOURCES = ["api.hip", "fwd_kernels.hip", "fwd_scan_kernels.hip", "fused_kernels.hip", "serve_kernels.hip",
            "split_kernels.hip", "conv_kernels.hip", "bwd_kernels.hip", "chunked_kernels.hip",
-           "bwd_generic.hip", "bwd_steps.hip", "bwd_scan.hip", "attn_kernels.hip", "attn_wide_kernels.hip",
+           "bwd_generic.hip", "bwd_steps.hip", "bwd_scan.hip", "attn_kernels.hip", "attn_staged_kernels.hip",
            "verify_kernels.hip",
            "cache_kernels.hip", "round_api.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -32,7 +32,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-I" + INCLUDE, 
 EXTRA = {"chunked_kernels.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
          "bwd_scan.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
          "attn_kernels.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
-         "attn_wide_kernels.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+         "attn_staged_kernels.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 
 def _compile(src: str, objdir: str) -> str:

@@ -1,12 +1,13 @@
 // attn_kernels.hip -- attention of a block of nodes over a paged cache and over the nodes
-// themselves: the kernel for few rows, the joining kernel, tree masks, dispatch.
+// themselves: the kernel for fp32 and for pages of any size, the joining kernel, tree masks,
+// dispatch.  (bf16 over pages of whole runs of 16 tokens takes the kernel of
+// attn_staged_kernels.hip, which is never slower: one node on 64 requests of up to 4096 tokens
+// 112 against 114 us, four 119 against 122, eight 128 against 135, 32 157 against 259.)
 //
 // One wave streams its tiles from memory to registers, the next keys requested when the scores
 // are done with these and the next values when the output is.  Four waves are a workgroup:
 // those with different rows take the same keys, those with the same rows every KW-th tile,
-// and are joined through LDS.  The keys of all requests are cut into equal ranges, as many as
-// the chip holds workgroups (attn.hpp), so that it is busy to the end whatever the requests'
-// lengths; a second kernel joins (maximum, sum, output) of requests in several ranges.
+// and are joined through LDS.  Latency bounds it: a wave has one tile on its way at a time.
 #include <type_traits>
 
 #include "attn.hpp"
@@ -156,15 +157,15 @@ __global__ void __launch_bounds__(64) bdgdn_tree_mask_kernel(int N, const int32_
     }
 }
 
-// 16-row groups of a wave at most (bf16 calls with more rows take the wide kernel where the
-// pages allow it): what its registers hold, 512 a lane.
+// 16-row groups of a wave at most: what its registers hold, 512 a lane.
 constexpr int most_mt(bool bf16, int d) { return d == 256 ? 1 : bf16 ? 4 : 2; }
 
 template <typename T, int D, int MT, bool F32OUT> hipError_t launch_m(const AttnPlan &p, const AttnArgs &a, hipStream_t s)
 {
     constexpr bool SP = sizeof(T) == 2 && F32OUT;
     typedef typename std::conditional<F32OUT, float, __bf16>::type Out;
-    if (a.page % 16 == 0) bdgdn_tree_attn_kernel<T, D, MT, SP, true, Out><<<p.grid, 64 * kWaves, 0, s>>>(a);
+    constexpr bool HALVES = sizeof(T) == 4;   // (bf16 over such pages is the staged kernel's)
+    if (HALVES && a.page % 16 == 0) bdgdn_tree_attn_kernel<T, D, MT, SP, HALVES, Out><<<p.grid, 64 * kWaves, 0, s>>>(a);
     else bdgdn_tree_attn_kernel<T, D, MT, SP, false, Out><<<p.grid, 64 * kWaves, 0, s>>>(a);
     return hipGetLastError();
 }
@@ -172,7 +173,7 @@ template <typename T, int D, int MT, bool F32OUT> hipError_t launch_m(const Attn
 template <typename T, int D, bool F32OUT> hipError_t launch_d(const AttnPlan &p, const AttnArgs &a, hipStream_t s)
 {
     constexpr int most = most_mt(sizeof(T) == 2, D);
-    hipError_t e = p.wide ? launch_tree_attn_wide(F32OUT, D, p.grid, a, s)
+    hipError_t e = p.staged ? launch_tree_attn_staged(F32OUT, D, p.grid, a, s)
                    : p.mt == 1 ? launch_m<T, D, 1, F32OUT>(p, a, s)
                    : p.mt == 2 ? launch_m<T, D, (most < 2 ? most : 2), F32OUT>(p, a, s)
                                : launch_m<T, D, most, F32OUT>(p, a, s);
@@ -189,15 +190,17 @@ AttnPlan attn_plan(bool bf16, int d, int page, int R, int N, int h_q, int h_kv)
 {
     AttnPlan p;
     const int M = N * (h_q / h_kv);
-    p.wide = bf16 && page % 16 == 0 && M > (d == 256 ? 16 : 32);
-    const int groups = M <= 16 ? 1 : M <= 32 ? 2 : 4, most = p.wide ? 2 : most_mt(bf16, d);
-    p.mt = groups < most ? groups : most;
+    p.staged = bf16 && page % 16 == 0;
+    // a staged wave always has 32 rows, idle ones load for the others; a streaming wave has as
+    // many 16-row groups as the rows fill, and waves without rows take tiles instead
+    const int groups = M <= 16 ? 1 : M <= 32 ? 2 : 4, most = most_mt(bf16, d);
+    p.mt = p.staged ? 2 : groups < most ? groups : most;
     const int waves = (M + 16 * p.mt - 1) / (16 * p.mt);
-    p.RW = waves <= 1 && !p.wide ? 1 : waves <= 2 ? 2 : 4;
+    p.RW = waves <= 1 && !p.staged ? 1 : waves <= 2 ? 2 : 4;
     p.RG = (waves + p.RW - 1) / p.RW;
     p.rows_padded = p.RG * p.RW * 16 * p.mt;
     // one range for every workgroup that the chip holds at once (one or two to a compute unit)
-    const long heads = (long)h_kv * p.RG, ranges = 256 * (p.wide ? (d == 256 ? 1 : 2) : waves_per_simd(bf16, d, p.mt)) / heads;
+    const long heads = (long)h_kv * p.RG, ranges = 256 * (p.staged ? (d == 256 ? 1 : 2) : waves_per_simd(bf16, d, p.mt)) / heads;
     p.ranges = (int)(ranges < 1 ? 1 : ranges);
     p.least = 4;   // tiles of a range, one to a wave
     p.grid = (int)(((long)p.ranges * h_kv + 7) / 8 * 8 * p.RG);

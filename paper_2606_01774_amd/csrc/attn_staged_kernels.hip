@@ -1,12 +1,21 @@
-// attn_wide_kernels.hip -- attention of a block of nodes over a paged cache: the kernel for many
-// rows to a key head (bf16, pages of whole runs of 16 tokens).
+// attn_staged_kernels.hip -- attention of a block of nodes over a paged cache: the kernel for bf16
+// over pages of whole runs of 16 tokens.
 //
-// Eight waves (four with heads of 256) are a workgroup of RW x KW: RW waves have 32 rows each and
-// read the same tiles, KW take different tiles.  Tiles go from memory to LDS without passing
-// through registers, S stages deep, one barrier a stage; a stage is KW tiles of 32 keys and
-// values.  A row of D elements is D / 8 chunks of 16 bytes; chunk c of key x lies at place
-// c ^ (x & 15) of its row (c ^ (x / 2 & 7) in rows of 8 chunks), so that the 16 lanes that read one chunk of
-// 16 keys, and those that read 16 chunks of one key, meet different banks.
+// Four waves are a workgroup of RW x KW: RW (two or four) have 32 rows each and read the same
+// tiles, KW take different tiles.  Tiles go from memory to LDS without passing through
+// registers, S stages of two tiles (one where heads of 256 and four row waves need the room),
+// one barrier a stage; the softmax takes a wave's tiles of a stage in one turn.  Two workgroups
+// share a compute unit (one with heads of 256, whose accumulators need the registers), so that
+// the ends of one's pieces and its barriers pass while the other computes.  A row of D elements
+// is D / 8 chunks of 16 bytes; chunk c of key x lies at place c ^ (x & 15) of its row
+// (c ^ (x / 2 & 7) in rows of 8 chunks), so that the 16 lanes that read one chunk of 16 keys, and
+// those that read 16 chunks of one key, meet different banks.
+//
+// What bounds it: memory, up to 32 nodes or so.  With the products taken out of a copy, the
+// loads alone of 64 requests of 2048 tokens (32 query heads on 8 of 128, 32 nodes) took 116 of
+// 123 us; one node on 64 requests of up to 4096 takes 112 us, 5.0 TB/s.  From 64 nodes
+// on the products do: 580 TFLOP/s, the vector units busy half the time and the matrix units a
+// quarter.
 #include <mutex>
 #include <type_traits>
 
@@ -19,7 +28,7 @@ namespace {
 typedef __attribute__((address_space(1))) const void *GlobalPtr;
 typedef __attribute__((address_space(3))) void *LdsPtr;
 
-template <int D, int RW> struct Wide {
+template <int D, int RW> struct Staged {
     static constexpr int CH = D / 8;                    // chunks of a row
     static constexpr int W = 4;                         // waves
     static constexpr int KW = W / RW;
@@ -40,11 +49,11 @@ template <int N> __device__ __forceinline__ void wait_loads_barrier()
 }
 
 template <int D, int RW, bool SPLITP, typename Out>
-__global__ void __launch_bounds__(256, D == 256 ? 1 : 2) bdgdn_tree_attn_wide_kernel(AttnArgs a)
+__global__ void __launch_bounds__(256, D == 256 ? 1 : 2) bdgdn_tree_attn_staged_kernel(AttnArgs a)
 {
     typedef __bf16 T;
     typedef Geo<T, D> G;
-    typedef Wide<D, RW> X;
+    typedef Staged<D, RW> X;
     constexpr int CH = X::CH, KW = X::KW, TP = X::TP, S = X::S, LOADS = X::LOADS, ROWS = 64 / CH;   // rows of one load
     extern __shared__ u32x4 lds[];
     __shared__ uint32_t s_seen[S][X::TILES][2];
@@ -57,6 +66,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) bdgdn_tree_attn_wide_ke
     Range span = find_range(a, range, threadIdx.x & 63);
     Wave<T, D, 2, SPLITP> w;
     const int row0 = (rg * RW + rw) * 32;   // of this wave's rows
+    const bool idle = row0 >= a.N * a.G;    // it has none, and only loads
 
     // this wave's share of a stage: rows [first, first + LOADS ROWS) of the keys or the values of one tile
     const int block = wave * LOADS, ltile = block / CH, first = block % (CH / 2) * ROWS;
@@ -141,7 +151,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) bdgdn_tree_attn_wide_ke
             }
             const u32x4 *stage = lds + buf * X::STAGE + kw * 64 * CH;
             buf = buf + 1 == S ? 0 : buf + 1;
-            if (!any) continue;
+            if (!any || idle) continue;
             f32x4 s[TP][2][2];
 #pragma unroll
             for (int tp = 0; tp < TP; ++tp) {
@@ -174,7 +184,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) bdgdn_tree_attn_wide_ke
                 w.values(s[tp], v);
             }
         }
-        if (it.nodes && kw == KW - 1) attend_nodes(w, a, it.r, kvh, count, node, g, rr);
+        if (it.nodes && kw == KW - 1 && !idle) attend_nodes(w, a, it.r, kvh, count, node, g, rr);
         __syncthreads();   // the stages are read: their memory is free
         if constexpr (KW > 1) {
             f32x4(*s_o)[G::NT][64] = reinterpret_cast<f32x4(*)[G::NT][64]>(lds);
@@ -187,10 +197,10 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) bdgdn_tree_attn_wide_ke
 
 template <int D, int RW, bool SPLITP, typename Out> hipError_t launch(int grid, const AttnArgs &a, hipStream_t s)
 {
-    typedef Wide<D, RW> X;
+    typedef Staged<D, RW> X;
     static std::once_flag once;
     static hipError_t err;
-    const auto kernel = bdgdn_tree_attn_wide_kernel<D, RW, SPLITP, Out>;
+    const auto kernel = bdgdn_tree_attn_staged_kernel<D, RW, SPLITP, Out>;
     std::call_once(once, [&] {
         err = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, X::LDS);
     });
@@ -206,11 +216,11 @@ template <int D, bool SPLITP, typename Out> hipError_t launch_rw(int grid, const
 
 }  // namespace
 
-hipError_t launch_tree_attn_wide(bool f32_out, int d, int grid, const AttnArgs &a, hipStream_t s)
+hipError_t launch_tree_attn_staged(bool f32_out, int d, int grid, const AttnArgs &a, hipStream_t s)
 {
-#define BDGDN_WIDE(D) (f32_out ? launch_rw<D, true, float>(grid, a, s) : launch_rw<D, false, __bf16>(grid, a, s))
-    return d == 64 ? BDGDN_WIDE(64) : d == 128 ? BDGDN_WIDE(128) : BDGDN_WIDE(256);
-#undef BDGDN_WIDE
+#define BDGDN_STAGED(D) (f32_out ? launch_rw<D, true, float>(grid, a, s) : launch_rw<D, false, __bf16>(grid, a, s))
+    return d == 64 ? BDGDN_STAGED(64) : d == 128 ? BDGDN_STAGED(128) : BDGDN_STAGED(256);
+#undef BDGDN_STAGED
 }
 
 }  // namespace bdgdn
