@@ -512,7 +512,8 @@ typedef struct {
     int32_t n_pages;        /* pages of every pool                                        */
     int32_t page;           /* tokens of a page, 1 .. 65536                               */
     int32_t n_slots;        /* rows of page_table, entries of seq_len                     */
-    int32_t max_pages;      /* columns of page_table; max_pages * page < 2^31             */
+    int32_t max_pages;      /* columns of page_table; max_pages * page < 2^31 (for
+                               attention at most 2^31 - 2^16)                             */
     int32_t h_kv, d;        /* heads and head dimension of the pools                      */
     int32_t dtype;          /* bdgdn_dtype_t of the pools                                 */
     int64_t page_stride, token_stride, head_stride;   /* elements, multiples of 16 bytes;
@@ -538,7 +539,8 @@ typedef struct {
                                of the rows of one projection)                             */
 } bdgdn_attn_desc_t;
 
-/* Bytes of device workspace bdgdn_tree_attn needs, 0 for descriptors that it rejects. */
+/* Bytes of device workspace bdgdn_tree_attn needs, 0 for descriptors that it rejects (more
+ * than R (max_pages page / 32 + 9) = 2^31 - 2^16 tiles or R N h_q = 2^30 rows among them). */
 size_t bdgdn_tree_attn_workspace(const bdgdn_attn_desc_t *desc, const bdgdn_cache_desc_t *cache);
 
 /*

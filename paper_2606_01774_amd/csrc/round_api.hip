@@ -60,9 +60,11 @@ int check_attn(const bdgdn_attn_desc_t *d, const bdgdn_cache_desc_t *c)
     const int64_t stride[3] = {d->q_stride, d->k_stride, d->v_stride};
     for (int i = 0; i < 3; ++i)
         if (stride[i] != 0 && (stride[i] < least[i] || stride[i] % unit)) return BDGDN_ERR_INVALID_ARG;
-    // workgroups of the call, tiles of all requests
+    // token numbers up to some tiles past a sequence's end
+    if ((long)c->max_pages * c->page > 0x7fff0000L) return BDGDN_ERR_UNSUPPORTED;
+    // workgroups of the call; tiles of all requests, their nodes counting as eight at most
     if ((long)d->num_req * d->nodes * d->h_q > 0x40000000L ||
-        (long)d->num_req * ((long)c->max_pages * c->page / 32 + 2) > 0x7fffffffL)
+        (long)d->num_req * ((long)c->max_pages * c->page / 32 + 9) > 0x7fff0000L)
         return BDGDN_ERR_UNSUPPORTED;
     return BDGDN_OK;
 }

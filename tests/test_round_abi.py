@@ -60,6 +60,24 @@ def test_attention_rejects_bad_pointers(ptr, status):
     assert _call_attn(_attn(), _cache(), ptr=ptr) == status
 
 
+def test_attention_limits():
+    """Rows of tokens further apart than 32-bit offsets within a page allow, more tiles of keys
+    or more workgroups than 31 bits count."""
+    token = 1 << 25                                 # bf16 elements: 2^26 bytes
+    far = dict(n_pages=1, page=1, page_stride=token, max_pages=5)
+    assert bd.bdgdn_tree_attn_workspace(_attn(), _cache(token_stride=token, **far)) > 0
+    assert _call_attn(_attn(), _cache(token_stride=token + 8, **far)) == UNS
+    for page, columns, want in ((65536, 32767, bd.BDGDN_OK), (1, 0x7fff0001, UNS), (1, 0x7fffffff, UNS)):
+        cache = _cache(page=page, max_pages=columns)
+        got = bd.bdgdn_tree_attn_workspace(_attn(num_req=1), cache) > 0
+        assert got == (want == bd.BDGDN_OK) and (got or _call_attn(_attn(num_req=1), cache) == want)
+    # 65535 requests of 32764 tiles: 2^31 is passed by what their nodes count for
+    many = dict(num_req=65535, nodes=64, h_q=2)
+    assert bd.bdgdn_tree_attn_workspace(_attn(**many), _cache(n_slots=65535, max_pages=2 * 32700)) > 0
+    assert _call_attn(_attn(**many), _cache(n_slots=65535, max_pages=2 * 32764)) == UNS
+    assert _call_attn(_attn(num_req=65535, nodes=64, h_q=512), _cache(n_slots=65535)) == UNS
+
+
 def test_attention_checks_mask_and_workspace():
     assert _call_attn(_attn(), _cache(), mask=FAKE) == INV
     assert _call_attn(_attn(mask=bd.BDGDN_MASK_BITS), _cache()) == INV
