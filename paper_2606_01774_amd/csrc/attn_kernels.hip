@@ -85,46 +85,62 @@ __global__ void __launch_bounds__(64 * kWaves, waves_per_simd(sizeof(T) == 2, D,
     }
 }
 
-// One workgroup per (request, key head, 16 rows), 16 lanes to a row:
-// o = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s over the pieces s of a request.
-template <typename Out, int D> __global__ void __launch_bounds__(256) bdgdn_tree_attn_join_kernel(AttnArgs a, int row_tiles)
+// One workgroup per (request, key head, 16 / W rows), 16 lanes to a row, W waves to a row's
+// pieces:  o = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s over the pieces s of a request.
+template <typename Out, int D, int W> __global__ void __launch_bounds__(256) bdgdn_tree_attn_join_kernel(AttnArgs a, int row_tiles)
 {
     constexpr int C = D / 64;   // float4s of a lane
     const int tile = blockIdx.x % row_tiles, rest = blockIdx.x / row_tiles, kvh = rest % a.h_kv, r = rest / a.h_kv;
     const int size = a.info[0], pos = a.info[1 + 2 * r], w0 = pos / size, splits = (pos + a.info[2 + 2 * r] - 1) / size - w0 + 1;
     if (splits == 1) return;   // one piece, whose workgroup wrote the result
-    const int c = threadIdx.x & 15, lane = threadIdx.x & 63, row = tile * 16 + (threadIdx.x >> 4);
-    if (row >= a.N * a.G) return;
+    const int lane = threadIdx.x & 63, wave = wave_id(), part = wave % W, c = lane & 15;
+    const int row = tile * (16 / W) + wave / W * 4 + (lane >> 4);
+    const bool there = row < a.N * a.G;
     // the first piece ends its range unless it begins there too, the others begin theirs
     const int second = pos % size != 0;
     const auto place = [&](int s) {
         return ((long)(2 * (w0 + s) + (s == 0 ? second : 0)) * a.h_kv + kvh) * a.rows_padded + row;
     };
-    float top = -INFINITY;
-    for (int s = c; s < splits; s += 16) top = fmaxf(top, a.part_ml[2 * place(s)]);
-#pragma unroll
-    for (int o = 8; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-    const float ref = top == -INFINITY ? 0.f : top;
+    float top = -INFINITY, l = 0.f;
     f32x4 o[C] = {};
-    float l = 0.f;
-    for (int s0 = 0; s0 < splits; s0 += 16) {
-        float f = 0.f;
-        if (s0 + c < splits) {
-            const long at = place(s0 + c);
-            f = fexp2(a.part_ml[2 * at] - ref);
-            l += f * a.part_ml[2 * at + 1];
-        }
-        const int n = min(16, splits - s0);
-#pragma unroll 8
-        for (int i = 0; i < n; ++i) {
-            const float fi = __shfl(f, (lane & 48) + i);
-            const f32x4 *po = reinterpret_cast<const f32x4 *>(a.part_o + place(s0 + i) * D) + c;
+    if (there) {
+        // (each wave takes the maximum and the sum of all of them: only the outputs are many)
+        for (int s = c; s < splits; s += 16) top = fmaxf(top, a.part_ml[2 * place(s)]);
 #pragma unroll
-            for (int x = 0; x < C; ++x) o[x] += fi * po[16 * x];
+        for (int x = 8; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
+        const float ref = top == -INFINITY ? 0.f : top;
+        for (int s0 = 0; s0 < splits; s0 += 16) {
+            float f = 0.f;
+            if (s0 + c < splits) {
+                const long at = place(s0 + c);
+                f = fexp2(a.part_ml[2 * at] - ref);
+                l += f * a.part_ml[2 * at + 1];
+            }
+            const int n = min(16, splits - s0);
+#pragma unroll (W == 1 ? 8 : 4)
+            for (int i = part; i < n; i += W) {
+                const float fi = __shfl(f, (lane & 48) + i);
+                const f32x4 *po = reinterpret_cast<const f32x4 *>(a.part_o + place(s0 + i) * D) + c;
+#pragma unroll
+                for (int x = 0; x < C; ++x) o[x] += fi * po[16 * x];
+            }
         }
+#pragma unroll
+        for (int x = 8; x; x >>= 1) l += __shfl_xor(l, x);
     }
+    if (W > 1) {
+        __shared__ f32x4 s_o[W][C][64];
+        if (part)
 #pragma unroll
-    for (int x = 8; x; x >>= 1) l += __shfl_xor(l, x);
+            for (int x = 0; x < C; ++x) s_o[part][x][lane] = o[x];
+        __syncthreads();
+        if (part) return;
+#pragma unroll
+        for (int w = 1; w < W; ++w)
+#pragma unroll
+            for (int x = 0; x < C; ++x) o[x] += s_o[w][x][lane];
+    }
+    if (!there) return;
     const int n = row / a.G, count = a.count ? min(max(a.count[r], 0), a.N) : a.N;
     const bool none = n >= count || l == 0.f;
     const long at = ((long)r * a.N + n) * a.h_q + kvh * a.G + row - n * a.G;
@@ -178,9 +194,11 @@ template <typename T, int D, bool F32OUT> hipError_t launch_d(const AttnPlan &p,
                    : p.mt == 2 ? launch_m<T, D, (most < 2 ? most : 2), F32OUT>(p, a, s)
                                : launch_m<T, D, most, F32OUT>(p, a, s);
     if (e != hipSuccess) return e;
-    const int row_tiles = (a.N * a.G + 15) / 16;
     typedef typename std::conditional<F32OUT, float, __bf16>::type Out;
-    bdgdn_tree_attn_join_kernel<Out, D><<<a.R * a.h_kv * row_tiles, 256, 0, s>>>(a, row_tiles);
+    // four waves to a row where requests have eight pieces or more
+    const int M = a.N * a.G;
+    if (p.ranges >= 8 * a.R) bdgdn_tree_attn_join_kernel<Out, D, 4><<<a.R * a.h_kv * ((M + 3) / 4), 256, 0, s>>>(a, (M + 3) / 4);
+    else bdgdn_tree_attn_join_kernel<Out, D, 1><<<a.R * a.h_kv * ((M + 15) / 16), 256, 0, s>>>(a, (M + 15) / 16);
     return hipGetLastError();
 }
 
