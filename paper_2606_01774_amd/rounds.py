@@ -160,10 +160,19 @@ def _vector(t, name, n, dtype=_I32):
     return _p(t, name, dtype)
 
 
-def _scratch(workspace, need, device):
+def _empty(shape, dtype, device, stream):
+    """Memory of the stream that the call runs on: another stream's could be handed out again, or
+    still be in use there, while this one's kernels work on it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _scratch(workspace, need, device, stream):
     """(workspace, its size), allocated where none is given."""
     if workspace is None:
-        return torch.empty(need, dtype=torch.uint8, device=device), need
+        return _empty(need, torch.uint8, device, stream), need
     _p(workspace, "workspace")
     return workspace, workspace.numel() * workspace.element_size()
 
@@ -217,15 +226,15 @@ def bdgdn_tree_attn(q, k, v, k_pages, v_pages, page_table, seq_len, *, mask="ful
     R, N, h_q, _ = shape
     device = q.device
     if o is None:
-        o = torch.empty(shape, dtype=out_dtype, device=device)
+        o = _empty(shape, out_dtype, device, stream)
         po = o.data_ptr()
     else:
         if o.shape != shape:
             raise ValueError("o must have q's shape")
         po = _p(o, "o", out_dtype)
     if lse is None and want_lse:
-        lse = torch.empty((R, N, h_q), dtype=_F32, device=device)
-    workspace, size = _scratch(workspace, need, device)
+        lse = _empty((R, N, h_q), _F32, device, stream)
+    workspace, size = _scratch(workspace, need, device, stream)
     st = lib.bdgdn_tree_attn(desc, cache, q.data_ptr(), k.data_ptr(), v.data_ptr(), k_pages.data_ptr(),
                              v_pages.data_ptr(), _p(page_table, "page_table", _I32), _p(seq_len, "seq_len", _I32),
                              _vector(slot, "slot", R), _vector(count, "count", R),
@@ -244,9 +253,9 @@ def bdgdn_tree_mask(parent, *, mask=None, depth=None, want_depth=False, stream=N
         raise ValueError("parent must be [R, N]")
     R, N = parent.shape
     if mask is None:
-        mask = torch.empty(R, N, dtype=torch.int64, device=parent.device)
+        mask = _empty((R, N), torch.int64, parent.device, stream)
     if depth is None and want_depth:
-        depth = torch.empty_like(parent)
+        depth = _empty(parent.shape, _I32, parent.device, stream)
     st = lib.bdgdn_tree_mask(R, N, pp, _vector(mask, "mask", R * N, torch.int64), _vector(depth, "depth", R * N),
                              _stream(stream))
     _check(st, "bdgdn_tree_mask")
@@ -297,14 +306,14 @@ def bdgdn_verify(target, token, u, noise, *, draft=None, parent=None, count=None
         draft = None
     dev = target.device
     if n_accept is None:
-        n_accept = torch.empty(R, dtype=_I32, device=dev)
+        n_accept = _empty(R, _I32, dev, stream)
     if path is None:
-        path = torch.empty(R, N, dtype=_I32, device=dev)
+        path = _empty((R, N), _I32, dev, stream)
     if next_token is None:
-        next_token = torch.empty(R, dtype=_I32, device=dev)
+        next_token = _empty(R, _I32, dev, stream)
     if n_path is None and want_n_path:
-        n_path = torch.empty(R, dtype=_I32, device=dev)
-    workspace, size = _scratch(workspace, need, dev)
+        n_path = _empty(R, _I32, dev, stream)
+    workspace, size = _scratch(workspace, need, dev, stream)
     st = lib.bdgdn_verify(desc, target.data_ptr(), None if draft is None else draft.data_ptr(),
                           _vector(token, "token", R * N), _vector(parent, "parent", R * N), _vector(count, "count", R),
                           _vector(temperature, "temperature", R, _F32), _vector(u, "u", R * N, _F32), noise.data_ptr(),
@@ -349,8 +358,8 @@ def bdgdn_cache_append(tables, pools, rows, slot, count, *, path=None, status=No
                                      r0.stride())
     device = p0.device
     if status is None:
-        status = torch.empty(R, dtype=_I32, device=device)
-    workspace, size = _scratch(workspace, need, device)
+        status = _empty(R, _I32, device, stream)
+    workspace, size = _scratch(workspace, need, device, stream)
     st = lib.bdgdn_cache_append(desc, _tables(tables), pool_ptrs, row_ptrs, n, R, N, stride, _vector(slot, "slot", R),
                                 _vector(path, "path", R * N), _vector(count, "count", R), _vector(status, "status", R),
                                 workspace.data_ptr(), size, _stream(stream))
@@ -363,7 +372,7 @@ def bdgdn_cache_fork(tables, src, dst, *, page, status=None, stream=None):
     lib = load_library()
     n = src.numel()
     if status is None:
-        status = torch.empty(n, dtype=_I32, device=src.device)
+        status = _empty(n, _I32, src.device, stream)
     st = lib.bdgdn_cache_fork(_table_desc(*tables.page_table.shape, tables.refcount.numel(), int(page)), _tables(tables), n,
                               _p(src, "src", _I32), _vector(dst, "dst", n), _vector(status, "status", n), _stream(stream))
     _check(st, "bdgdn_cache_fork")
@@ -382,8 +391,8 @@ def bdgdn_cache_compact(tables, pools, slot, keep, count, *, status=None, worksp
     R, M = keep.shape
     desc, need, _ = _pools_plan(tables[0].shape, tables[2].numel(), p0.shape, p0.stride(), p0.dtype, R, M, None, None)
     if status is None:
-        status = torch.empty(R, dtype=_I32, device=p0.device)
-    workspace, size = _scratch(workspace, need, p0.device)
+        status = _empty(R, _I32, p0.device, stream)
+    workspace, size = _scratch(workspace, need, p0.device, stream)
     st = lib.bdgdn_cache_compact(desc, _tables(tables), ptrs, len(pools), R, M, _vector(slot, "slot", R), pk,
                                  _vector(count, "count", R), _vector(status, "status", R), workspace.data_ptr(), size,
                                  _stream(stream))

@@ -16,6 +16,8 @@ import pytest
 import torch
 
 import oracle
+import paper_2606_01774_amd as bd
+from paper_2606_01774_amd import rounds
 
 pytestmark = pytest.mark.gpu
 
@@ -167,3 +169,54 @@ def test_trees_need_attention_layers():
     with pytest.raises(ValueError, match="chain"):
         model.tree_round(torch.zeros(1, dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda"),
                          [2])
+
+
+def _calls():
+    """Calls with temporaries of their own, on tensors made beforehand: (name, call(stream) ->
+    results, its workspace's bytes)."""
+    gen = torch.Generator(device="cuda").manual_seed(5)
+
+    def rand(*shape, dtype=torch.bfloat16):
+        return torch.randn(*shape, generator=gen, device="cuda").to(dtype)
+
+    R, N, V = 4, 8, 4096
+    model = sd.Decoder("a", slots=R, max_len=4096)
+    slot = torch.arange(R, dtype=torch.int32, device="cuda")
+    prompt = _prompts(R, 1500, model.vocab)
+    model.prefill(prompt, slot)
+    q, k = rand(R, N, sd.HEADS, sd.DIM), rand(R, N, sd.KV_HEADS, sd.DIM)
+    t = model.tables
+    cache = rounds.CacheDesc(t.refcount.numel(), model.page, R, t.page_table.shape[1], sd.KV_HEADS, sd.DIM,
+                             bd.BDGDN_BF16, *model.pools[0].stride()[:3])
+    attn = rounds.AttnDesc(R, N, sd.HEADS, sd.KV_HEADS, sd.DIM, 0.125, bd.BDGDN_BF16, bd.BDGDN_BF16,
+                           bd.BDGDN_MASK_CAUSAL)
+    target, token = rand(R, N, V, dtype=torch.float32), torch.zeros(R, N, dtype=torch.int32, device="cuda")
+    u, noise = torch.full((R, N), 0.5, device="cuda"), torch.empty(R, V, device="cuda").exponential_(generator=gen)
+    none = torch.zeros(R, dtype=torch.int32, device="cuda")
+    return [
+        ("tree_attn", lambda s: bd.bdgdn_tree_attn(q, k, k, *model.pools, t.page_table, t.seq_len, mask="causal", stream=s,
+                                                   scale=0.125)[:1], bd.bdgdn_tree_attn_workspace(attn, cache)),
+        ("verify", lambda s: bd.bdgdn_verify(target, token, u, noise, stream=s),
+         bd.bdgdn_verify_workspace(rounds.VerifyDesc(R, N, V, bd.BDGDN_F32, N * V, V, 0, 0, V))),
+        ("append", lambda s: (bd.bdgdn_cache_append(t, model.pools, [k, k], slot, none, stream=s),),
+         bd.bdgdn_cache_workspace(cache, R, N)),
+    ]
+
+
+@pytest.mark.parametrize("which", range(3))
+def test_temporaries_belong_to_the_stream_of_the_call(which):
+    """A call on a stream that is busy for a while must not leave its memory to the stream that
+    the caller goes on with."""
+    name, call, need = _calls()[which]
+    want = [x.clone() for x in call(None)]
+    side, big = torch.cuda.Stream(), torch.zeros(1 << 28, device="cuda")
+    call(side)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(60):
+            big.add_(1)
+    got = call(side)
+    taken = [torch.full((need,), 7, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    torch.cuda.synchronize()
+    assert all(bool((x == 7).all()) for x in taken), name
+    assert all(torch.equal(g, w) for g, w in zip(got, want)), name
