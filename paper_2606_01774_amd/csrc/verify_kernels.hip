@@ -515,8 +515,10 @@ size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 // that joins them.
 VerifyPlan verify_plan(int R, int N, int V)
 {
-    const auto cut = [V](long rows, long limit, int &parts, int &part) {
-        const long most = (V + 4095) / 4096;
+    // as many parts as give 2048 workgroups, of 4096 logits or 1024 raced ones at least (a race
+    // is all latency: parts of 4096 took 8.6 us where those of 1024 take 6.3, 12 rows of 100003)
+    const auto cut = [V](long rows, long limit, int least, int &parts, int &part) {
+        const long most = (V + least - 1) / least;
         long n = (2048 + rows - 1) / rows;
         n = n > most ? most : n;
         n = n > limit ? limit : n;
@@ -524,8 +526,8 @@ VerifyPlan verify_plan(int R, int N, int V)
         parts = (V + part - 1) / part;
     };
     VerifyPlan p;
-    cut(2L * R * N, 64, p.splits, p.part);
-    cut(R, 2048, p.race_splits, p.race_part);
+    cut(2L * R * N, 64, 4096, p.splits, p.part);
+    cut(R, 2048, 1024, p.race_splits, p.race_part);
     p.walked_at = align256(2 * (size_t)R * N * p.splits * 16);
     p.best_at = p.walked_at + align256((size_t)R * sizeof(Walked));
     p.bytes = p.best_at + align256((size_t)R * p.race_splits * sizeof(Best));
