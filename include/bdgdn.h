@@ -540,7 +540,8 @@ typedef struct {
 } bdgdn_attn_desc_t;
 
 /* Bytes of device workspace bdgdn_tree_attn needs, 0 for descriptors that it rejects (more
- * than R (max_pages page / 32 + 9) = 2^31 - 2^16 tiles or R N h_q = 2^30 rows among them). */
+ * than R (max_pages page / 32 + 9) = 2^31 - 2^16 tiles, R N h_q = 2^30 rows or, in groups of 16 to
+ * a key head, 2^24 groups of rows among them). */
 size_t bdgdn_tree_attn_workspace(const bdgdn_attn_desc_t *desc, const bdgdn_cache_desc_t *cache);
 
 /*
@@ -662,7 +663,8 @@ typedef struct {
 
 /* Bytes of device workspace bdgdn_cache_append (rows_max: the rows that a request may add)
  * and bdgdn_cache_compact (rows_max: the positions that it may keep) need for num_req
- * requests, 0 for a descriptor or sizes that they reject. */
+ * requests, 0 for a descriptor or sizes that they reject (at most 65535 requests, which
+ * together may touch 2^30 pages). */
 size_t bdgdn_cache_workspace(const bdgdn_cache_desc_t *cache, int32_t num_req, int32_t rows_max);
 
 /*

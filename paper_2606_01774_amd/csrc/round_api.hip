@@ -62,11 +62,19 @@ int check_attn(const bdgdn_attn_desc_t *d, const bdgdn_cache_desc_t *c)
         if (stride[i] != 0 && (stride[i] < least[i] || stride[i] % unit)) return BDGDN_ERR_INVALID_ARG;
     // token numbers up to some tiles past a sequence's end
     if ((long)c->max_pages * c->page > 0x7fff0000L) return BDGDN_ERR_UNSUPPORTED;
-    // workgroups of the call; tiles of all requests, their nodes counting as eight at most
-    if ((long)d->num_req * d->nodes * d->h_q > 0x40000000L ||
+    // workgroups of 256 threads, of which a launch has 2^32; tiles of all requests, their nodes
+    // counting as eight at most
+    const long rows = (long)d->nodes * (d->h_q / d->h_kv);
+    if ((long)d->num_req * d->nodes * d->h_q > 0x40000000L || (long)d->num_req * d->h_kv * ((rows + 15) / 16) >= (1L << 24) ||
         (long)d->num_req * ((long)c->max_pages * c->page / 32 + 9) > 0x7fff0000L)
         return BDGDN_ERR_UNSUPPORTED;
     return BDGDN_OK;
+}
+
+// Requests are a grid's second dimension, and the pages that a call may take a 32-bit count.
+bool countable(const bdgdn_cache_desc_t *c, int32_t num_req, int32_t rows_max)
+{
+    return num_req <= 65535 && (long)num_req * (((long)rows_max + c->page - 1) / c->page + 1) <= 0x40000000L;
 }
 
 int check_verify(const bdgdn_verify_desc_t *d)
@@ -236,7 +244,7 @@ int bdgdn_verify(const bdgdn_verify_desc_t *desc, const void *target, const void
 
 size_t bdgdn_cache_workspace(const bdgdn_cache_desc_t *cache, int32_t num_req, int32_t rows_max)
 {
-    if (check_tables(cache) != BDGDN_OK || num_req <= 0 || num_req > 65535 || rows_max < 0) return 0;
+    if (check_tables(cache) != BDGDN_OK || num_req <= 0 || rows_max < 0 || !countable(cache, num_req, rows_max)) return 0;
     return cache_workspace(num_req, rows_max, cache->page);
 }
 
@@ -250,7 +258,7 @@ int bdgdn_cache_append(const bdgdn_cache_desc_t *cache, const bdgdn_cache_tables
     if (num_req < 0 || nodes < 0) return BDGDN_ERR_INVALID_ARG;
     const int64_t unit = 16 / size_of(cache->dtype);
     if (row_stride != 0 && (row_stride < (int64_t)cache->h_kv * cache->d || row_stride % unit)) return BDGDN_ERR_INVALID_ARG;
-    if (num_req > 65535) return BDGDN_ERR_UNSUPPORTED;
+    if (!countable(cache, num_req, nodes)) return BDGDN_ERR_UNSUPPORTED;
     if (num_req == 0) return BDGDN_OK;
     if (!tables_there(tables) || !slot || !count) return BDGDN_ERR_INVALID_ARG;
     st = check_pool_list(pools, rows, nodes > 0, n_pools);
@@ -287,7 +295,7 @@ int bdgdn_cache_compact(const bdgdn_cache_desc_t *cache, const bdgdn_cache_table
     int st = check_pools(cache);
     if (st != BDGDN_OK) return st;
     if (num_req < 0 || keep_max < 0) return BDGDN_ERR_INVALID_ARG;
-    if (num_req > 65535) return BDGDN_ERR_UNSUPPORTED;
+    if (!countable(cache, num_req, keep_max)) return BDGDN_ERR_UNSUPPORTED;
     if (num_req == 0) return BDGDN_OK;
     if (!tables_there(tables) || !slot || !count || (keep_max > 0 && !keep)) return BDGDN_ERR_INVALID_ARG;
     st = check_pool_list(pools, nullptr, false, n_pools);

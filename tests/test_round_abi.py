@@ -76,6 +76,11 @@ def test_attention_limits():
     assert bd.bdgdn_tree_attn_workspace(_attn(**many), _cache(n_slots=65535, max_pages=2 * 32700)) > 0
     assert _call_attn(_attn(**many), _cache(n_slots=65535, max_pages=2 * 32764)) == UNS
     assert _call_attn(_attn(num_req=65535, nodes=64, h_q=512), _cache(n_slots=65535)) == UNS
+    for h_kv, want in ((256, bd.BDGDN_OK), (257, UNS)):
+        cache = _cache(n_slots=65535, h_kv=h_kv, token_stride=128 * h_kv, page_stride=128 * h_kv * 16)
+        attn = _attn(num_req=65535, nodes=1, h_q=h_kv, h_kv=h_kv)
+        assert (bd.bdgdn_tree_attn_workspace(attn, cache) > 0) == (want == bd.BDGDN_OK)
+        assert want == bd.BDGDN_OK or _call_attn(attn, cache) == want
 
 
 def test_attention_checks_mask_and_workspace():
@@ -155,6 +160,18 @@ def test_cache_calls_reject():
     assert lib.bdgdn_cache_truncate(_cache(), t, 1, None, None, None) == INV
     assert lib.bdgdn_cache_truncate(_cache(max_pages=0), t, 1, FAKE, None, None) == INV
     assert bd.bdgdn_cache_workspace(_cache(), 0, 4) == 0 and bd.bdgdn_cache_workspace(_cache(), 2, -1) == 0
+
+
+def test_cache_limits():
+    """More pages in one call than 32 bits count, more requests than a grid has room for."""
+    lib, one = bd.load_library(), _cache(page=1, max_pages=1 << 20, page_stride=256)
+    tables = rounds._Tables(FAKE, FAKE, FAKE, FAKE)
+    pools = (ctypes.c_void_p * 1)(FAKE)
+    for R, rows, want in ((65535, 16382, WS), (65535, 16384, UNS), (65536, 1, UNS), (1024, 0x7fffffff, UNS)):
+        assert (bd.bdgdn_cache_workspace(one, R, rows) > 0) == (want == WS)
+        assert lib.bdgdn_cache_append(one, tables, pools, pools, 1, R, rows, 0, FAKE, None, FAKE, None, FAKE, 16,
+                                      None) == want
+        assert lib.bdgdn_cache_compact(one, tables, pools, 1, R, rows, FAKE, FAKE, FAKE, None, FAKE, 16, None) == want
 
 
 def test_tables_of_an_empty_cache():
