@@ -267,7 +267,9 @@ template <typename T, int D, int MT, bool SPLITP> struct Wave {
     }
 
     // o += V^T P^T; v[e] is the lane's part of value row
-    // 16 (e / 4) + 4 g + e % 4.
+    // 16 (e / 4) + 4 g + e % 4.  With bf16 inputs the weights are rounded to bf16, which the matrix
+    // units take: to one part where the output is rounded as much, to two (16 bits) where it is
+    // fp32.  Their sum is of the unrounded ones.
     __device__ __forceinline__ void values(const f32x4 (&p)[MT][2], const u32x4 (&v)[8][G::NV])
     {
         if constexpr (sizeof(T) == 2) {

@@ -3,6 +3,11 @@
 // no trip to the host; the lowest free pages are taken in the order of the requests, so that
 // the tables do not depend on the order in which workgroups run.  A plan kernel of one
 // workgroup takes the pages, move kernels copy rows in 16-byte chunks.
+//
+// What bounds it: the copies memory, the rest launches.  Compacting 8 sequences of up to 4096
+// tokens to their halves in 4 pools: move 39 us (5.5 TB/s read and written), keep 5.4, plan 7.1,
+// finish 4.7.  Appending to 64 sequences in 8 pools: plan 5.4, move 5.1; to 64 that share their
+// last page with others: plan 7.6, move 12.5 (5.8 TB/s).  A fork is 3.4 us, a truncation 3.3.
 #include "kernels.hpp"
 #include "round.hpp"
 

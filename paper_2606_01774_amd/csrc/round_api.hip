@@ -195,7 +195,7 @@ int bdgdn_tree_attn(const bdgdn_attn_desc_t *desc, const bdgdn_cache_desc_t *cac
     a.token16 = (uint32_t)(cache->token_stride * size / 16);
     // scale s: the sign goes into q's (exactly), so that the largest score is the largest
     // product; scale 0 makes every product 0
-    a.c = desc->scale == 0.f ? 1.f : fabsf(desc->scale) * 1.4426950408889634f;
+    a.c = desc->scale == 0.f ? 1.f : fminf(fabsf(desc->scale) * 1.4426950408889634f, 3.402823466e38f);
     a.q_and = desc->scale == 0.f ? 0u : ~0u;
     a.q_xor = desc->scale < 0.f ? (bf16 ? 0x80008000u : 0x80000000u) : 0u;
     return status_of(launch_tree_attn(bf16, desc->out_dtype == BDGDN_F32, desc->d, p, a, workspace,

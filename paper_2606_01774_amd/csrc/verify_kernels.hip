@@ -3,11 +3,16 @@
 //
 //   stats  (row, part of the vocabulary): reads every row of logits that a walk may need once
 //          and leaves the part's maximum and sum of exponentials, or (greedy requests) the
-//          index of its maximum.  This is where the bytes are.
+//          index of its maximum.  This is where the bytes are: 64 requests of 8 nodes over
+//          131072 bf16 logits, some greedy, 39 us, over 6 TB/s; bound by memory.
 //   walk   (request): the rows' laws and every child's odds at once, then the walk itself in
 //          LDS.  Only a refusal with a sibling left reads a row again, for the residual's mass.
-//   race   (request, part): argmax of law(t) / noise(t) over a part of one row.
-//   pick   (request): the best of the parts.
+//          7.5 us for the same requests, 9 for trees of 24 over 100003 fp32 logits: latency.
+//   race   (request, part): argmax of law(t) / noise(t) over a part of one row; 13.9 us for the
+//          same 64 (67 MB, what a copy takes).
+//   pick   (request): the best of the parts; 4 us, of which most is a launch's own.
+// Statistics, laws, residuals and scores are fp32, from logits of either type; the only rounding
+// to fewer bits is the caller's.
 // One workgroup to a request for walk and race together takes three times as long (36 us for
 // a row of 131072 with its draft and noise, 64 requests), and joining the parts by the last of
 // a request's workgroups twice (each has to write back its caches first).
@@ -68,12 +73,13 @@ __device__ __forceinline__ Stat join(Stat a, Stat b, float k, bool greedy)
     return r;
 }
 
-// log2(e) / T, or 1 for a greedy request.
+// log2(e) / T, or 1 for a greedy request; kept where no product with a difference of logits is
+// 0 x inf.
 __device__ __forceinline__ float temper(const VerifyArgs &a, int r, bool &greedy)
 {
     const float T = a.temperature ? a.temperature[r] : 1.f;
     greedy = !(T > 0.f);
-    return greedy ? 1.f : kLog2e / T;
+    return greedy ? 1.f : fminf(fmaxf(kLog2e / T, 1.2e-38f), 1e38f);
 }
 
 // Nodes of request r.

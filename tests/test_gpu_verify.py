@@ -131,6 +131,13 @@ def test_against_the_rule(R, N, V, dtype, draft, tree):
     _check(_random(R, N, V, dtype, draft, tree, seed=R * N + V, T=T))
 
 
+@pytest.mark.parametrize("draft", ["sampled", "point"])
+def test_temperatures_at_the_ends_of_fp32(draft):
+    """The law tends to one token, and to all of them alike."""
+    T = [1e-45, 1e-39, 1e-30, 1e30, 3e38, math.inf]
+    _check(_random(6, 5, 501, torch.float32, draft, False, seed=8, T=T))
+
+
 def test_chains_need_no_parents_and_no_last_draft_row():
     c = _random(6, 5, 501, torch.bfloat16, "sampled", False, seed=3, T=[1.0] * 6)
     want = [t.clone() for t in bd.bdgdn_verify(c["target"], c["token"], c["u"], c["noise"], draft=c["draft"],
