@@ -1,5 +1,5 @@
 // verify_kernels.hip -- verification of drafted tokens against the target's logits from given
-// random numbers, in four launches.
+// random numbers, in four launches, or two for vocabularies of up to 32768.
 //
 //   stats  (row, part of the vocabulary): reads every row of logits that a walk may need once
 //          and leaves the part's maximum and sum of exponentials, or (greedy requests) the
@@ -8,12 +8,12 @@
 //   walk   (request): the rows' laws and every child's odds at once, then the walk itself in
 //          LDS.  Only a refusal with a sibling left reads a row again, for the residual's mass.
 //          7.5 us for the same requests, 9 for trees of 24 over 100003 fp32 logits: latency.
-//   race   (request, part): argmax of law(t) / noise(t) over a part of one row; 13.9 us for the
-//          same 64 (67 MB, what a copy takes).
+//   race   (request, part): argmax of law(t) / noise(t) over a part of one row; 13.6 us for the
+//          same 64 (67 MB, what a copy takes).  Short rows are raced over by the walk's workgroup.
 //   pick   (request): the best of the parts; 4 us, of which most is a launch's own.
 // Statistics, laws, residuals and scores are fp32, from logits of either type; the only rounding
 // to fewer bits is the caller's.
-// One workgroup to a request for walk and race together takes three times as long (36 us for
+// For long rows one workgroup to a request takes three times as long (36 us for
 // a row of 131072 with its draft and noise, 64 requests), and joining the parts by the last of
 // a request's workgroups twice (each has to write back its caches first).
 #include "common.hpp"
@@ -231,8 +231,10 @@ template <typename E> struct Residual {
     }
     // x: the target's logits, then what is left of the law but for what `out` says; y: the
     // draft's logits where c > 0
+    // (without a fused multiply-add, so that equal laws leave exactly nothing)
     template <int N> __device__ __forceinline__ void of(float (&x)[N], const float (&y)[N]) const
     {
+#pragma clang fp contract(off)
         if (c > 0.f) {
 #pragma unroll
             for (int i = 0; i < N; ++i) x[i] = fmaxf(p.of(x[i]) - c * q.of(y[i]), 0.f);
@@ -283,7 +285,54 @@ template <int THREADS> __device__ __forceinline__ Best best_of_block(Best b, Bes
     return b;
 }
 
-template <typename E> __global__ void __launch_bounds__(kWalkThreads) bdgdn_verify_walk_kernel(VerifyArgs a)
+// argmax over [v0, v1) of law / noise, -1 where nothing is above zero.  Every thread of the
+// workgroup gets it.  The quotient is formed only where a product says that it may pass the
+// best one of the wave (x >= best e, less what the rounding of either can hide).
+template <int THREADS, typename E> __device__ __forceinline__ Best race(const Residual<E> &res, const float *noise, int v0, int v1, Best *lds)
+{
+    constexpr int N = Vec<E>::n;
+    Best b = {0.f, -1};
+    float bar = 0.f;
+    const auto consider = [&](const float x, const float e, int at) {
+        const float y = x / e;
+        if (y > b.score && !res.out(at)) b = Best{y, at};
+    };
+    const int whole = v0 + (v1 - v0) / N * N;
+#pragma unroll 2
+    for (int v = v0; v < whole; v += THREADS * N) {
+        const int at = v + threadIdx.x * N;
+        const bool in = at < whole;
+        float x[N], y[N], e[N];
+        bool pass = false;
+        if (in) {
+            Vec<E>::load(x, res.t + at);
+            if (res.c > 0.f) Vec<E>::load(y, res.d + at);
+#pragma unroll
+            for (int i = 0; i < N; i += 4) Vec<float>::load(reinterpret_cast<float(&)[4]>(e[i]), noise + at + i);
+            res.of(x, y);
+#pragma unroll
+            for (int i = 0; i < N; ++i) pass |= x[i] >= bar * e[i];
+        }
+        if (!__any(pass)) continue;
+        if (pass) {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (x[i] >= bar * e[i]) consider(x[i], e[i], at + i);
+        }
+        float top = b.score;
+#pragma unroll
+        for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+        bar = top * 0.999999f;
+    }
+    if (whole + (int)threadIdx.x < v1) {
+        const int at = whole + threadIdx.x;
+        consider(res.one(at), noise[at], at);
+    }
+    return best_of_block<THREADS>(b, lds);
+}
+
+// RACE: the walk's workgroup also draws the next token.
+template <typename E, bool RACE> __global__ void __launch_bounds__(kWalkThreads) bdgdn_verify_walk_kernel(VerifyArgs a)
 {
     __shared__ Law s_law[2][kMaxNodes];
     __shared__ float s_p[kMaxNodes], s_q[kMaxNodes], s_u[kMaxNodes];
@@ -299,7 +348,8 @@ template <typename E> __global__ void __launch_bounds__(kWalkThreads) bdgdn_veri
         if (tid == 0) {
             a.n_accept[r] = 0;
             if (a.n_path) a.n_path[r] = 0;
-            out->node = out->next = -1;
+            if (RACE) a.next[r] = -1;
+            else out->node = out->next = -1;
         }
         return;
     }
@@ -401,10 +451,28 @@ template <typename E> __global__ void __launch_bounds__(kWalkThreads) bdgdn_veri
         a.n_accept[r] = steps;
         if (a.n_path) a.n_path[r] = steps + 1;
     }
-    if (tid < n_gone) out->gone[tid] = s_gone[tid];
     // (an integer comparison of the law's bits: from one of floats hipcc 7.2 has made a select
     // on a condition that it had not set)
     const bool lawful = __builtin_amdgcn_readfirstlane(__float_as_int(s_law[0][cur].inv)) > 0;
+    if (RACE) {
+        if (!lawful || greedy) {   // (a greedy law is all on one token, and that was not refused)
+            if (tid == 0) a.next[r] = lawful ? s_law[0][cur].arg : -1;
+            return;
+        }
+        __shared__ Best s_best[kWalkThreads / 64];
+        Residual<E> res = {target + cur * a.t_row, c > 0.f ? draft + cur * a.d_row : nullptr, s_law[0][cur],
+                           c > 0.f ? s_law[1][cur] : Law{}, c, s_gone, n_gone};
+        const float *noise = a.noise + r * a.noise_stride;
+        Best b = race<kWalkThreads>(res, noise, 0, a.V, s_best);
+        if (b.at < 0) {   // nothing is left of the law: p itself
+            res.c = 0.f;
+            res.n_gone = 0;
+            b = race<kWalkThreads>(res, noise, 0, a.V, s_best);
+        }
+        if (tid == 0) a.next[r] = b.at;
+        return;
+    }
+    if (tid < n_gone) out->gone[tid] = s_gone[tid];
     if (tid == 0) {
         out->p = s_law[0][cur];
         if (c > 0.f) out->q = s_law[1][cur];
@@ -414,52 +482,6 @@ template <typename E> __global__ void __launch_bounds__(kWalkThreads) bdgdn_veri
         // a greedy law is all on one token, and that was not refused
         out->next = lawful ? s_law[0][cur].arg : -1;
     }
-}
-
-// argmax over [v0, v1) of law / noise, -1 where nothing is above zero.  Every thread of the
-// workgroup gets it.  The quotient is formed only where a product says that it may pass the
-// best one of the wave (x >= best e, less what the rounding of either can hide).
-template <typename E> __device__ __forceinline__ Best race(const Residual<E> &res, const float *noise, int v0, int v1, Best *lds)
-{
-    constexpr int N = Vec<E>::n;
-    Best b = {0.f, -1};
-    float bar = 0.f;
-    const auto consider = [&](const float x, const float e, int at) {
-        const float y = x / e;
-        if (y > b.score && !res.out(at)) b = Best{y, at};
-    };
-    const int whole = v0 + (v1 - v0) / N * N;
-#pragma unroll 2
-    for (int v = v0; v < whole; v += kRaceThreads * N) {
-        const int at = v + threadIdx.x * N;
-        const bool in = at < whole;
-        float x[N], y[N], e[N];
-        bool pass = false;
-        if (in) {
-            Vec<E>::load(x, res.t + at);
-            if (res.c > 0.f) Vec<E>::load(y, res.d + at);
-#pragma unroll
-            for (int i = 0; i < N; i += 4) Vec<float>::load(reinterpret_cast<float(&)[4]>(e[i]), noise + at + i);
-            res.of(x, y);
-#pragma unroll
-            for (int i = 0; i < N; ++i) pass |= x[i] >= bar * e[i];
-        }
-        if (!__any(pass)) continue;
-        if (pass) {
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                if (x[i] >= bar * e[i]) consider(x[i], e[i], at + i);
-        }
-        float top = b.score;
-#pragma unroll
-        for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-        bar = top * 0.999999f;
-    }
-    if (whole + (int)threadIdx.x < v1) {
-        const int at = whole + threadIdx.x;
-        consider(res.one(at), noise[at], at);
-    }
-    return best_of_block<kRaceThreads>(b, lds);
 }
 
 template <typename E> __device__ __forceinline__ Residual<E> left_of(const VerifyArgs &a, const Walked &w, int r)
@@ -476,7 +498,7 @@ template <typename E> __global__ void __launch_bounds__(kRaceThreads) bdgdn_veri
     const Walked &w = static_cast<const Walked *>(a.walked)[r];
     if (w.node < 0) return;
     const int v0 = blockIdx.x * a.race_part, v1 = min(v0 + a.race_part, a.V);
-    const Best b = race(left_of<E>(a, w, r), a.noise + r * a.noise_stride, v0, v1, lds);
+    const Best b = race<kRaceThreads>(left_of<E>(a, w, r), a.noise + r * a.noise_stride, v0, v1, lds);
     if (threadIdx.x == 0) static_cast<Best *>(a.best)[(long)r * a.race_splits + blockIdx.x] = b;
 }
 
@@ -499,7 +521,7 @@ template <typename E> __global__ void __launch_bounds__(kRaceThreads) bdgdn_veri
         Residual<E> res = left_of<E>(a, w, r);
         res.c = 0.f;
         res.n_gone = 0;
-        b = race(res, a.noise + r * a.noise_stride, 0, a.V, lds);
+        b = race<kRaceThreads>(res, a.noise + r * a.noise_stride, 0, a.V, lds);
     }
     if (threadIdx.x == 0) a.next[r] = b.at;
 }
@@ -507,7 +529,11 @@ template <typename E> __global__ void __launch_bounds__(kRaceThreads) bdgdn_veri
 template <typename E> void launch(const VerifyArgs &a, hipStream_t s)
 {
     bdgdn_verify_stats_kernel<E><<<(a.draft ? 2 : 1) * a.R * a.N * a.splits, kStatThreads, 0, s>>>(a);
-    bdgdn_verify_walk_kernel<E><<<a.R, kWalkThreads, 0, s>>>(a);
+    if (a.race_splits == 0) {
+        bdgdn_verify_walk_kernel<E, true><<<a.R, kWalkThreads, 0, s>>>(a);
+        return;
+    }
+    bdgdn_verify_walk_kernel<E, false><<<a.R, kWalkThreads, 0, s>>>(a);
     bdgdn_verify_race_kernel<E><<<dim3(a.race_splits, a.R), kRaceThreads, 0, s>>>(a);
     bdgdn_verify_pick_kernel<E><<<a.R, kRaceThreads, 0, s>>>(a);
 }
@@ -534,6 +560,10 @@ VerifyPlan verify_plan(int R, int N, int V)
     VerifyPlan p;
     cut(2L * R * N, 64, 4096, p.splits, p.part);
     cut(R, 2048, 1024, p.race_splits, p.race_part);
+    // Up to 32768 logits the walk's workgroup races over all of them: two launches fewer (one
+    // request over 1000: 22 -> 17 us a call, over 32001 23 -> 19; 64 requests over 32001 33.5 ->
+    // 31, of fp32 40 -> 38; at 65536, 16 requests, it would be 30 instead of 25).
+    if (V <= 32768) p.race_splits = 0;
     p.walked_at = align256(2 * (size_t)R * N * p.splits * 16);
     p.best_at = p.walked_at + align256((size_t)R * sizeof(Walked));
     p.bytes = p.best_at + align256((size_t)R * p.race_splits * sizeof(Best));

@@ -213,6 +213,37 @@ def test_ties_go_to_the_lowest_index():
     assert acc.tolist() == [0, 0, 0] and nxt.tolist() == [1234, 77, 77]
 
 
+@pytest.mark.parametrize("V", [32760, 32768, 32769, 40003])
+@pytest.mark.parametrize("dtype,draft,tree", [(torch.float32, "point", True), (torch.bfloat16, "sampled", False)])
+def test_vocabularies_about_the_length_that_one_workgroup_races_over(V, dtype, draft, tree):
+    T = [(1.0, 0.6, 0.0, 1.4)[r % 4] for r in range(6)]
+    _check(_random(6, 6, V, dtype, draft, tree, seed=V, T=T))
+
+
+@pytest.mark.parametrize("V", [300, 40003])
+def test_long_and_short_rows_without_a_law_and_ties(V):
+    c = _random(6, 3, V, torch.float32, "sampled", False, seed=5, T=[1.0] * 6)
+    c["target"][0, 0] = float("-inf")
+    c["target"][1, 0, V - 1] = float("nan")
+    c["target"][2, :, 1:] = float("-inf")       # all on token 0
+    c["target"][3] = c["draft"][3]              # a refusal leaves nothing: the target's own law
+    c["u"][3, 1] = 1.0
+    c["target"][4, :, :] = 0                    # ties: the lowest of equal scores
+    c["noise"][4] = 1
+    c["u"][4, 1] = 0.9999
+    c["draft"][4, 0] = 0
+    c["draft"][4, 0, int(c["token"][4, 1])] = 3
+    count = torch.tensor([3, 3, 3, 2, 2, 0], dtype=torch.int32).cuda()
+    acc, path, nxt, n_path = (x.tolist() for x in bd.bdgdn_verify(
+        c["target"], c["token"], c["u"], c["noise"], draft=c["draft"], count=count, want_n_path=True))
+    assert nxt[0] == nxt[1] == nxt[5] == -1 and nxt[2] == 0
+    assert acc[:2] == [0, 0] and acc[3:] == [0, 0, 0] and n_path[5] == 0 and path[5] == [-1] * 3
+    score = torch.softmax(c["target"][3, 0].double(), 0) / c["noise"][3].double()
+    assert nxt[3] == int(score.argmax())
+    refused = int(c["token"][4, 1])
+    assert nxt[4] == (1 if refused == 0 else 0)
+
+
 @pytest.mark.parametrize("draft", ["sampled", "point"])
 def test_what_comes_out_is_distributed_as_the_target(draft):
     """The first token after the anchor, accepted or drawn, over 40000 requests with three drafts
