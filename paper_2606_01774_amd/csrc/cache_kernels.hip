@@ -8,6 +8,7 @@
 // tokens to their halves in 4 pools: move 39 us (5.5 TB/s read and written), keep 5.4, plan 7.1,
 // finish 4.7.  Appending to 64 sequences in 8 pools: plan 5.4, move 5.1; to 64 that share their
 // last page with others: plan 7.6, move 12.5 (5.8 TB/s).  A fork is 3.4 us, a truncation 3.3.
+// Small calls are bound by the host's launches, about 3 us each.
 #include "kernels.hpp"
 #include "round.hpp"
 
@@ -16,6 +17,7 @@ namespace bdgdn {
 namespace {
 
 constexpr int kPlanThreads = 1024;
+constexpr int kOneRequests = 256;   // of a compaction that one workgroup plans
 enum { kDone = 0, kNoPages = 1, kNoRoom = 2, kBadSlot = 3, kBadKeep = 4 };
 
 typedef unsigned int u32x4v __attribute__((ext_vector_type(4)));
@@ -99,11 +101,49 @@ template <bool APPEND> __device__ int plan_request(const CacheArgs &a, int f)
     return need;
 }
 
+// Do the positions of each request rise, are they there, how many stay in place (-1: they are
+// bad); and the tables as they are.  By the plan kernel's workgroup, 512 positions to a wave's turn.
+__device__ void look_at_keeps(const CacheArgs &a)
+{
+    __shared__ int s_stay[kOneRequests], s_bad[kOneRequests];
+    const int tid = threadIdx.x, lane = tid & 63;
+    if (tid < a.R) s_stay[tid] = s_bad[tid] = 0;
+    __syncthreads();
+    const int turns = (a.rows_max + 511) / 512;
+    for (int x = tid >> 6; x < a.R * turns; x += kPlanThreads / 64) {
+        const int f = x / turns, j0 = (x - f * turns) * 512, slot = a.slot[f], n = min(max(a.count[f], 0), a.rows_max);
+        const int old = (unsigned)slot < (unsigned)a.n_slots ? seq_of(a, slot) : 0;
+        const int32_t *keep = a.path + (long)f * a.rows_max;
+        int stay = 0;
+        bool bad = false;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int j = j0 + 64 * i + lane;
+            if (j < n) {
+                const int t = keep[j], before = j > 0 ? keep[j - 1] : -1;
+                stay += t == j;
+                bad |= t < 0 || t >= old || before >= t;
+            }
+        }
+        if (stay) atomicAdd(&s_stay[f], stay);
+        if (bad) s_bad[f] = 1;
+    }
+    for (int x = tid; x < a.R * a.max_pages; x += kPlanThreads) {
+        const int f = x / a.max_pages, i = x - f * a.max_pages, slot = a.slot[f];
+        if ((unsigned)slot < (unsigned)a.n_slots && i < pages_of(seq_of(a, slot), a.page))
+            a.saved[x] = a.table[(long)slot * a.max_pages + i];
+    }
+    __syncthreads();
+    if (tid < a.R) a.meta[(long)tid * kMeta + kStay] = s_bad[tid] ? -1 : s_stay[tid];
+    __syncthreads();
+}
+
 template <bool APPEND> __global__ void __launch_bounds__(kPlanThreads) bdgdn_cache_plan_kernel(CacheArgs a)
 {
     __shared__ int lds[kPlanThreads / 64];
     __shared__ int s_granted;
     const int tid = threadIdx.x;
+    if (!APPEND && a.saved) look_at_keeps(a);
     int want = 0;
     for (int f0 = 0; f0 < a.R; f0 += kPlanThreads) {
         const int f = f0 + tid;
@@ -152,7 +192,22 @@ template <bool APPEND> __global__ void __launch_bounds__(kPlanThreads) bdgdn_cac
         atomicAnd(&a.bits[p >> 5], ~(1u << (p & 31)));
         a.ref[p] = 1;
     }
-    if (!APPEND) return;
+    if (!APPEND) {
+        if (!a.saved) return;
+        // the compacted sequences' tables: the rows' moves go by the saved ones
+        for (int x = tid; x < a.R * a.max_pages; x += kPlanThreads) {
+            const int f = x / a.max_pages, i = x - f * a.max_pages;
+            const int32_t *m = a.meta + (long)f * kMeta;
+            if (m[kNew] < 0 || i < m[kStart] || i >= pages_of(m[kOld], a.page)) continue;
+            give_back(a, a.saved[x]);
+            a.table[(long)a.slot[f] * a.max_pages + i] = i < m[kStart] + m[kNeed] ? a.alloc[m[kOff] + i - m[kStart]] : -1;
+        }
+        for (int f = tid; f < a.R; f += kPlanThreads) {
+            const int n = a.meta[(long)f * kMeta + kNew];
+            if (n >= 0) a.len[a.slot[f]] = n;
+        }
+        return;
+    }
     for (int f = tid; f < a.R; f += kPlanThreads) {
         const int32_t *m = a.meta + (long)f * kMeta;
         if (m[kNew] <= 0) continue;
@@ -201,8 +256,13 @@ __global__ void __launch_bounds__(256) bdgdn_cache_finish_kernel(CacheArgs a)
     if (threadIdx.x == 0) a.len[slot] = m[kNew];
 }
 
+template <int POOLS> struct MoveArgs : MoveShape {
+    unsigned char *pool[POOLS];
+    const unsigned char *rows[POOLS];
+};
+
 // Copies 16-byte chunks: grid (chunks, requests, pools).
-template <bool APPEND> __global__ void __launch_bounds__(256) bdgdn_cache_move_kernel(MoveArgs a)
+template <bool APPEND, int POOLS> __global__ void __launch_bounds__(256) bdgdn_cache_move_kernel(MoveArgs<POOLS> a)
 {
     const CacheArgs &c = a.c;
     const int f = blockIdx.y;
@@ -210,7 +270,7 @@ template <bool APPEND> __global__ void __launch_bounds__(256) bdgdn_cache_move_k
     const int n = m[kNew];
     if (n <= 0) return;
     const int slot = c.slot[f], old = m[kOld];
-    const int32_t *row = c.table + (long)slot * c.max_pages;
+    const int32_t *row = !APPEND && c.saved ? c.saved + (long)f * c.max_pages : c.table + (long)slot * c.max_pages;
     // append: tokens from `first` on, of which the first `copied` come from a shared page;
     // compact: tokens from `first` on come from the positions kept
     const int copied = APPEND && m[kCow] >= 0 ? old % c.page : 0;
@@ -279,10 +339,19 @@ __global__ void __launch_bounds__(256) bdgdn_cache_truncate_kernel(CacheArgs a)
 
 }  // namespace
 
-size_t cache_workspace(int R, int rows_max, int page)
+// One workgroup plans a small compaction (it looks at the positions and tables itself and sets the
+// tables: two launches in all).  For others a kernel of a workgroup per request comes before it and
+// another after the moves.  Fork, truncate and compact of 1 to 64 sequences with up to 6400
+// positions to keep: 31 to 33 us with one, 37 to 40 with all; with 16384 positions 63 and 63, with
+// 32768 68 and 59.
+CachePlan cache_plan(int R, int rows_max, int page, int max_pages)
 {
-    const size_t ints = (size_t)R * (kMeta + (size_t)(rows_max + page - 1) / page + 1);
-    return (ints * 4 + 255) & ~(size_t)255;
+    CachePlan p;
+    p.one = R <= kOneRequests && (long)R * rows_max <= 8192 && (long)R * max_pages <= 8192;
+    p.alloc_at = (size_t)R * kMeta;
+    p.saved_at = p.alloc_at + (size_t)R * (((size_t)rows_max + page - 1) / page + 1);
+    p.ints = p.saved_at + (p.one ? (size_t)R * max_pages : 0);
+    return p;
 }
 
 hipError_t launch_cache_plan(bool append, const CacheArgs &a, hipStream_t s)
@@ -290,20 +359,44 @@ hipError_t launch_cache_plan(bool append, const CacheArgs &a, hipStream_t s)
     if (append) {
         bdgdn_cache_plan_kernel<true><<<1, kPlanThreads, 0, s>>>(a);
     } else {
-        bdgdn_cache_keep_kernel<<<a.R, 256, 0, s>>>(a);
+        if (!a.saved) bdgdn_cache_keep_kernel<<<a.R, 256, 0, s>>>(a);
         bdgdn_cache_plan_kernel<false><<<1, kPlanThreads, 0, s>>>(a);
     }
     return hipGetLastError();
 }
 
-hipError_t launch_cache_move(bool append, const MoveArgs &a, hipStream_t s)
+namespace {
+
+// Moves in `n` <= POOLS pools.
+template <int POOLS> hipError_t move_some(bool append, const MoveShape &m, void *const *pools, const void *const *rows, int n, hipStream_t s)
 {
-    const long rows = (long)a.c.rows_max + (append ? a.c.page - 1 : 0);
-    const long blocks = (rows * a.row16 + 1023) / 1024;
-    const dim3 grid((unsigned)(blocks < 1 ? 1 : blocks > 256 ? 256 : blocks), a.c.R, a.n_pools);
-    if (append) bdgdn_cache_move_kernel<true><<<grid, 256, 0, s>>>(a);
-    else bdgdn_cache_move_kernel<false><<<grid, 256, 0, s>>>(a);
+    MoveArgs<POOLS> a;
+    static_cast<MoveShape &>(a) = m;
+    for (int i = 0; i < n; ++i) {
+        a.pool[i] = static_cast<unsigned char *>(pools[i]);
+        a.rows[i] = rows ? static_cast<const unsigned char *>(rows[i]) : nullptr;
+    }
+    const long most = (long)m.c.rows_max + (append ? m.c.page - 1 : 0);
+    const long blocks = (most * m.row16 + 1023) / 1024;
+    const dim3 grid((unsigned)(blocks < 1 ? 1 : blocks > 256 ? 256 : blocks), m.c.R, n);
+    if (append) bdgdn_cache_move_kernel<true, POOLS><<<grid, 256, 0, s>>>(a);
+    else bdgdn_cache_move_kernel<false, POOLS><<<grid, 256, 0, s>>>(a);
     return hipGetLastError();
+}
+
+}  // namespace
+
+// (what a launch's arguments weigh costs the host: an append to 8 pools takes 30.6 us with room for
+// 16 pools' addresses, 31.3 with room for 96)
+hipError_t launch_cache_move(bool append, const MoveShape &m, void *const *pools, const void *const *rows, int n_pools, hipStream_t s)
+{
+    if (n_pools <= 16) return n_pools > 0 ? move_some<16>(append, m, pools, rows, n_pools, s) : hipSuccess;
+    for (int p0 = 0; p0 < n_pools; p0 += 96) {
+        const int n = n_pools - p0 < 96 ? n_pools - p0 : 96;
+        const hipError_t e = move_some<96>(append, m, pools + p0, rows ? rows + p0 : nullptr, n, s);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 hipError_t launch_cache_finish(const CacheArgs &a, hipStream_t s)

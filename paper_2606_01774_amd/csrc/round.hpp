@@ -65,7 +65,6 @@ VerifyPlan verify_plan(int R, int N, int V);
 hipError_t launch_verify(bool bf16, VerifyArgs &a, const VerifyPlan &p, void *workspace, hipStream_t s);
 
 // ------------------------------------------------------------------ the cache's pages (cache_kernels.hip)
-constexpr int kPoolsPerLaunch = 96;
 
 struct CacheArgs {
     int32_t *table, *len, *ref;
@@ -75,24 +74,28 @@ struct CacheArgs {
     const int32_t *slot, *path, *count;   // path: append's path or compact's positions
     int32_t *status;
     int32_t *meta, *alloc;     // workspace: kMeta ints per request, then the pages taken
+    int32_t *saved;            // and, for a compaction that one workgroup plans, the tables before it
 };
 
 // Per-request words of the workspace.
 enum { kOld = 0, kNew, kCow, kStart, kNeed, kOff, kStay, kMeta = 8 };
 
-struct MoveArgs {
+struct MoveShape {
     CacheArgs c;
-    int n_pools;
     int row16, head16_log;     // 16-byte chunks of a token's row; log2 of those of a head
     long page_stride, token_stride, head_stride, row_stride;   // bytes
     long head_bytes;           // of a head in the rows to append
-    unsigned char *pool[kPoolsPerLaunch];
-    const unsigned char *rows[kPoolsPerLaunch];
 };
 
-size_t cache_workspace(int R, int rows_max, int page);
+// Ints of the workspace: where each part of CacheArgs' begins, how many there are.
+struct CachePlan {
+    size_t alloc_at, saved_at, ints;
+    bool one;                  // one workgroup plans a compaction
+};
+
+CachePlan cache_plan(int R, int rows_max, int page, int max_pages);
 hipError_t launch_cache_plan(bool append, const CacheArgs &a, hipStream_t s);
-hipError_t launch_cache_move(bool append, const MoveArgs &a, hipStream_t s);
+hipError_t launch_cache_move(bool append, const MoveShape &m, void *const *pools, const void *const *rows, int n_pools, hipStream_t s);
 hipError_t launch_cache_finish(const CacheArgs &a, hipStream_t s);
 hipError_t launch_cache_fork(const CacheArgs &a, const int32_t *src, const int32_t *dst, hipStream_t s);
 hipError_t launch_cache_truncate(const CacheArgs &a, hipStream_t s);

@@ -106,12 +106,11 @@ bool tables_there(const bdgdn_cache_tables_t *t)
     return t && t->page_table && t->seq_len && t->refcount && t->free_bits;
 }
 
-// The moves of every pool, kPoolsPerLaunch to a launch.
 hipError_t move_pools(bool append, const bdgdn_cache_desc_t *c, const CacheArgs &ca, void *const *pools,
                       const void *const *rows, int n_pools, int64_t row_stride, hipStream_t s)
 {
     const long size = size_of(c->dtype);
-    MoveArgs m = {};
+    MoveShape m = {};
     m.c = ca;
     m.row16 = (int)(c->h_kv * c->d * size / 16);
     while ((16L << m.head16_log) < c->d * size) ++m.head16_log;
@@ -120,16 +119,21 @@ hipError_t move_pools(bool append, const bdgdn_cache_desc_t *c, const CacheArgs 
     m.head_stride = c->head_stride * size;
     m.row_stride = (row_stride ? row_stride : (int64_t)c->h_kv * c->d) * size;
     m.head_bytes = c->d * size;
-    for (int p0 = 0; p0 < n_pools; p0 += kPoolsPerLaunch) {
-        m.n_pools = n_pools - p0 < kPoolsPerLaunch ? n_pools - p0 : kPoolsPerLaunch;
-        for (int i = 0; i < m.n_pools; ++i) {
-            m.pool[i] = static_cast<unsigned char *>(pools[p0 + i]);
-            m.rows[i] = rows ? static_cast<const unsigned char *>(rows[p0 + i]) : nullptr;
-        }
-        const hipError_t e = launch_cache_move(append, m, s);
-        if (e != hipSuccess) return e;
-    }
-    return hipSuccess;
+    return launch_cache_move(append, m, pools, rows, n_pools, s);
+}
+
+size_t cache_workspace(const bdgdn_cache_desc_t *c, int32_t num_req, int32_t rows_max)
+{
+    return (cache_plan(num_req, rows_max, c->page, c->max_pages).ints * 4 + 255) & ~(size_t)255;
+}
+
+// The parts of a workspace.
+void place_workspace(CacheArgs &a, const bdgdn_cache_desc_t *c, void *workspace)
+{
+    const CachePlan p = cache_plan(a.R, a.rows_max, c->page, c->max_pages);
+    a.meta = static_cast<int32_t *>(workspace);
+    a.alloc = a.meta + p.alloc_at;
+    a.saved = p.one ? a.meta + p.saved_at : nullptr;
 }
 
 int check_pool_list(void *const *pools, const void *const *rows, bool with_rows, int n_pools)
@@ -245,7 +249,7 @@ int bdgdn_verify(const bdgdn_verify_desc_t *desc, const void *target, const void
 size_t bdgdn_cache_workspace(const bdgdn_cache_desc_t *cache, int32_t num_req, int32_t rows_max)
 {
     if (check_tables(cache) != BDGDN_OK || num_req <= 0 || rows_max < 0 || !countable(cache, num_req, rows_max)) return 0;
-    return cache_workspace(num_req, rows_max, cache->page);
+    return cache_workspace(cache, num_req, rows_max);
 }
 
 int bdgdn_cache_append(const bdgdn_cache_desc_t *cache, const bdgdn_cache_tables_t *tables, void *const *pools,
@@ -264,11 +268,10 @@ int bdgdn_cache_append(const bdgdn_cache_desc_t *cache, const bdgdn_cache_tables
     st = check_pool_list(pools, rows, nodes > 0, n_pools);
     if (st != BDGDN_OK) return st;
     if (!aligned(workspace, 256)) return BDGDN_ERR_INVALID_ARG;
-    if (!workspace || workspace_bytes < cache_workspace(num_req, nodes, cache->page)) return BDGDN_ERR_WORKSPACE;
+    if (!workspace || workspace_bytes < cache_workspace(cache, num_req, nodes)) return BDGDN_ERR_WORKSPACE;
     CacheArgs a = cache_args(cache, tables, num_req, slot, status);
     a.rows_max = nodes; a.path = path; a.count = count;
-    a.meta = static_cast<int32_t *>(workspace);
-    a.alloc = a.meta + (size_t)num_req * kMeta;
+    place_workspace(a, cache, workspace);
     hipStream_t s = static_cast<hipStream_t>(stream);
     hipError_t e = launch_cache_plan(true, a, s);
     if (e == hipSuccess && nodes > 0) e = move_pools(true, cache, a, pools, rows, n_pools, row_stride, s);
@@ -301,15 +304,14 @@ int bdgdn_cache_compact(const bdgdn_cache_desc_t *cache, const bdgdn_cache_table
     st = check_pool_list(pools, nullptr, false, n_pools);
     if (st != BDGDN_OK) return st;
     if (!aligned(workspace, 256)) return BDGDN_ERR_INVALID_ARG;
-    if (!workspace || workspace_bytes < cache_workspace(num_req, keep_max, cache->page)) return BDGDN_ERR_WORKSPACE;
+    if (!workspace || workspace_bytes < cache_workspace(cache, num_req, keep_max)) return BDGDN_ERR_WORKSPACE;
     CacheArgs a = cache_args(cache, tables, num_req, slot, status);
     a.rows_max = keep_max; a.path = keep; a.count = count;
-    a.meta = static_cast<int32_t *>(workspace);
-    a.alloc = a.meta + (size_t)num_req * kMeta;
+    place_workspace(a, cache, workspace);
     hipStream_t s = static_cast<hipStream_t>(stream);
     hipError_t e = launch_cache_plan(false, a, s);
     if (e == hipSuccess && keep_max > 0) e = move_pools(false, cache, a, pools, nullptr, n_pools, 0, s);
-    if (e == hipSuccess) e = launch_cache_finish(a, s);
+    if (e == hipSuccess && !a.saved) e = launch_cache_finish(a, s);
     return status_of(e);
 }
 

@@ -282,6 +282,44 @@ def test_many_requests_and_many_pages():
     c.check()
 
 
+@pytest.mark.parametrize("R,tokens,page,max_pages,n_pages,pools", [
+    (3, 700, 16, 50, 200, 1),        # planned by one workgroup
+    (300, 11, 2, 8, 3000, 1),        # by many: requests,
+    (2, 17000, 64, 300, 900, 1),     # positions,
+    (4, 300, 16, 5000, 160, 2),      # columns of the table
+    (2, 100, 8, 20, 60, 17),         # more pools than a small launch takes
+    (2, 40, 8, 20, 40, 100),         # more than any launch takes
+])
+def test_compactions_of_few_and_of_many(R, tokens, page, max_pages, n_pages, pools):
+    rng = random.Random(R * tokens)
+    c = Cache(R + 1, max_pages, n_pages, page, 1, 64, torch.bfloat16, pools, False)
+    slots, counts = list(range(R)), [tokens - i % 3 for i in range(R)]
+    ids, rows = c.rows(R, tokens)
+    want = c.model.append(slots, counts, ids)
+    assert bd.bdgdn_cache_append(c.tables, c.pools, rows, _ints(slots), _ints(counts)).tolist() == want
+    c.model.fork([0], [R])
+    bd.bdgdn_cache_fork(c.tables, _ints([0]), _ints([R]), page=page)
+    for turn in range(3):
+        keeps = []
+        for i in range(R):
+            n = c.model.len[i]
+            first = rng.randrange(n + 1) if i % 2 else 0     # some keep their beginnings
+            keeps.append([t for t in range(n) if t < first or rng.random() < 0.6])
+        asked = list(slots)
+        if turn == 1:
+            keeps[-1] = []
+            asked[0] = R + 7
+        if turn == 2 and len(keeps[0]) > 1:
+            keeps[0][1] = keeps[0][0]                        # does not rise
+        keep = torch.zeros(R, max(map(len, keeps)), dtype=torch.int32)
+        for i, k in enumerate(keeps):
+            keep[i, :len(k)] = torch.tensor(k, dtype=torch.int32)
+        want = c.model.compact(asked, keeps)
+        got = bd.bdgdn_cache_compact(c.tables, c.pools, _ints(asked), keep.cuda(), _ints([len(k) for k in keeps]))
+        assert got.tolist() == want
+        c.check()
+
+
 def test_nodes_that_are_none_and_rows_of_a_projection():
     c = Cache(2, 4, 8, 4, 2, 64, torch.bfloat16, 2, False)
     whole = torch.randn(2, 3, 6, 64, device="cuda").to(torch.bfloat16)
