@@ -84,15 +84,30 @@ __device__ __forceinline__ int length_of(const AttnArgs &a, int r)
 
 __device__ __forceinline__ int tiles_of(int len) { return (len + kTile - 1) / kTile; }
 
+// The length of request g.r, its tiles.
+__device__ __forceinline__ void go_to(const AttnArgs &a, Range &g)
+{
+    const int slot = a.slot ? ((TablePtr)(uintptr_t)a.slot)[g.r] : g.r;
+    g.len = (unsigned)slot < (unsigned)a.n_slots ? min(max(((TablePtr)(uintptr_t)a.len)[slot], 0), a.max_pages * a.page) : 0;
+    g.tiles = tiles_of(g.len);
+}
+
 __device__ __forceinline__ Range find_range(const AttnArgs &a, int w, int lane)
 {
+    Range g = {};
+    if (a.uncut) {
+        if (w >= a.R) return g;
+        g.r = w;
+        go_to(a, g);
+        g.end = g.size = g.tiles + a.node_units;
+        return g;
+    }
     const int len0 = lane < a.R ? length_of(a, lane) : 0;
     int sum = lane < a.R ? tiles_of(len0) + a.node_units : 0;
     for (int r = lane + 64; r < a.R; r += 64) sum += tiles_of(length_of(a, r)) + a.node_units;
 #pragma unroll
     for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
     sum = __builtin_amdgcn_readfirstlane(sum);
-    Range g = {};
     g.size = max(a.least, (sum + a.ranges - 1) / a.ranges);
     // (in 64 bits: ranges past the end may lie beyond 2^31)
     const long pos = (long)w * g.size;
@@ -154,9 +169,7 @@ __device__ __forceinline__ void next_piece(const AttnArgs &a, Range &g)
     if (g.pos >= g.end) return;
     ++g.r;
     g.off = 0;
-    const int slot = a.slot ? ((TablePtr)(uintptr_t)a.slot)[g.r] : g.r;
-    g.len = (unsigned)slot < (unsigned)a.n_slots ? min(max(((TablePtr)(uintptr_t)a.len)[slot], 0), a.max_pages * a.page) : 0;
-    g.tiles = tiles_of(g.len);
+    go_to(a, g);
 }
 
 // What the joining kernel needs to know of a request that a range begins.

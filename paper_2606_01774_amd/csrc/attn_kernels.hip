@@ -41,7 +41,7 @@ __global__ void __launch_bounds__(64 * kWaves, waves_per_simd(sizeof(T) == 2, D,
         const Piece it = piece_of(a, span, range);
         if (it.none) continue;
         const int count = a.count ? min(max(a.count[it.r], 0), a.N) : a.N;
-        if (span.off == 0 && kvh == 0 && rg == 0 && threadIdx.x == 0) note_request(a, span);
+        if (!a.uncut && span.off == 0 && kvh == 0 && rg == 0 && threadIdx.x == 0) note_request(a, span);
         w.init(a.c);
         int node[MT];
         load_rows(w, a, it.r, kvh, row0, node, g, rr);
@@ -195,7 +195,7 @@ template <typename T, int D, bool F32OUT> hipError_t launch_d(const AttnPlan &p,
                    : p.mt == 1 ? launch_m<T, D, 1, F32OUT>(p, a, s)
                    : p.mt == 2 ? launch_m<T, D, (most < 2 ? most : 2), F32OUT>(p, a, s)
                                : launch_m<T, D, most, F32OUT>(p, a, s);
-    if (e != hipSuccess) return e;
+    if (e != hipSuccess || p.uncut) return e;
     typedef typename std::conditional<F32OUT, float, __bf16>::type Out;
     // four waves to a row where requests have eight pieces or more (2 requests in 32 pieces, 96
     // rows of 128 to a key head: 19.4 us with one wave to a row, 10.5 with four; with two pieces
@@ -208,25 +208,31 @@ template <typename T, int D, bool F32OUT> hipError_t launch_d(const AttnPlan &p,
 
 }  // namespace
 
-AttnPlan attn_plan(bool bf16, int d, int page, int R, int N, int h_q, int h_kv)
+AttnPlan attn_plan(bool bf16, int d, int page, long most, int R, int N, int h_q, int h_kv)
 {
     AttnPlan p;
     const int M = N * (h_q / h_kv);
     p.staged = bf16 && page % 16 == 0;
     // a staged wave always has 32 rows, idle ones load for the others; a streaming wave has as
     // many 16-row groups as the rows fill, and waves without rows take tiles instead
-    const int groups = M <= 16 ? 1 : M <= 32 ? 2 : 4, most = most_mt(bf16, d);
-    p.mt = p.staged ? 2 : groups < most ? groups : most;
+    const int groups = M <= 16 ? 1 : M <= 32 ? 2 : 4, mt_most = most_mt(bf16, d);
+    p.mt = p.staged ? 2 : groups < mt_most ? groups : mt_most;
     const int waves = (M + 16 * p.mt - 1) / (16 * p.mt);
     p.RW = waves <= 1 && !p.staged ? 1 : waves <= 2 ? 2 : 4;
     p.RG = (waves + p.RW - 1) / p.RW;
     p.rows_padded = p.RG * p.RW * 16 * p.mt;
     // one range for every workgroup that the chip holds at once (one or two to a compute unit)
     const long heads = (long)h_kv * p.RG, ranges = 256 * (p.staged ? (d == 256 ? 1 : 2) : waves_per_simd(bf16, d, p.mt)) / heads;
-    p.ranges = (int)(ranges < 1 ? 1 : ranges);
+    // A table of few columns holds no long request: one workgroup (of a key head) takes each, and
+    // nothing is joined.  Of up to 128 tokens, 32 query heads on 8 of 128: 64 requests of 8 nodes 14.2 us where
+    // cutting takes 22.9, of 64 nodes 42 for 57, one of one node 14.3 for 16.5 (one of 64 nodes on
+    // one head of 256 24.7 for 23.5).  Of up to 256: 17.6 for 25, 14.1 for 16.8; but with heads of 256 one
+    // of one node 19.1 for 16.6, and with 192 rows in fp32 33 for 21.  Of up to 512: 19 for 16.6.
+    p.uncut = most <= 128 || (most <= 256 && M <= 64 && d <= 128);
+    p.ranges = p.uncut ? R : (int)(ranges < 1 ? 1 : ranges);
     p.least = 4;   // tiles of a range, one to a wave
     p.grid = (int)(((long)p.ranges * h_kv + 7) / 8 * 8 * p.RG);
-    const size_t rows = 2 * (size_t)p.ranges * h_kv * p.rows_padded;
+    const size_t rows = p.uncut ? 0 : 2 * (size_t)p.ranges * h_kv * p.rows_padded;
     p.ml_at = ((size_t)(1 + 2 * (size_t)R) * 4 + 255) & ~(size_t)255;
     p.o_at = p.ml_at + ((rows * 8 + 255) & ~(size_t)255);
     p.bytes = p.o_at + rows * d * 4;
@@ -239,6 +245,7 @@ hipError_t launch_tree_attn(bool bf16, bool f32_out, int d, const AttnPlan &p, A
     a.RG = p.RG;
     a.ranges = p.ranges;
     a.least = p.least;
+    a.uncut = p.uncut;
     a.node_units = 4 + p.RW * p.mt / 2;
     a.rows_padded = p.rows_padded;
     char *ws = static_cast<char *>(workspace);

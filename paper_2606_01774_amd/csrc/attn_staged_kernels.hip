@@ -90,7 +90,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) bdgdn_tree_attn_staged_
         const Piece it = piece_of(a, span, range);
         if (it.none) continue;
         const int count = a.count ? min(max(a.count[it.r], 0), a.N) : a.N;
-        if (span.off == 0 && kvh == 0 && rg == 0 && threadIdx.x == 0) note_request(a, span);
+        if (!a.uncut && span.off == 0 && kvh == 0 && rg == 0 && threadIdx.x == 0) note_request(a, span);
         const TablePtr table = table_of(a, it.r);
         const int n = (it.t1 - it.t0 + X::TILES - 1) / X::TILES;   // stages
         int pages[2];

@@ -31,15 +31,17 @@ struct AttnArgs {
     int rows_padded;           // rows of a key head, filled up to those of RW x RG waves
     int node_units;            // tiles that a request's nodes, queries and output count as
     int ranges, least;         // ranges that the keys are cut into, at most, and their tiles, at least
+    int uncut;                 // a range is a request
 };
 
 // How a call is cut: 16-row groups of a wave, the above, workgroups, and the workspace.
 struct AttnPlan {
     bool staged;               // the kernel that stages tiles in LDS
+    bool uncut;                // every request is one piece
     int mt, RW, RG, rows_padded, ranges, least, grid;
     size_t ml_at, o_at, bytes;
 };
-AttnPlan attn_plan(bool bf16, int d, int page, int R, int N, int h_q, int h_kv);
+AttnPlan attn_plan(bool bf16, int d, int page, long most, int R, int N, int h_q, int h_kv);
 hipError_t launch_tree_attn(bool bf16, bool f32_out, int d, const AttnPlan &p, AttnArgs &a, void *workspace, hipStream_t s);
 hipError_t launch_tree_attn_staged(bool f32_out, int d, int grid, const AttnArgs &a, hipStream_t s);
 hipError_t launch_tree_mask(int R, int N, const int32_t *parent, uint64_t *mask, int32_t *depth, hipStream_t s);

@@ -153,7 +153,7 @@ extern "C" {
 size_t bdgdn_tree_attn_workspace(const bdgdn_attn_desc_t *desc, const bdgdn_cache_desc_t *cache)
 {
     if (check_attn(desc, cache) != BDGDN_OK || desc->num_req == 0) return 0;
-    return attn_plan(desc->dtype == BDGDN_BF16, desc->d, cache->page, desc->num_req, desc->nodes, desc->h_q, desc->h_kv).bytes;
+    return attn_plan(desc->dtype == BDGDN_BF16, desc->d, cache->page, (long)cache->max_pages * cache->page, desc->num_req, desc->nodes, desc->h_q, desc->h_kv).bytes;
 }
 
 int bdgdn_tree_attn(const bdgdn_attn_desc_t *desc, const bdgdn_cache_desc_t *cache, const void *q,
@@ -172,7 +172,7 @@ int bdgdn_tree_attn(const bdgdn_attn_desc_t *desc, const bdgdn_cache_desc_t *cac
         !aligned(o, 16) || !aligned(mask, 8))
         return BDGDN_ERR_INVALID_ARG;
     const bool bf16 = desc->dtype == BDGDN_BF16;
-    const AttnPlan p = attn_plan(bf16, desc->d, cache->page, desc->num_req, desc->nodes, desc->h_q, desc->h_kv);
+    const AttnPlan p = attn_plan(bf16, desc->d, cache->page, (long)cache->max_pages * cache->page, desc->num_req, desc->nodes, desc->h_q, desc->h_kv);
     if (!aligned(workspace, 256)) return BDGDN_ERR_INVALID_ARG;
     if (workspace_bytes < p.bytes || !workspace) return BDGDN_ERR_WORKSPACE;
     const long size = size_of(desc->dtype);

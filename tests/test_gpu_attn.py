@@ -277,3 +277,61 @@ def test_masks_of_trees(N):
                     break
                 a, up = a2, up + 1
             assert int(mask[r, n]) & (2 ** 64 - 1) == word and int(depth[r, n]) == up
+
+
+@pytest.fixture
+def wide_tables(monkeypatch):
+    """Cases whose tables have room for long requests, which are cut into pieces however short they are."""
+    narrow = _case
+    monkeypatch.setitem(globals(), "_case", lambda *args, **kw: narrow(*args, **{**kw, "max_pages": 700}))
+
+
+@pytest.mark.parametrize("dtype,h_q", [("bf16", 4), ("f32", 4), ("bf16", 16)])
+@pytest.mark.parametrize("page", [16, 32, 20])
+def test_nothing_unseen_enters_from_wide_tables(wide_tables, dtype, h_q, page):
+    test_nothing_unseen_enters(dtype, h_q, page)
+
+
+@pytest.mark.parametrize("dtype,page", [("bf16", 32), ("f32", 32), ("bf16", 20)])
+def test_what_is_seen_is_not_hidden_by_wide_tables(wide_tables, dtype, page):
+    test_what_is_seen_is_not_hidden(dtype, page)
+
+
+_SHORT = [
+    (1, 1, 4, 1, 128, 16, [128], "bf16", "bf16", "full", False),
+    (3, 8, 8, 2, 128, 16, [0, 127, 1], "bf16", "f32", "causal", True),
+    (2, 16, 8, 2, 128, 32, [256, 200], "bf16", "bf16", "tree", False),
+    (2, 17, 8, 2, 128, 32, [256, 33], "bf16", "bf16", "full", False),
+    (2, 64, 16, 2, 64, 16, [111, 96], "bf16", "bf16", "causal", False),
+    (2, 64, 8, 1, 256, 64, [64, 30], "bf16", "f32", "full", False),
+    (2, 5, 6, 3, 256, 64, [128, 90], "bf16", "bf16", "causal", False),
+    (2, 6, 4, 2, 128, 12, [120, 5], "bf16", "bf16", "tree", False),
+    (2, 50, 8, 2, 64, 20, [100, 61], "bf16", "bf16", "full", False),
+    (3, 7, 4, 2, 128, 24, [240, 0, 17], "f32", "f32", "tree", True),
+    (1, 40, 8, 2, 256, 16, [128], "f32", "f32", "causal", False),
+    (600, 2, 4, 2, 64, 16, [(53 * i) % 113 for i in range(600)], "bf16", "bf16", "causal", False),
+]
+
+
+@pytest.mark.parametrize("case", range(len(_SHORT)))
+def test_short_requests(case):
+    test_against_the_definition(*_SHORT[case])
+
+
+@pytest.mark.parametrize("case", range(len(_SHORT)))
+def test_short_requests_in_wide_tables(wide_tables, case):
+    test_against_the_definition(*_SHORT[case])
+
+
+def test_narrow_tables_with_lengths_past_their_end_and_odd_slots():
+    """Lengths beyond the columns, negative ones, slots that are none."""
+    c = _case(4, 5, 4, 2, 128, 16, [64, 20, 31, 64], "bf16", seed=4)
+    table = c["table"][:, :4].contiguous()
+    seq = torch.tensor([100000, 20, 31, 64], dtype=torch.int32).cuda()
+    got = bd.bdgdn_tree_attn(c["q"], c["k"], c["v"], c["kp"], c["vp"], table, seq, mask="causal", want_lse=True)
+    _compare(c, got, "causal", 1 / math.sqrt(128), "bf16", "bf16")
+    seq[1] = -5
+    slot = torch.tensor([0, 1, -1, 4], dtype=torch.int32).cuda()
+    got = bd.bdgdn_tree_attn(c["q"], c["k"], c["v"], c["kp"], c["vp"], table, seq, mask="causal", want_lse=True, slot=slot)
+    c["lens"] = [64, 0, 0, 0]
+    _compare(c, got, "causal", 1 / math.sqrt(128), "bf16", "bf16")
