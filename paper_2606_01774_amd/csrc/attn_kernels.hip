@@ -85,18 +85,23 @@ __global__ void __launch_bounds__(64 * kWaves, waves_per_simd(sizeof(T) == 2, D,
     }
 }
 
-// One workgroup per (request, key head, 16 / W rows), 16 lanes to a row, W waves to a row's
-// pieces:  o = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s over the pieces s of a request.
+// Threads of a joining workgroup, and its rows: D / 4 lanes to a row, W waves to the pieces of
+// one wave's rows.
+constexpr int join_threads(int W) { return W > 4 ? 64 * W : 256; }
+constexpr int join_rows(int d, int W) { return join_threads(W) / 64 / W * (256 / d); }
+
+// One workgroup per (request, key head, some rows):
+// o = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s over the pieces s of a request.
 // Bound by memory where there are many requests (64 in two pieces each, 128 rows of 128 to a
 // key head: 13.4 us, 70 MB), by latency where there are few.
-template <typename Out, int D, int W> __global__ void __launch_bounds__(256) bdgdn_tree_attn_join_kernel(AttnArgs a, int row_tiles)
+template <typename Out, int D, int W> __global__ void __launch_bounds__(join_threads(W)) bdgdn_tree_attn_join_kernel(AttnArgs a, int row_tiles)
 {
-    constexpr int C = D / 64;   // float4s of a lane
+    constexpr int LANES = D / 4, ROWS = join_rows(D, W);
     const int tile = blockIdx.x % row_tiles, rest = blockIdx.x / row_tiles, kvh = rest % a.h_kv, r = rest / a.h_kv;
     const int size = a.info[0], pos = a.info[1 + 2 * r], w0 = pos / size, splits = (pos + a.info[2 + 2 * r] - 1) / size - w0 + 1;
     if (splits == 1) return;   // one piece, whose workgroup wrote the result
-    const int lane = threadIdx.x & 63, wave = wave_id(), part = wave % W, c = lane & 15;
-    const int row = tile * (16 / W) + wave / W * 4 + (lane >> 4);
+    const int lane = threadIdx.x & 63, wave = wave_id(), part = wave % W, c = lane % LANES;
+    const int row = tile * ROWS + wave / W * (64 / LANES) + lane / LANES;
     const bool there = row < a.N * a.G;
     // the first piece ends its range unless it begins there too, the others begin theirs
     const int second = pos % size != 0;
@@ -104,56 +109,50 @@ template <typename Out, int D, int W> __global__ void __launch_bounds__(256) bdg
         return ((long)(2 * (w0 + s) + (s == 0 ? second : 0)) * a.h_kv + kvh) * a.rows_padded + row;
     };
     float top = -INFINITY, l = 0.f;
-    f32x4 o[C] = {};
+    f32x4 o = {0, 0, 0, 0};
     if (there) {
-        // (each wave takes the maximum and the sum of all of them: only the outputs are many)
-        for (int s = c; s < splits; s += 16) top = fmaxf(top, a.part_ml[2 * place(s)]);
+        // (each wave takes the maximum and the sum of all pieces: only the outputs are many)
+        for (int s = c; s < splits; s += LANES) top = fmaxf(top, a.part_ml[2 * place(s)]);
 #pragma unroll
-        for (int x = 8; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
+        for (int x = LANES / 2; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
         const float ref = top == -INFINITY ? 0.f : top;
-        for (int s0 = 0; s0 < splits; s0 += 16) {
+        for (int s0 = 0; s0 < splits; s0 += LANES) {
             float f = 0.f;
             if (s0 + c < splits) {
                 const long at = place(s0 + c);
                 f = fexp2(a.part_ml[2 * at] - ref);
                 l += f * a.part_ml[2 * at + 1];
             }
-            const int n = min(16, splits - s0);
-#pragma unroll (W == 1 ? 8 : 4)
-            for (int i = part; i < n; i += W) {
-                const float fi = __shfl(f, (lane & 48) + i);
-                const f32x4 *po = reinterpret_cast<const f32x4 *>(a.part_o + place(s0 + i) * D) + c;
-#pragma unroll
-                for (int x = 0; x < C; ++x) o[x] += fi * po[16 * x];
-            }
+            const int n = min(LANES, splits - s0);
+#pragma unroll 8
+            for (int i = part; i < n; i += W)
+                o += __shfl(f, lane - c + i) * reinterpret_cast<const f32x4 *>(a.part_o + place(s0 + i) * D)[c];
         }
 #pragma unroll
-        for (int x = 8; x; x >>= 1) l += __shfl_xor(l, x);
+        for (int x = LANES / 2; x; x >>= 1) l += __shfl_xor(l, x);
     }
     if (W > 1) {
-        __shared__ f32x4 s_o[W][C][64];
-        if (part)
-#pragma unroll
-            for (int x = 0; x < C; ++x) s_o[part][x][lane] = o[x];
+        __shared__ f32x4 s_o[W][64];
+        if (part) s_o[part][lane] = o;
         __syncthreads();
         if (part) return;
 #pragma unroll
-        for (int w = 1; w < W; ++w)
-#pragma unroll
-            for (int x = 0; x < C; ++x) o[x] += s_o[w][x][lane];
+        for (int w = 1; w < W; ++w) o += s_o[w][lane];
     }
     if (!there) return;
     const int n = row / a.G, count = a.count ? min(max(a.count[r], 0), a.N) : a.N;
     const bool none = n >= count || l == 0.f;
     const long at = ((long)r * a.N + n) * a.h_q + kvh * a.G + row - n * a.G;
-    Out *out = static_cast<Out *>(a.o) + at * D + 4 * c;
     const float inv = none ? 0.f : 1.f / l;
-#pragma unroll
-    for (int x = 0; x < C; ++x) {
-        const f32x4 y = none ? f32x4{0, 0, 0, 0} : o[x] * inv;
-        st4(out + 64 * x, y[0], y[1], y[2], y[3]);
-    }
+    const f32x4 y = none ? f32x4{0, 0, 0, 0} : o * inv;
+    st4(static_cast<Out *>(a.o) + at * D + 4 * c, y[0], y[1], y[2], y[3]);
     if (a.lse && c == 0) a.lse[at] = none ? -INFINITY : (top + __log2f(l)) * 0.6931471805599453f;
+}
+
+template <typename Out, int D, int W> void launch_join(const AttnArgs &a, hipStream_t s)
+{
+    const int row_tiles = (a.N * a.G + join_rows(D, W) - 1) / join_rows(D, W);
+    bdgdn_tree_attn_join_kernel<Out, D, W><<<a.R * a.h_kv * row_tiles, join_threads(W), 0, s>>>(a, row_tiles);
 }
 
 __global__ void __launch_bounds__(64) bdgdn_tree_mask_kernel(int N, const int32_t *parent, uint64_t *mask, int32_t *depth)
@@ -197,12 +196,9 @@ template <typename T, int D, bool F32OUT> hipError_t launch_d(const AttnPlan &p,
                                : launch_m<T, D, most, F32OUT>(p, a, s);
     if (e != hipSuccess || p.uncut) return e;
     typedef typename std::conditional<F32OUT, float, __bf16>::type Out;
-    // four waves to a row where requests have eight pieces or more (2 requests in 32 pieces, 96
-    // rows of 128 to a key head: 19.4 us with one wave to a row, 10.5 with four; with two pieces
-    // to a request three of them would have nothing to do)
-    const int M = a.N * a.G;
-    if (p.ranges >= 8 * a.R) bdgdn_tree_attn_join_kernel<Out, D, 4><<<a.R * a.h_kv * ((M + 3) / 4), 256, 0, s>>>(a, (M + 3) / 4);
-    else bdgdn_tree_attn_join_kernel<Out, D, 1><<<a.R * a.h_kv * ((M + 15) / 16), 256, 0, s>>>(a, (M + 15) / 16);
+    if (p.ranges >= 64 * a.R) launch_join<Out, D, 16>(a, s);
+    else if (p.ranges >= 8 * a.R) launch_join<Out, D, 4>(a, s);
+    else launch_join<Out, D, 1>(a, s);
     return hipGetLastError();
 }
 
