@@ -1,13 +1,14 @@
 // attn_kernels.hip -- attention of a block of nodes over a paged cache and over the nodes
-// themselves: the kernel for fp32 and for pages of any size, the joining kernel, tree masks,
-// dispatch.  (bf16 over pages of whole runs of 16 tokens takes the kernel of
+// themselves: the kernel for fp32, and for few rows over pages of any size, the joining kernel,
+// tree masks, dispatch.  (bf16 over pages of whole runs of 16 tokens takes the kernel of
 // attn_staged_kernels.hip, which is never slower: one node on 64 requests of up to 4096 tokens
 // 112 against 114 us, four 119 against 122, eight 128 against 135, 32 157 against 259.)
 //
 // One wave streams its tiles from memory to registers, the next keys requested when the scores
 // are done with these and the next values when the output is.  Four waves are a workgroup:
 // those with different rows take the same keys, those with the same rows every KW-th tile,
-// and are joined through LDS.  Latency bounds it: a wave has one tile on its way at a time.
+// and are joined through LDS.  Latency bounds it: a wave has one tile on its way at a time.  3 requests of up to 1003
+// tokens in fp32, 15 rows of 64 to a key head: 9 us, and 4 to join them.
 #include <type_traits>
 
 #include "attn.hpp"
@@ -19,10 +20,10 @@ namespace {
 constexpr int kWaves = 4;          // of a workgroup
 
 // Waves of a SIMD that a kernel's registers allow (two of up to 256, one of more).
-constexpr int waves_per_simd(bool bf16, int d, int mt) { return bf16 ? (mt * d <= 256 && d < 256 ? 2 : 1) : d == 64 ? 2 : 1; }
+constexpr int waves_per_simd(bool bf16, int d) { return d == 64 || (bf16 && d == 128) ? 2 : 1; }
 
 template <typename T, int D, int MT, bool SPLITP, bool HALVES, typename Out>
-__global__ void __launch_bounds__(64 * kWaves, waves_per_simd(sizeof(T) == 2, D, MT)) bdgdn_tree_attn_kernel(AttnArgs a)
+__global__ void __launch_bounds__(64 * kWaves, waves_per_simd(sizeof(T) == 2, D)) bdgdn_tree_attn_kernel(AttnArgs a)
 {
     typedef Geo<T, D> G;
     __shared__ f32x4 s_o[2][G::NT][64];
@@ -197,7 +198,7 @@ __global__ void __launch_bounds__(64) bdgdn_tree_mask_kernel(int N, const int32_
 }
 
 // 16-row groups of a wave at most: what its registers hold, 512 a lane.
-constexpr int most_mt(bool bf16, int d) { return d == 256 ? 1 : bf16 ? 4 : 2; }
+constexpr int most_mt(int d) { return d == 256 ? 1 : 2; }
 
 template <typename T, int D, int MT, bool F32OUT> hipError_t launch_m(const AttnPlan &p, const AttnArgs &a, hipStream_t s)
 {
@@ -211,10 +212,9 @@ template <typename T, int D, int MT, bool F32OUT> hipError_t launch_m(const Attn
 
 template <typename T, int D, bool F32OUT> hipError_t launch_d(const AttnPlan &p, const AttnArgs &a, hipStream_t s)
 {
-    constexpr int most = most_mt(sizeof(T) == 2, D);
+    constexpr int most = most_mt(D);
     hipError_t e = p.staged ? launch_tree_attn_staged(F32OUT, D, p.grid, a, s)
                    : p.mt == 1 ? launch_m<T, D, 1, F32OUT>(p, a, s)
-                   : p.mt == 2 ? launch_m<T, D, (most < 2 ? most : 2), F32OUT>(p, a, s)
                                : launch_m<T, D, most, F32OUT>(p, a, s);
     if (e != hipSuccess || p.uncut) return e;
     typedef typename std::conditional<F32OUT, float, __bf16>::type Out;
@@ -234,17 +234,20 @@ AttnPlan attn_plan(bool bf16, int d, int page, long most, int R, int N, int h_q,
 {
     AttnPlan p;
     const int M = N * (h_q / h_kv);
-    p.staged = bf16 && page % 16 == 0;
+    // Pages of other sizes: a staged wave's rows have an address to a lane, which pays from 33 rows to a
+    // key head on.  16 requests of up to 4000 tokens, pages of 24 and 8 key heads of 256: 96 rows 142 us
+    // staged and 246 streamed, but 24 rows 98 and 91, four 92 and 70; pages of 100, 4 heads of 128: 48 rows
+    // 32 and 42, two 25 and 24.
+    p.staged = bf16 && (page % 16 == 0 || M > 32);
     // a staged wave always has 32 rows, idle ones load for the others; a streaming wave has as
     // many 16-row groups as the rows fill, and waves without rows take tiles instead
-    const int groups = M <= 16 ? 1 : M <= 32 ? 2 : 4, mt_most = most_mt(bf16, d);
-    p.mt = p.staged ? 2 : groups < mt_most ? groups : mt_most;
+    p.mt = p.staged ? 2 : M <= 16 ? 1 : most_mt(d);
     const int waves = (M + 16 * p.mt - 1) / (16 * p.mt);
     p.RW = waves <= 1 && !p.staged ? 1 : waves <= 2 ? 2 : 4;
     p.RG = (waves + p.RW - 1) / p.RW;
     p.rows_padded = p.RG * p.RW * 16 * p.mt;
     // one range for every workgroup that the chip holds at once (one or two to a compute unit)
-    const long heads = (long)h_kv * p.RG, ranges = 256 * (p.staged ? (d == 256 ? 1 : 2) : waves_per_simd(bf16, d, p.mt)) / heads;
+    const long heads = (long)h_kv * p.RG, ranges = 256 * (p.staged ? (d == 256 ? 1 : 2) : waves_per_simd(bf16, d)) / heads;
     // A table of few columns holds no long request: one workgroup (of a key head) takes each, and
     // nothing is joined.  Of up to 128 tokens, 32 query heads on 8 of 128: 64 requests of 8 nodes 14.2 us where
     // cutting takes 22.9, of 64 nodes 42 for 57, one of one node 14.3 for 16.5 (one of 64 nodes on

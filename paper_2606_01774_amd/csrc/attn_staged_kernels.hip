@@ -1,5 +1,6 @@
 // attn_staged_kernels.hip -- attention of a block of nodes over a paged cache: the kernel for bf16
-// over pages of whole runs of 16 tokens.
+// over pages of whole runs of 16 tokens (HALVES: a tile is two runs of rows), and for many rows
+// over pages of any size (each lane asks the one that has looked a key's page up).
 //
 // Four waves are a workgroup of RW x KW: RW (two or four) have 32 rows each and read the same
 // tiles, KW take different tiles.  Tiles go from memory to LDS without passing through
@@ -48,7 +49,7 @@ template <int N> __device__ __forceinline__ void wait_loads_barrier()
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-template <int D, int RW, bool SPLITP, typename Out>
+template <int D, int RW, bool HALVES, bool SPLITP, typename Out>
 __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) bdgdn_tree_attn_staged_kernel(AttnArgs a)
 {
     typedef __bf16 T;
@@ -74,12 +75,14 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) bdgdn_tree_attn_staged_
     const unsigned char *pool = static_cast<const unsigned char *>(is_value ? a.vp : a.kp) + (long)kvh * a.head_stride;
     for (; span.pos < span.end; next_piece(a, span)) {
         const int lane = lane_anew(), g = lane >> 4, rr = lane & 15;
-        uint32_t off[LOADS];
+        // HALVES (a page holds whole runs of 16 tokens): this lane's chunks behind the first of their run
+        uint32_t off[HALVES ? LOADS : 1];
+        if (HALVES)
 #pragma unroll
-        for (int l = 0; l < LOADS; ++l) {
-            const int key = first + l * ROWS + lane / CH;
-            off[l] = (key & 15) * a.token16 * 16 + X::place(lane % CH, key) * 16;
-        }
+            for (int l = 0; l < LOADS; ++l) {
+                const int key = first + l * ROWS + lane / CH;
+                off[HALVES ? l : 0] = (key & 15) * a.token16 * 16 + X::place(lane % CH, key) * 16;
+            }
         // where this lane's chunks of keys and values lie in a tile
         int ko[G::NK], vo[4];
 #pragma unroll
@@ -93,8 +96,13 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) bdgdn_tree_attn_staged_
         if (!a.uncut && span.off == 0 && kvh == 0 && rg == 0 && threadIdx.x == 0) note_request(a, span);
         const TablePtr table = table_of(a, it.r);
         const int n = (it.t1 - it.t0 + X::TILES - 1) / X::TILES;   // stages
-        int pages[2];
+        int pages[2];   // HALVES: of the tile's runs, else of key lane & 31
         const auto look_up = [&](int i) {
+            if (!HALVES) {
+                const int t = it.t0 + i * X::TILES + ltile, tok = t * kTile + (lane & 31);
+                pages[0] = t < it.t1 && tok < it.len ? ((const int32_t *)(uintptr_t)table)[column(a, tok)] : -1;
+                return;
+            }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int t = it.t0 + i * X::TILES + ltile, tok = t * kTile + 16 * h;
@@ -104,6 +112,23 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) bdgdn_tree_attn_staged_
         const auto request = [&](int i) {
             const int tok0 = (it.t0 + i * X::TILES + ltile) * kTile;
             const int buf = i % S;
+            if (!HALVES) {
+                const int tok = tok0 + (lane & 31);
+                const bool there = (unsigned)pages[0] < (unsigned)a.n_pages;
+                const uint32_t where = there ? pages[0] * a.page16 + (uint32_t)(tok - column(a, tok) * a.page) * a.token16 : 0;
+                const uint32_t seen = (uint32_t)__ballot(there);
+                if (!is_value && lane == 0) {
+                    s_seen[buf][ltile][0] = seen & 0xffffu;
+                    s_seen[buf][ltile][1] = seen >> 16;
+                }
+#pragma unroll
+                for (int l = 0; l < LOADS; ++l) {
+                    const int key = first + l * ROWS + lane / CH;
+                    const unsigned char *p = pool + (long)(uint32_t)__shfl((int)where, key) * 16 + X::place(lane % CH, key) * 16;
+                    __builtin_amdgcn_global_load_lds((GlobalPtr)p, (LdsPtr)&lds[buf * X::STAGE + (block + l) * 64], 16, 0, 0);
+                }
+                return;
+            }
             const unsigned char *at[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -117,7 +142,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) bdgdn_tree_attn_staged_
 #pragma unroll
             for (int l = 0; l < LOADS; ++l) {
                 // (held as 32 bits, so that the address is a scalar base and a lane's offset)
-                uint32_t lane_off = off[l];
+                uint32_t lane_off = off[HALVES ? l : 0];
                 asm("" : "+v"(lane_off));
                 const unsigned char *p = at[(first + l * ROWS) >> 4] + lane_off;
                 __builtin_amdgcn_global_load_lds((GlobalPtr)p, (LdsPtr)&lds[buf * X::STAGE + (block + l) * 64], 16, 0, 0);
@@ -195,12 +220,12 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) bdgdn_tree_attn_staged_
     }
 }
 
-template <int D, int RW, bool SPLITP, typename Out> hipError_t launch(int grid, const AttnArgs &a, hipStream_t s)
+template <int D, int RW, bool HALVES, bool SPLITP, typename Out> hipError_t launch(int grid, const AttnArgs &a, hipStream_t s)
 {
     typedef Staged<D, RW> X;
     static std::once_flag once;
     static hipError_t err;
-    const auto kernel = bdgdn_tree_attn_staged_kernel<D, RW, SPLITP, Out>;
+    const auto kernel = bdgdn_tree_attn_staged_kernel<D, RW, HALVES, SPLITP, Out>;
     std::call_once(once, [&] {
         err = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, X::LDS);
     });
@@ -211,7 +236,8 @@ template <int D, int RW, bool SPLITP, typename Out> hipError_t launch(int grid, 
 
 template <int D, bool SPLITP, typename Out> hipError_t launch_rw(int grid, const AttnArgs &a, hipStream_t s)
 {
-    return a.RW == 2 ? launch<D, 2, SPLITP, Out>(grid, a, s) : launch<D, 4, SPLITP, Out>(grid, a, s);
+    if (a.page % 16 == 0) return a.RW == 2 ? launch<D, 2, true, SPLITP, Out>(grid, a, s) : launch<D, 4, true, SPLITP, Out>(grid, a, s);
+    return a.RW == 2 ? launch<D, 2, false, SPLITP, Out>(grid, a, s) : launch<D, 4, false, SPLITP, Out>(grid, a, s);
 }
 
 }  // namespace

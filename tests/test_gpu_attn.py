@@ -335,3 +335,18 @@ def test_narrow_tables_with_lengths_past_their_end_and_odd_slots():
     got = bd.bdgdn_tree_attn(c["q"], c["k"], c["v"], c["kp"], c["vp"], table, seq, mask="causal", want_lse=True, slot=slot)
     c["lens"] = [64, 0, 0, 0]
     _compare(c, got, "causal", 1 / math.sqrt(128), "bf16", "bf16")
+
+
+@pytest.mark.parametrize("R,N,h_q,h_kv,d,page,lens,dtype,out,mask,htd", [
+    # many rows to a key head over pages that are not whole runs of 16 tokens
+    (2, 40, 8, 2, 128, 24, [700, 77], "bf16", "bf16", "causal", False),
+    (1, 64, 8, 1, 128, 1, [450], "bf16", "f32", "tree", True),
+    (2, 30, 8, 2, 256, 20, [129, 912], "bf16", "bf16", "full", False),
+    (2, 11, 4, 1, 256, 100, [1300, 0], "bf16", "f32", "causal", True),
+    (3, 12, 8, 2, 64, 36, [5, 700, 36], "bf16", "bf16", "tree", False),
+    (1, 50, 8, 2, 64, 7, [333], "bf16", "f32", "causal", False),
+    (2, 10, 4, 1, 128, 100, [1500, 99], "bf16", "bf16", "full", True),
+    (90, 9, 4, 1, 128, 40, [(91 * i) % 390 for i in range(90)], "bf16", "bf16", "causal", False),
+])
+def test_many_rows_over_odd_pages(R, N, h_q, h_kv, d, page, lens, dtype, out, mask, htd):
+    test_against_the_definition(R, N, h_q, h_kv, d, page, lens, dtype, out, mask, htd)
