@@ -113,15 +113,15 @@ def _check_pool(shape, strides, name):
 
 def _row_stride(shape, strides, name):
     """Elements between the nodes' rows of [R, N, h, d], which may be a part of longer rows; 0
-    for contiguous ones."""
+    for contiguous ones, which is why rows that share memory (an expanded tensor's) are refused."""
     if len(shape) != 4:
         raise ValueError(f"{name} must be [R, N, heads, d]")
     R, N, h, d = shape
     if R * N == 0:
         return 0
     row = strides[1] if N > 1 else strides[0] if R > 1 else h * d
-    if (d > 1 and strides[3] != 1) or (h > 1 and strides[2] != d) or (R > 1 and N > 1 and strides[0] != N * row):
-        raise ValueError(f"{name} must have contiguous heads and one stride between its rows")
+    if (d > 1 and strides[3] != 1) or (h > 1 and strides[2] != d) or (R > 1 and N > 1 and strides[0] != N * row) or row < h * d:
+        raise ValueError(f"{name} must have contiguous heads and one stride between its rows, which share no memory")
     return 0 if row == h * d else row
 
 

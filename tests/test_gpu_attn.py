@@ -350,3 +350,17 @@ def test_narrow_tables_with_lengths_past_their_end_and_odd_slots():
 ])
 def test_many_rows_over_odd_pages(R, N, h_q, h_kv, d, page, lens, dtype, out, mask, htd):
     test_against_the_definition(R, N, h_q, h_kv, d, page, lens, dtype, out, mask, htd)
+
+
+def test_expanded_inputs_are_refused():
+    """One row for all requests, as a fork's first token has it: refused, and taken as a copy."""
+    c = _case(4, 1, 8, 2, 128, 16, [40, 0, 7, 16], "bf16", seed=15)
+    args = (c["kp"], c["vp"], c["table"], c["seq"])
+    for name in ("q", "k", "v"):
+        x = {n: c[n] for n in ("q", "k", "v")}
+        x[name] = x[name][:1].expand(4, -1, -1, -1)
+        with pytest.raises(ValueError, match=f"{name} must have"):
+            bd.bdgdn_tree_attn(x["q"], x["k"], x["v"], *args)
+        kept, c[name] = c[name], x[name].contiguous()
+        _compare(c, bd.bdgdn_tree_attn(c["q"], c["k"], c["v"], *args, want_lse=True), "full", 1 / math.sqrt(128), "bf16", "bf16")
+        c[name] = kept

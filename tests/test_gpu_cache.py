@@ -376,3 +376,15 @@ def test_a_replayed_graph_of_a_round():
         torch.cuda.synchronize()
         for a, b in zip((*made[0].tables, *made[0].pools), (*made[1].tables, *made[1].pools)):
             assert torch.equal(a, b)
+
+
+def test_expanded_rows_are_refused():
+    """One first row for all ways of a fork: refused, and taken as a copy."""
+    c = Cache(3, 4, 8, 4, 1, 64, torch.float32, 1, False)
+    row = torch.randn(1, 1, 1, 64, device="cuda")
+    with pytest.raises(ValueError, match="must have"):
+        bd.bdgdn_cache_append(c.tables, c.pools, [row.expand(3, 1, 1, 64)], _ints([0, 1, 2]), _ints([1, 1, 1]))
+    c.check()
+    bd.bdgdn_cache_append(c.tables, c.pools, [row.expand(3, 1, 1, 64).contiguous()], _ints([0, 1, 2]), _ints([1, 1, 1]))
+    for page in c.tables.page_table[:, 0].tolist():
+        assert torch.equal(c.pools[0][page, 0], row[0, 0])

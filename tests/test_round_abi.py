@@ -190,3 +190,47 @@ def test_binding_refuses():
         bd.bdgdn_verify(torch.zeros(1, 2, 3), x, x, x)
     with pytest.raises(ValueError, match="at least one pool"):
         bd.bdgdn_cache_append(bd.make_cache_tables(1, 1, 1, device="cpu"), [], [], x, x)
+
+
+_EXPANDED = [((1, 1), (64, 1)), ((1, 1), (16, 4)), ((1, 1), (1, 4)), ((1, 4), (3, 4)), ((3, 1), (3, 4))]
+
+
+@pytest.mark.parametrize("made,seen", _EXPANDED)
+@pytest.mark.parametrize("name", ["q", "k", "v"])
+def test_attention_refuses_expanded_inputs(name, made, seen):
+    """Rows that share memory have no stride that the library knows: its 0 stands for contiguous rows."""
+    (R, N), d = seen, 128
+    x = dict(q=torch.zeros(R, N, 8, d), k=torch.zeros(R, N, 2, d), v=torch.zeros(R, N, 2, d))
+
+    def plan():
+        pool = torch.zeros(3, 16, 2, d)
+        args = [y for t in (x["q"], x["k"], x["v"], pool, pool) for y in (t.shape, t.stride())]
+        return rounds._attn_plan(*args, (R, 4), R, None, torch.float32, torch.float32, bd.BDGDN_MASK_FULL)
+
+    assert plan()[2] > 0
+    x[name] = torch.zeros(*made, *x[name].shape[2:]).expand(x[name].shape)
+    with pytest.raises(ValueError, match=f"{name} must have"):
+        plan()
+
+
+@pytest.mark.parametrize("made,seen", _EXPANDED)
+def test_append_refuses_expanded_rows(made, seen):
+    pool, table = torch.zeros(3, 16, 2, 64), (80, 4)
+
+    def plan(rows):
+        return rounds._pools_plan(table, 3, pool.shape, pool.stride(), torch.float32, *seen, rows.shape, rows.stride())
+
+    assert plan(torch.zeros(*seen, 2, 64))[2] == 0
+    with pytest.raises(ValueError, match=r"rows\[0\] must have"):
+        plan(torch.zeros(*made, 2, 64).expand(*seen, 2, 64))
+
+
+def test_rows_closer_than_their_heads_are_refused():
+    base = torch.zeros(4096)
+    with pytest.raises(ValueError, match="q must have"):
+        x = base.as_strided((2, 3, 2, 64), (3 * 64, 64, 64, 1))
+        rounds._row_stride(x.shape, x.stride(), "q")
+    # dimensions of one say nothing, whatever their strides
+    for shape, strides in (((1, 1, 2, 64), (0, 0, 64, 1)), ((1, 3, 2, 64), (0, 128, 64, 1)), ((3, 1, 1, 64), (64, 0, 0, 1))):
+        x = base.as_strided(shape, strides)
+        assert rounds._row_stride(x.shape, x.stride(), "q") == 0
