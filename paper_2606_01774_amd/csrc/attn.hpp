@@ -292,8 +292,15 @@ template <typename T, int D, int MT, bool SPLITP> struct Wave {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const float x = p[mt][e >> 2][e & 3];
-                    hi[mt][e] = (__bf16)x;
-                    if (SPLITP) lo[mt][e] = (__bf16)(x - (float)hi[mt][e]);
+                    if (SPLITP) {
+                        // The first part is cut off, not rounded, and the second is more than zero by
+                        // the 2^-23 of x: of one sign, they take an infinite value over as it is.
+                        const uint32_t top = __float_as_uint(x) & 0xffff0000u;
+                        hi[mt][e] = __builtin_bit_cast(__bf16, (unsigned short)(top >> 16));
+                        lo[mt][e] = (__bf16)__builtin_fmaf(x, 0x1.000002p0f, -__uint_as_float(top));
+                    } else {
+                        hi[mt][e] = (__bf16)x;
+                    }
                 }
             }
 #pragma unroll

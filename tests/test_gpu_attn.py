@@ -364,3 +364,22 @@ def test_expanded_inputs_are_refused():
         kept, c[name] = c[name], x[name].contiguous()
         _compare(c, bd.bdgdn_tree_attn(c["q"], c["k"], c["v"], *args, want_lse=True), "full", 1 / math.sqrt(128), "bf16", "bf16")
         c[name] = kept
+
+
+@pytest.mark.parametrize("dtype,out", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "f32")])
+@pytest.mark.parametrize("N,page", [(3, 32), (40, 32), (3, 20), (40, 20)])
+def test_infinite_cached_values(dtype, out, N, page):
+    """A weight above zero takes an infinity over as it is; infinities of both signs, and a NaN, give NaN.  The
+    first key has the largest score of all rows, so that weights of exactly one are among them."""
+    c = _case(1, N, 2, 1, 128, page, [75], dtype, seed=2, std=0.3)
+    c["q"][...] = c["q"].abs() + 0.5
+    at = [(int(c["table"][0, t // page]), t % page) for t in range(75)]
+    c["kp"][at[0]] = 1.0
+    for t, x, value in ((0, 5, "inf"), (31, 6, "-inf"), (70, 7, "inf"), (3, 8, "inf"), (9, 8, "-inf"), (44, 9, "nan")):
+        c["vp"][at[t]][0, x] = float(value)
+    o, lse = bd.bdgdn_tree_attn(c["q"], c["k"], c["v"], c["kp"], c["vp"], c["table"], c["seq"], out_dtype=DT[out],
+                                want_lse=True)
+    inf = float("inf")
+    assert (o[..., 5] == inf).all() and (o[..., 6] == -inf).all() and (o[..., 7] == inf).all()
+    assert torch.isnan(o[..., 8:10]).all() and torch.isfinite(lse).all()
+    assert torch.isfinite(o[..., :5]).all() and torch.isfinite(o[..., 10:]).all()
