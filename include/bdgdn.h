@@ -563,9 +563,9 @@ size_t bdgdn_tree_attn_workspace(const bdgdn_attn_desc_t *desc, const bdgdn_cach
  *   lse             [R][N][h_q] fp32, or NULL
  *   workspace       256-byte aligned, owned by the call until the stream passes it
  * Scores, the softmax's statistics and all sums are fp32.  With bf16 inputs the products are
- * exact in fp32 and the weights exp(s - m) are rounded to bf16 for the product with v, in two
- * bf16 parts (16 significant bits) where the output is fp32; their sum, and lse with it, is
- * that of the unrounded ones.  Results are deterministic.  (dtype, out_dtype) as for the other entry
+ * exact in fp32 and the weights exp(s - m) enter the product with v in two bf16 parts (16
+ * significant bits); their sum, and lse with it, is that of the unrounded ones.  Results are
+ * deterministic.  (dtype, out_dtype) as for the other entry
  * points: (bf16, bf16), (bf16, fp32), (fp32, fp32).
  */
 int bdgdn_tree_attn(const bdgdn_attn_desc_t *desc, const bdgdn_cache_desc_t *cache, const void *q,

@@ -181,7 +181,7 @@ __device__ __forceinline__ void note_request(const AttnArgs &a, const Range &g)
 }
 
 // One step of 32 keys for MT groups of 16 rows.
-template <typename T, int D, int MT, bool SPLITP> struct Wave {
+template <typename T, int D, int MT> struct Wave {
     typedef Geo<T, D> G;
     u32x4 q[MT][G::NK];
     f32x4 o[MT][G::NT];
@@ -280,9 +280,12 @@ template <typename T, int D, int MT, bool SPLITP> struct Wave {
     }
 
     // o += V^T P^T; v[e] is the lane's part of value row
-    // 16 (e / 4) + 4 g + e % 4.  With bf16 inputs the weights are rounded to bf16, which the matrix
-    // units take: to one part where the output is rounded as much, to two (16 bits) where it is
-    // fp32.  Their sum is of the unrounded ones.
+    // 16 (e / 4) + 4 g + e % 4.  With bf16 inputs the weights go to the matrix units in two bf16 parts
+    // (16 bits), so that a bf16 result is an fp32 one rounded: with one part it is off by
+    // 2.2e-3 in the mean square, with two by its own 1.65e-3.  Where memory bounds a call that costs
+    // 0.5 to 6 % (64 requests of up to 4096 tokens, 32 heads on 8 of 128, 8 nodes: 126.8 for 126.1 us),
+    // where the products do 8 to 17 (32 nodes 171 for 158, 64 nodes 285 for 243, trees of 24 over
+    // 128k 221 for 191).  Their sum is of the whole ones.
     __device__ __forceinline__ void values(const f32x4 (&p)[MT][2], const u32x4 (&v)[8][G::NV])
     {
         if constexpr (sizeof(T) == 2) {
@@ -292,15 +295,11 @@ template <typename T, int D, int MT, bool SPLITP> struct Wave {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const float x = p[mt][e >> 2][e & 3];
-                    if (SPLITP) {
-                        // The first part is cut off, not rounded, and the second is more than zero by
-                        // the 2^-23 of x: of one sign, they take an infinite value over as it is.
-                        const uint32_t top = __float_as_uint(x) & 0xffff0000u;
-                        hi[mt][e] = __builtin_bit_cast(__bf16, (unsigned short)(top >> 16));
-                        lo[mt][e] = (__bf16)__builtin_fmaf(x, 0x1.000002p0f, -__uint_as_float(top));
-                    } else {
-                        hi[mt][e] = (__bf16)x;
-                    }
+                    // The first part is cut off, not rounded, and the second is more than zero by
+                    // the 2^-23 of x: of one sign, they take an infinite value over as it is.
+                    const uint32_t top = __float_as_uint(x) & 0xffff0000u;
+                    hi[mt][e] = __builtin_bit_cast(__bf16, (unsigned short)(top >> 16));
+                    lo[mt][e] = (__bf16)__builtin_fmaf(x, 0x1.000002p0f, -__uint_as_float(top));
                 }
             }
 #pragma unroll
@@ -315,15 +314,13 @@ template <typename T, int D, int MT, bool SPLITP> struct Wave {
                     }
                     const bf16x8 a0 = __builtin_bit_cast(bf16x8, even), a1 = __builtin_bit_cast(bf16x8, odd);
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt) {
-                        f32x4 &o0 = o[mt][j * G::EV + 2 * w], &o1 = o[mt][j * G::EV + 2 * w + 1];
-                        o0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a0, hi[mt], o0, 0, 0, 0);
-                        o1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a1, hi[mt], o1, 0, 0, 0);
-                        if (SPLITP) {
-                            o0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a0, lo[mt], o0, 0, 0, 0);
-                            o1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a1, lo[mt], o1, 0, 0, 0);
+                    for (int part = 0; part < 2; ++part)
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt) {
+                            f32x4 &o0 = o[mt][j * G::EV + 2 * w], &o1 = o[mt][j * G::EV + 2 * w + 1];
+                            o0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a0, part ? lo[mt] : hi[mt], o0, 0, 0, 0);
+                            o1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a1, part ? lo[mt] : hi[mt], o1, 0, 0, 0);
                         }
-                    }
                 }
         } else {
 #pragma unroll
@@ -453,8 +450,8 @@ __device__ __forceinline__ uint32_t finite_part(uint32_t x, bool wide)
 }
 
 // The queries of a wave's 16 MT rows from row0 on, and the nodes that they belong to.
-template <typename T, int D, int MT, bool SPLITP>
-__device__ __forceinline__ void load_rows(Wave<T, D, MT, SPLITP> &w, const AttnArgs &a, int r, int kvh, int row0, int (&node)[MT],
+template <typename T, int D, int MT>
+__device__ __forceinline__ void load_rows(Wave<T, D, MT> &w, const AttnArgs &a, int r, int kvh, int row0, int (&node)[MT],
                                           int g, int rr)
 {
     typedef Geo<T, D> G;
@@ -467,7 +464,7 @@ __device__ __forceinline__ void load_rows(Wave<T, D, MT, SPLITP> &w, const AttnA
     }
 }
 
-template <typename T, int D, int MT, bool SPLITP> __device__ __forceinline__ void sign_rows(Wave<T, D, MT, SPLITP> &w, const AttnArgs &a)
+template <typename T, int D, int MT> __device__ __forceinline__ void sign_rows(Wave<T, D, MT> &w, const AttnArgs &a)
 {
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
@@ -478,8 +475,8 @@ template <typename T, int D, int MT, bool SPLITP> __device__ __forceinline__ voi
 }
 
 // The nodes themselves as keys and values, for the rows of one wave.
-template <typename T, int D, int MT, bool SPLITP>
-__device__ __forceinline__ void attend_nodes(Wave<T, D, MT, SPLITP> &w, const AttnArgs &a, int r, int kvh, int count,
+template <typename T, int D, int MT>
+__device__ __forceinline__ void attend_nodes(Wave<T, D, MT> &w, const AttnArgs &a, int r, int kvh, int count,
                                              const int (&node)[MT], int g, int rr)
 {
     typedef Geo<T, D> G;
@@ -561,8 +558,8 @@ __device__ __forceinline__ void attend_nodes(Wave<T, D, MT, SPLITP> &w, const At
 
 // Waves with the same rows (RW apart, KW of them) joined two by two; the first of them holds
 // the result.  s_o and s_ml have room for KW / 2 * RW waves.
-template <typename T, int D, int MT, bool SPLITP>
-__device__ __forceinline__ void join_waves(Wave<T, D, MT, SPLITP> &w, f32x4 (*s_o)[Geo<T, D>::NT][64], float (*s_ml)[2][64],
+template <typename T, int D, int MT>
+__device__ __forceinline__ void join_waves(Wave<T, D, MT> &w, f32x4 (*s_o)[Geo<T, D>::NT][64], float (*s_ml)[2][64],
                                            int kw, int rw, int KW, int RW, int lane)
 {
     typedef Geo<T, D> G;
@@ -591,8 +588,8 @@ __device__ __forceinline__ void join_waves(Wave<T, D, MT, SPLITP> &w, f32x4 (*s_
 }
 
 // The rows of one wave: the result where the request is one piece, else the piece's part.
-template <typename Out, typename T, int D, int MT, bool SPLITP>
-__device__ __forceinline__ void write_rows(const Wave<T, D, MT, SPLITP> &w, const AttnArgs &a, const Piece &it, int kvh,
+template <typename Out, typename T, int D, int MT>
+__device__ __forceinline__ void write_rows(const Wave<T, D, MT> &w, const AttnArgs &a, const Piece &it, int kvh,
                                            int count, int row0, const int (&node)[MT], int g, int rr)
 {
     typedef Geo<T, D> G;

@@ -22,7 +22,7 @@ constexpr int kWaves = 4;          // of a workgroup
 // Waves of a SIMD that a kernel's registers allow (two of up to 256, one of more).
 constexpr int waves_per_simd(bool bf16, int d) { return d == 64 || (bf16 && d == 128) ? 2 : 1; }
 
-template <typename T, int D, int MT, bool SPLITP, bool HALVES, typename Out>
+template <typename T, int D, int MT, bool HALVES, typename Out>
 __global__ void __launch_bounds__(64 * kWaves, waves_per_simd(sizeof(T) == 2, D)) bdgdn_tree_attn_kernel(AttnArgs a)
 {
     typedef Geo<T, D> G;
@@ -35,7 +35,7 @@ __global__ void __launch_bounds__(64 * kWaves, waves_per_simd(sizeof(T) == 2, D)
     const int unit = y / a.RG * 8 + x, rg = y % a.RG;
     const int range = unit / a.h_kv, kvh = unit - range * a.h_kv;
     Range span = find_range(a, range, threadIdx.x & 63);
-    Wave<T, D, MT, SPLITP> w;
+    Wave<T, D, MT> w;
     const int row0 = (rg * a.RW + rw) * 16 * MT;   // of this wave's rows
     for (; span.pos < span.end; next_piece(a, span)) {
         const int lane = lane_anew(), g = lane >> 4, rr = lane & 15;
@@ -202,11 +202,10 @@ constexpr int most_mt(int d) { return d == 256 ? 1 : 2; }
 
 template <typename T, int D, int MT, bool F32OUT> hipError_t launch_m(const AttnPlan &p, const AttnArgs &a, hipStream_t s)
 {
-    constexpr bool SP = sizeof(T) == 2 && F32OUT;
     typedef typename std::conditional<F32OUT, float, __bf16>::type Out;
     constexpr bool HALVES = sizeof(T) == 4;   // (bf16 over such pages is the staged kernel's)
-    if (HALVES && a.page % 16 == 0) bdgdn_tree_attn_kernel<T, D, MT, SP, HALVES, Out><<<p.grid, 64 * kWaves, 0, s>>>(a);
-    else bdgdn_tree_attn_kernel<T, D, MT, SP, false, Out><<<p.grid, 64 * kWaves, 0, s>>>(a);
+    if (HALVES && a.page % 16 == 0) bdgdn_tree_attn_kernel<T, D, MT, HALVES, Out><<<p.grid, 64 * kWaves, 0, s>>>(a);
+    else bdgdn_tree_attn_kernel<T, D, MT, false, Out><<<p.grid, 64 * kWaves, 0, s>>>(a);
     return hipGetLastError();
 }
 

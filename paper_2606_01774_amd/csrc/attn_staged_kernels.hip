@@ -49,7 +49,7 @@ template <int N> __device__ __forceinline__ void wait_loads_barrier()
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-template <int D, int RW, bool HALVES, bool SPLITP, typename Out>
+template <int D, int RW, bool HALVES, typename Out>
 __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) bdgdn_tree_attn_staged_kernel(AttnArgs a)
 {
     typedef __bf16 T;
@@ -65,7 +65,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) bdgdn_tree_attn_staged_
     const int unit = y / a.RG * 8 + x, rg = y % a.RG;
     const int range = unit / a.h_kv, kvh = unit - range * a.h_kv;
     Range span = find_range(a, range, threadIdx.x & 63);
-    Wave<T, D, 2, SPLITP> w;
+    Wave<T, D, 2> w;
     const int row0 = (rg * RW + rw) * 32;   // of this wave's rows
     const bool idle = row0 >= a.N * a.G;    // it has none, and only loads
 
@@ -220,12 +220,12 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) bdgdn_tree_attn_staged_
     }
 }
 
-template <int D, int RW, bool HALVES, bool SPLITP, typename Out> hipError_t launch(int grid, const AttnArgs &a, hipStream_t s)
+template <int D, int RW, bool HALVES, typename Out> hipError_t launch(int grid, const AttnArgs &a, hipStream_t s)
 {
     typedef Staged<D, RW> X;
     static std::once_flag once;
     static hipError_t err;
-    const auto kernel = bdgdn_tree_attn_staged_kernel<D, RW, HALVES, SPLITP, Out>;
+    const auto kernel = bdgdn_tree_attn_staged_kernel<D, RW, HALVES, Out>;
     std::call_once(once, [&] {
         err = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, X::LDS);
     });
@@ -234,17 +234,17 @@ template <int D, int RW, bool HALVES, bool SPLITP, typename Out> hipError_t laun
     return hipGetLastError();
 }
 
-template <int D, bool SPLITP, typename Out> hipError_t launch_rw(int grid, const AttnArgs &a, hipStream_t s)
+template <int D, typename Out> hipError_t launch_rw(int grid, const AttnArgs &a, hipStream_t s)
 {
-    if (a.page % 16 == 0) return a.RW == 2 ? launch<D, 2, true, SPLITP, Out>(grid, a, s) : launch<D, 4, true, SPLITP, Out>(grid, a, s);
-    return a.RW == 2 ? launch<D, 2, false, SPLITP, Out>(grid, a, s) : launch<D, 4, false, SPLITP, Out>(grid, a, s);
+    if (a.page % 16 == 0) return a.RW == 2 ? launch<D, 2, true, Out>(grid, a, s) : launch<D, 4, true, Out>(grid, a, s);
+    return a.RW == 2 ? launch<D, 2, false, Out>(grid, a, s) : launch<D, 4, false, Out>(grid, a, s);
 }
 
 }  // namespace
 
 hipError_t launch_tree_attn_staged(bool f32_out, int d, int grid, const AttnArgs &a, hipStream_t s)
 {
-#define BDGDN_STAGED(D) (f32_out ? launch_rw<D, true, float>(grid, a, s) : launch_rw<D, false, __bf16>(grid, a, s))
+#define BDGDN_STAGED(D) (f32_out ? launch_rw<D, float>(grid, a, s) : launch_rw<D, __bf16>(grid, a, s))
     return d == 64 ? BDGDN_STAGED(64) : d == 128 ? BDGDN_STAGED(128) : BDGDN_STAGED(256);
 #undef BDGDN_STAGED
 }

@@ -383,3 +383,24 @@ def test_infinite_cached_values(dtype, out, N, page):
     assert (o[..., 5] == inf).all() and (o[..., 6] == -inf).all() and (o[..., 7] == inf).all()
     assert torch.isnan(o[..., 8:10]).all() and torch.isfinite(lse).all()
     assert torch.isfinite(o[..., :5]).all() and torch.isfinite(o[..., 10:]).all()
+
+
+@pytest.mark.parametrize("R,N,h_q,h_kv,d,page,lens,mask", [
+    (1, 1, 4, 1, 128, 64, [300], "full"),
+    (2, 8, 8, 2, 128, 16, [129, 1000], "causal"),
+    (2, 32, 8, 2, 128, 64, [2049, 95], "full"),
+    (2, 30, 8, 2, 64, 16, [700, 0], "causal"),
+    (1, 9, 4, 1, 256, 32, [650], "full"),
+    (2, 30, 8, 2, 256, 64, [129, 512], "causal"),
+    (2, 3, 4, 2, 128, 24, [500, 33], "full"),
+    (2, 40, 8, 2, 128, 24, [700, 77], "causal"),
+])
+def test_bf16_results_are_off_by_their_own_rounding(R, N, h_q, h_kv, d, page, lens, mask):
+    """A bf16 output is an fp32 one rounded: 2^-8 |o| on top of the fp32 output's tolerance (above), which the
+    rounding of the weights, in two parts, enters with 2^-16 A alone."""
+    c = _case(R, N, h_q, h_kv, d, page, lens, "bf16", seed=R + N + d)
+    o, _ = bd.bdgdn_tree_attn(c["q"], c["k"], c["v"], c["kp"], c["vp"], c["table"], c["seq"], mask=mask)
+    ro, _, A, S = _reference(c, mask, 1 / math.sqrt(d))
+    tol = ((4 * (d + 8) * S + max(lens) + N + 64) * 2.0 ** -24 + 2.0 ** -16)[..., None] * A
+    err = (o.double() - ro).abs()
+    assert (err <= 2.0 ** -8 * (ro.abs() + tol) + tol).all(), float((err / (2.0 ** -8 * ro.abs() + tol)).max())
