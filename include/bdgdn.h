@@ -671,7 +671,8 @@ size_t bdgdn_cache_workspace(const bdgdn_cache_desc_t *cache, int32_t num_req, i
  * Appends rows to the sequences in slot[0 .. R-1]: rows path[r][0 .. count[r]-1] of request r
  * (rows 0 .. count[r]-1 where path is NULL) go behind its last token, in every pool.  A last
  * page that is not full and is shared with another sequence when the call begins is replaced
- * by a page of its own with a copy of its tokens (copy on write).
+ * by a page of its own with a copy of its tokens (copy on write); one that is not there (its table
+ * entry was dropped), by a page with rows of zeros for them.
  *   pools        host array of n_pools device pointers (keys and values of every layer), each
  *                with the geometry of `cache`, 16-byte aligned
  *   rows         host array of n_pools device pointers: [R][N][h_kv][d] of the pools' dtype
@@ -699,7 +700,8 @@ int bdgdn_cache_fork(const bdgdn_cache_desc_t *cache, const bdgdn_cache_tables_t
  * Keeps the positions keep[r][0 .. count[r]-1] (rising, each below the sequence's length) of
  * slot[r] and drops the others: token j of the sequence is now what token keep[r][j] was, in
  * every pool.  Leading pages whose tokens all stay where they are are kept (also shared ones);
- * the tokens behind them move to new pages, and the old ones are given back.  keep is [R][M]
+ * the tokens behind them move to new pages (as rows of zeros where their page is not there), and
+ * the old ones are given back.  keep is [R][M]
  * int32, count [R] int32 (values outside 0 .. M are clamped); pools, status and workspace
  * (bdgdn_cache_workspace(cache, R, M)) as for bdgdn_cache_append.
  */

@@ -78,7 +78,7 @@ template <bool APPEND> __device__ int plan_request(const CacheArgs &a, int f)
                     const bool there = (unsigned)last < (unsigned)a.n_pages;
                     if (!there || a.ref[last] > 1) {
                         --start;
-                        cow = there ? last : -2;   // -2: a new page with nothing to copy
+                        cow = there ? last : -2;   // -2: a new page for one that is not there
                     }
                 }
                 need = pages_of(old + n, a.page) - start;
@@ -271,9 +271,10 @@ template <bool APPEND, int POOLS> __global__ void __launch_bounds__(256) bdgdn_c
     if (n <= 0) return;
     const int slot = c.slot[f], old = m[kOld];
     const int32_t *row = !APPEND && c.saved ? c.saved + (long)f * c.max_pages : c.table + (long)slot * c.max_pages;
-    // append: tokens from `first` on, of which the first `copied` come from a shared page;
+    // append: tokens from `first` on, of which the first `copied` come from a shared page or, where
+    // there is none, are zeros (the new page may hold another sequence's rows);
     // compact: tokens from `first` on come from the positions kept
-    const int copied = APPEND && m[kCow] >= 0 ? old % c.page : 0;
+    const int copied = APPEND && m[kCow] != -1 ? old % c.page : 0;
     const int first = APPEND ? old - copied : min(m[kStart] * c.page, n);
     const int rows = APPEND ? n + copied : n - first;
     unsigned char *pool = a.pool[blockIdx.z];
@@ -288,7 +289,8 @@ template <bool APPEND, int POOLS> __global__ void __launch_bounds__(256) bdgdn_c
         if (APPEND) {
             to = row[t / c.page];
             if (j < copied) {
-                val = *reinterpret_cast<const u32x4v *>(pool + m[kCow] * a.page_stride + j * a.token_stride + head);
+                if (m[kCow] >= 0)
+                    val = *reinterpret_cast<const u32x4v *>(pool + m[kCow] * a.page_stride + j * a.token_stride + head);
             } else {
                 const int i = j - copied;
                 const int node = c.path ? c.path[(long)f * c.rows_max + i] : i;

@@ -388,3 +388,22 @@ def test_expanded_rows_are_refused():
     bd.bdgdn_cache_append(c.tables, c.pools, [row.expand(3, 1, 1, 64).contiguous()], _ints([0, 1, 2]), _ints([1, 1, 1]))
     for page in c.tables.page_table[:, 0].tolist():
         assert torch.equal(c.pools[0][page, 0], row[0, 0])
+
+
+@pytest.mark.parametrize("page,old,htd,pools", [(4, 6, False, 1), (16, 47, True, 2), (64, 1, False, 17)])
+def test_a_replaced_page_holds_nothing_of_its_last_owner(page, old, htd, pools):
+    """The new page in place of a missing one: the tokens before the appended ones, which now have a page
+    again, are rows of zeros, not what the page held before."""
+    c = Cache(2, 8, 12, page, 2, 64, torch.bfloat16, pools, htd)
+    ids, rows = c.rows(1, old)
+    assert bd.bdgdn_cache_append(c.tables, c.pools, rows, _ints([0]), _ints([old])).tolist() == [0]
+    last = (old - 1) // page
+    c.tables.page_table[0, last] = 12 if pools == 2 else -1
+    ids, rows = c.rows(1, page + 1)
+    path = None if pools == 1 else _ints([list(range(page + 1))])
+    assert bd.bdgdn_cache_append(c.tables, c.pools, rows, _ints([0]), _ints([page + 1]), path=path).tolist() == [0]
+    cols, n = c.tables.page_table[0].tolist(), old + page + 1
+    assert 0 <= cols[last] < 12 and c.tables.seq_len.tolist() == [n, 0]
+    for pool, new in zip(c.pools, rows):
+        got = torch.stack([pool[cols[t // page], t % page] for t in range(last * page, n)])
+        assert not got[:old - last * page].any() and torch.equal(got[old - last * page:], new[0])
