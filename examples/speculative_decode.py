@@ -69,7 +69,7 @@ class Decoder:
                        for x in layers]
         max_pages = -(-max_len // page)
         self.page, n_pages = page, slots * max_pages if pages is None else pages
-        self.tables = bd.make_cache_tables(slots, max_pages, n_pages, device=device)
+        self.tables = bd.make_cache_tables(slots, max_pages, n_pages, device=device, page=page)
         self.pools = [torch.zeros(n_pages, page, KV_HEADS, DIM, dtype=torch.bfloat16, device=device)
                       for _ in range(2 * layers.count("a"))]   # keys, values of each "a"
 
@@ -128,7 +128,7 @@ class Decoder:
         for s in self.states:
             if s is not None:
                 s[dst.long()] = s[src.long()]
-        return bd.bdgdn_cache_fork(self.tables, src, dst, page=self.page)
+        return bd.bdgdn_cache_fork(self.tables, src, dst)
 
     def _draft(self, logits, temperature):
         if temperature <= 0:
@@ -184,7 +184,7 @@ class Decoder:
         return bd.bdgdn_cache_compact(self.tables, self.pools, slot, keep.contiguous(), count)
 
     def finish(self, slot):
-        bd.bdgdn_cache_truncate(self.tables, slot, page=self.page)
+        bd.bdgdn_cache_truncate(self.tables, slot)
 
 
 def main():

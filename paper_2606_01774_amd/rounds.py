@@ -50,17 +50,33 @@ class _Tables(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("page_table", "seq_len", "refcount", "free_bits")]
 
 
-class CacheTables(NamedTuple):
-    """The tables of a cache on the device, all int32: page_table [n_slots, max_pages], seq_len
-    [n_slots], refcount [n_pages], free_bits [(n_pages + 31) // 32]."""
+class _CacheTables(NamedTuple):
     page_table: torch.Tensor
     seq_len: torch.Tensor
     refcount: torch.Tensor
     free_bits: torch.Tensor
 
 
-def make_cache_tables(n_slots, max_pages, n_pages, device="cuda") -> CacheTables:
-    """The tables of an empty cache."""
+class CacheTables(_CacheTables):
+    """The tables of a cache on the device, all int32: page_table [n_slots, max_pages], seq_len
+    [n_slots], refcount [n_pages], free_bits [(n_pages + 31) // 32].  Beside these four it may know
+    the tokens of a page (``page``, else None); calls with another page are then refused."""
+    page = None
+
+    def __new__(cls, page_table, seq_len, refcount, free_bits, page=None):
+        if page is not None and int(page) < 1:
+            raise ValueError(f"page must be a number of tokens, got {page}")
+        self = super().__new__(cls, page_table, seq_len, refcount, free_bits)
+        self.page = None if page is None else int(page)
+        return self
+
+    def _replace(self, **kw):
+        page = kw.pop("page", self.page)
+        return CacheTables(*super()._replace(**kw), page=page)
+
+
+def make_cache_tables(n_slots, max_pages, n_pages, device="cuda", page=None) -> CacheTables:
+    """The tables of an empty cache; page is what the calls hold its pools' pages to."""
     bits = [-1] * (n_pages // 32)
     if n_pages % 32:
         last = (1 << n_pages % 32) - 1
@@ -68,7 +84,19 @@ def make_cache_tables(n_slots, max_pages, n_pages, device="cuda") -> CacheTables
     return CacheTables(torch.full((n_slots, max_pages), -1, dtype=_I32, device=device),
                        torch.zeros(n_slots, dtype=_I32, device=device),
                        torch.zeros(n_pages, dtype=_I32, device=device),
-                       torch.tensor(bits, dtype=_I32).to(device))
+                       torch.tensor(bits, dtype=_I32).to(device), page)
+
+
+def _page_of(tables, page):
+    """Tokens of a page, from what the caller or the pools say (or None) and what the tables know."""
+    known = getattr(tables, "page", None)
+    if page is None:
+        if known is None:
+            raise ValueError("page must be given for tables that do not know it")
+        return known
+    if known is not None and page != known:
+        raise ValueError(f"these are tables of pages of {known} tokens, not of {page}")
+    return int(page)
 
 
 def bind(lib):
@@ -356,6 +384,7 @@ def bdgdn_cache_append(tables, pools, rows, slot, count, *, path=None, status=No
     R, N = r0.shape[:2]
     desc, need, stride = _pools_plan(tables[0].shape, tables[2].numel(), p0.shape, p0.stride(), p0.dtype, R, N, r0.shape,
                                      r0.stride())
+    _page_of(tables, p0.shape[1])
     device = p0.device
     if status is None:
         status = _empty(R, _I32, device, stream)
@@ -367,13 +396,15 @@ def bdgdn_cache_append(tables, pools, rows, slot, count, *, path=None, status=No
     return status
 
 
-def bdgdn_cache_fork(tables, src, dst, *, page, status=None, stream=None):
-    """Slots dst[i] (empty) share the sequences of src[i].  Returns status."""
+def bdgdn_cache_fork(tables, src, dst, *, page=None, status=None, stream=None):
+    """Slots dst[i] (empty) share the sequences of src[i].  page: tokens of a page, for tables that do
+    not know it.  Returns status."""
     lib = load_library()
+    page = _page_of(tables, page)
     n = src.numel()
     if status is None:
         status = _empty(n, _I32, src.device, stream)
-    st = lib.bdgdn_cache_fork(_table_desc(*tables.page_table.shape, tables.refcount.numel(), int(page)), _tables(tables), n,
+    st = lib.bdgdn_cache_fork(_table_desc(*tables.page_table.shape, tables.refcount.numel(), page), _tables(tables), n,
                               _p(src, "src", _I32), _vector(dst, "dst", n), _vector(status, "status", n), _stream(stream))
     _check(st, "bdgdn_cache_fork")
     return status
@@ -390,6 +421,7 @@ def bdgdn_cache_compact(tables, pools, slot, keep, count, *, status=None, worksp
         raise ValueError("keep must be [R, M]")
     R, M = keep.shape
     desc, need, _ = _pools_plan(tables[0].shape, tables[2].numel(), p0.shape, p0.stride(), p0.dtype, R, M, None, None)
+    _page_of(tables, p0.shape[1])
     if status is None:
         status = _empty(R, _I32, p0.device, stream)
     workspace, size = _scratch(workspace, need, p0.device, stream)
@@ -400,10 +432,12 @@ def bdgdn_cache_compact(tables, pools, slot, keep, count, *, status=None, worksp
     return status
 
 
-def bdgdn_cache_truncate(tables, slot, length=None, *, page, stream=None):
-    """Shortens the sequences in slot[r] to length[r] tokens (None: frees the slots)."""
+def bdgdn_cache_truncate(tables, slot, length=None, *, page=None, stream=None):
+    """Shortens the sequences in slot[r] to length[r] tokens (None: frees the slots).  page as for
+    bdgdn_cache_fork."""
     lib = load_library()
+    page = _page_of(tables, page)
     n = slot.numel()
-    st = lib.bdgdn_cache_truncate(_table_desc(*tables.page_table.shape, tables.refcount.numel(), int(page)), _tables(tables),
+    st = lib.bdgdn_cache_truncate(_table_desc(*tables.page_table.shape, tables.refcount.numel(), page), _tables(tables),
                                   n, _p(slot, "slot", _I32), _vector(length, "length", n), _stream(stream))
     _check(st, "bdgdn_cache_truncate")

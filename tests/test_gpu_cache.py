@@ -407,3 +407,18 @@ def test_a_replaced_page_holds_nothing_of_its_last_owner(page, old, htd, pools):
     for pool, new in zip(c.pools, rows):
         got = torch.stack([pool[cols[t // page], t % page] for t in range(last * page, n)])
         assert not got[:old - last * page].any() and torch.equal(got[old - last * page:], new[0])
+
+
+def test_pools_of_another_page_are_refused():
+    t = bd.make_cache_tables(2, 4, 8, page=16)
+    rows, one = [torch.zeros(1, 2, 1, 64, device="cuda")], _ints([0])
+    other = [torch.zeros(8, 8, 1, 64, device="cuda")]
+    with pytest.raises(ValueError, match="pages of 16"):
+        bd.bdgdn_cache_append(t, other, rows, one, _ints([2]))
+    with pytest.raises(ValueError, match="pages of 16"):
+        bd.bdgdn_cache_compact(t, other, one, _ints([[0]]), _ints([1]))
+    pools = [torch.zeros(8, 16, 1, 64, device="cuda")]
+    assert bd.bdgdn_cache_append(t, pools, rows, one, _ints([2])).tolist() == [0]
+    assert bd.bdgdn_cache_fork(t, one, _ints([1])).tolist() == [0] and t.refcount.tolist()[:2] == [2, 0]
+    bd.bdgdn_cache_truncate(t, _ints([0, 1]))
+    assert not t.refcount.any() and not t.seq_len.any()

@@ -1,5 +1,6 @@
 """Host-side validation of the entry points that serve the softmax half of a round (no GPU is
 touched: every call here fails validation, or has no requests)."""
+import copy
 import ctypes
 
 import pytest
@@ -234,3 +235,24 @@ def test_rows_closer_than_their_heads_are_refused():
     for shape, strides in (((1, 1, 2, 64), (0, 0, 64, 1)), ((1, 3, 2, 64), (0, 128, 64, 1)), ((3, 1, 1, 64), (64, 0, 0, 1))):
         x = base.as_strided(shape, strides)
         assert rounds._row_stride(x.shape, x.stride(), "q") == 0
+
+
+def test_tables_that_know_their_page_refuse_another():
+    """The tables say nothing of their page by themselves, and a call with another one would give back pages that are in use."""
+    t = bd.make_cache_tables(2, 3, 40, device="cpu", page=16)
+    assert t.page == 16 and len(t) == 4 and copy.copy(t).page == 16 and t._replace(seq_len=t.seq_len).page == 16
+    slot = torch.zeros(1, dtype=torch.int32)
+    with pytest.raises(ValueError, match="pages of 16"):
+        bd.bdgdn_cache_fork(t, slot, slot, page=8)
+    with pytest.raises(ValueError, match="pages of 16"):
+        bd.bdgdn_cache_truncate(t, slot, page=64)
+    with pytest.raises(ValueError, match="pages of 16"):
+        rounds._page_of(t, 24)
+    assert rounds._page_of(t, None) == rounds._page_of(t, 16) == 16
+    unknown = bd.CacheTables(*t)
+    assert unknown.page is None and rounds._page_of(unknown, 24) == 24 and rounds._page_of(tuple(t), 24) == 24
+    for call in (lambda: bd.bdgdn_cache_fork(unknown, slot, slot), lambda: bd.bdgdn_cache_truncate(unknown, slot)):
+        with pytest.raises(ValueError, match="page must be given"):
+            call()
+    with pytest.raises(ValueError, match="page must be"):
+        bd.make_cache_tables(2, 3, 40, device="cpu", page=0)
