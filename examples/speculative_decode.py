@@ -187,13 +187,20 @@ class Decoder:
         bd.bdgdn_cache_truncate(self.tables, slot)
 
 
+def positive(text):
+    n = int(text)
+    if n < 1:
+        raise argparse.ArgumentTypeError(f"{n} is not above zero")
+    return n
+
+
 def main():
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     ap.add_argument("--layers", default="gaga", help='of "g" (Gated DeltaNet) and "a" (attention)')
-    ap.add_argument("--prompts", type=int, default=8)
-    ap.add_argument("--ways", type=int, default=4, help="continuations of each prompt")
-    ap.add_argument("--length", type=int, default=100, help="of a prompt")
-    ap.add_argument("--rounds", type=int, default=64)
+    ap.add_argument("--prompts", type=positive, default=8)
+    ap.add_argument("--ways", type=positive, default=4, help="continuations of each prompt")
+    ap.add_argument("--length", type=positive, default=100, help="of a prompt")
+    ap.add_argument("--rounds", type=positive, default=64)
     ap.add_argument("--drafts", type=int, default=7)
     ap.add_argument("--tree", help="children of a node at each depth, as 3,2,1: draft trees")
     ap.add_argument("--temperature", type=float, default=1.0)
@@ -216,8 +223,9 @@ def main():
     anchor = anchor.repeat(ways)
     start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
     emitted = torch.zeros((), dtype=torch.int64, device=model.device)
+    start.record()
     for i in range(args.rounds):
-        if i == 1:
+        if i == 1:   # (the first of several rounds loads kernels and fills allocators)
             start.record()
         if i and i % every == 0 and model.pools:
             bad = torch.maximum(bad, model.shorten(slot, 4, args.window - 4).max())

@@ -220,3 +220,11 @@ def test_temporaries_belong_to_the_stream_of_the_call(which):
     torch.cuda.synchronize()
     assert all(bool((x == 7).all()) for x in taken), name
     assert all(torch.equal(g, w) for g, w in zip(got, want)), name
+
+
+@pytest.mark.parametrize("argv", [["--prompts", "2", "--ways", "2", "--rounds", "1"],
+                                  ["--layers", "aa", "--tree", "2,2", "--rounds", "1", "--prompts", "1", "--ways", "1"]])
+def test_the_command_for_one_round(argv, monkeypatch, capsys):
+    monkeypatch.setattr("sys.argv", ["speculative_decode.py", *argv])
+    sd.main()
+    assert "tokens a sequence and round" in capsys.readouterr().out
