@@ -1,8 +1,8 @@
 // attn_kernels.hip -- attention of a block of nodes over a paged cache and over the nodes
 // themselves: the kernel for fp32, and for few rows over pages of any size, the joining kernel,
 // tree masks, dispatch.  (bf16 over pages of whole runs of 16 tokens takes the kernel of
-// attn_staged_kernels.hip, which is never slower: one node on 64 requests of up to 4096 tokens
-// 112 against 114 us, four 119 against 122, eight 128 against 135, 32 157 against 259.)
+// attn_staged_kernels.hip, which is as fast or faster: one node on 64 requests of up to 4096 tokens
+// 110.5 against 115 us, four 122.5 against 122, eight 126 against 134, 32 174 against 231.)
 //
 // One wave streams its tiles from memory to registers, the next keys requested when the scores
 // are done with these and the next values when the output is.  Four waves are a workgroup:
@@ -234,9 +234,9 @@ AttnPlan attn_plan(bool bf16, int d, int page, long most, int R, int N, int h_q,
     AttnPlan p;
     const int M = N * (h_q / h_kv);
     // Pages of other sizes: a staged wave's rows have an address to a lane, which pays from 33 rows to a
-    // key head on.  16 requests of up to 4000 tokens, pages of 24 and 8 key heads of 256: 96 rows 142 us
-    // staged and 246 streamed, but 24 rows 98 and 91, four 92 and 70; pages of 100, 4 heads of 128: 48 rows
-    // 32 and 42, two 25 and 24.
+    // key head on.  16 requests of 100 to 4000 tokens, pages of 24 and 8 key heads of 256: 96 rows 126 us
+    // staged and 196 streamed, 36 rows 81 and 106, but 24 rows 76 and 65, four 73 and 52; pages of 100, 4 heads of
+    // 128: 48 rows 28.4 and 29.4, but 32 rows 25 and 28, two (one head of four) 23 and 24.
     p.staged = bf16 && (page % 16 == 0 || M > 32);
     // a staged wave always has 32 rows, idle ones load for the others; a streaming wave has as
     // many 16-row groups as the rows fill, and waves without rows take tiles instead
@@ -248,10 +248,12 @@ AttnPlan attn_plan(bool bf16, int d, int page, long most, int R, int N, int h_q,
     // one range for every workgroup that the chip holds at once (one or two to a compute unit)
     const long heads = (long)h_kv * p.RG, ranges = 256 * (p.staged ? (d == 256 ? 1 : 2) : waves_per_simd(bf16, d)) / heads;
     // A table of few columns holds no long request: one workgroup (of a key head) takes each, and
-    // nothing is joined.  Of up to 128 tokens, 32 query heads on 8 of 128: 64 requests of 8 nodes 14.2 us where
-    // cutting takes 22.9, of 64 nodes 42 for 57, one of one node 14.3 for 16.5 (one of 64 nodes on
-    // one head of 256 24.7 for 23.5).  Of up to 256: 17.6 for 25, 14.1 for 16.8; but with heads of 256 one
-    // of one node 19.1 for 16.6, and with 192 rows in fp32 33 for 21.  Of up to 512: 19 for 16.6.
+    // nothing is joined.  Room for 128 tokens, 32 query heads on 8 of 128: 64 requests of 8 nodes 13.0 us where
+    // cutting takes 23.7, of 64 nodes 42 for 59.5, one of one node 10.5 for 13.5 (one of 64 nodes on
+    // one head of 256 21.9 for 22.3).  For 256: 18.0 for 26.9, 13.6 for 13.5; but with heads of 256 one
+    // of one node 21.2 for 17.3, and with 192 rows in fp32 51 for 32.  For 512: one of one node 20 for
+    // 13.6.  It goes by the table, which the host knows: short requests in a table with room for a
+    // long context are cut.
     p.uncut = most <= 128 || (most <= 256 && M <= 64 && d <= 128);
     p.ranges = p.uncut ? R : (int)(ranges < 1 ? 1 : ranges);
     p.least = 4;   // tiles of a range, one to a wave

@@ -12,11 +12,11 @@
 // (c ^ (x / 2 & 7) in rows of 8 chunks), so that the 16 lanes that read one chunk of 16 keys, and
 // those that read 16 chunks of one key, meet different banks.
 //
-// What bounds it: memory, up to 32 nodes or so.  With the products taken out of a copy, the
-// loads alone of 64 requests of 2048 tokens (32 query heads on 8 of 128, 32 nodes) took 116 of
-// 123 us; one node on 64 requests of up to 4096 takes 112 us, 5.0 TB/s.  From 64 nodes
-// on the products do: 580 TFLOP/s, the vector units busy half the time and the matrix units a
-// quarter.
+// What bounds it: memory, up to 16 nodes or so (32 query heads on 8 of 128): one node on 64 requests of up
+// to 4096 tokens takes 110.5 us, 5.0 TB/s, 16 take 142.  From 32 nodes on the products and the softmax do: 64
+// requests of 2048 tokens and 32 nodes take 147.5 us, of which the loads alone (the products taken out of a
+// copy) 116; 64 nodes on up to 4096 take 285, 510 TFLOP/s of the formula's operations (a value's product
+// is done twice), the vector units busy 54 % of the time and the matrix units 37.
 #include <mutex>
 #include <type_traits>
 

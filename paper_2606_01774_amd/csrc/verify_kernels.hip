@@ -4,12 +4,17 @@
 //   stats  (row, part of the vocabulary): reads every row of logits that a walk may need once
 //          and leaves the part's maximum and sum of exponentials, or (greedy requests) the
 //          index of its maximum.  This is where the bytes are: 64 requests of 8 nodes over
-//          131072 bf16 logits, some greedy, 39 us, over 6 TB/s; bound by memory.
+//          131072 bf16 logits, 16 of them greedy (their draft rows are not read), 39 us, 222 MB at
+//          5.7 TB/s; bound by memory.
 //   walk   (request): the rows' laws and every child's odds at once, then the walk itself in
-//          LDS.  Only a refusal with a sibling left reads a row again, for the residual's mass.
-//          7.5 us for the same requests, 9 for trees of 24 over 100003 fp32 logits: latency.
-//   race   (request, part): argmax of law(t) / noise(t) over a part of one row; 13.6 us for the
-//          same 64 (67 MB, what a copy takes).  Short rows are raced over by the walk's workgroup.
+//          LDS.  7.5 us for the same requests, 9 for trees of 24 over 100003 fp32 logits with certain
+//          drafts: latency.  Only a refusal with a sibling left reads a row again, for the
+//          residual's mass, and that is one workgroup's work: with sampled drafts each such refusal takes 17 us
+//          over 131072 bf16 logits (5 over 32001), one after the other.  64 requests with 2, 4, 7
+//          drafts side by side: calls of 82, 114, 161 us where one takes 69.
+//   race   (request, part): argmax of law(t) / noise(t) over a part of one row; 13.8 us for the
+//          same 64 (50 MB read, 3.6 TB/s: half of it latency).  Short rows are raced over by the walk's
+//          workgroup.
 //   pick   (request): the best of the parts; 4 us, of which most is a launch's own.
 // Statistics, laws, residuals and scores are fp32, from logits of either type; the only rounding
 // to fewer bits is the caller's.
@@ -542,13 +547,15 @@ size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 }  // namespace
 
-// Parts of a row: enough workgroups for the chip (2048 hold all its threads), of two steps of
-// a workgroup's loads at least; of a row's statistics at most 64, one to a lane of the wave
-// that joins them.
+// Parts of a row: enough workgroups for the chip (2048 hold all its threads); of a row's statistics
+// at most 64, one to a lane of the wave that joins them.
 VerifyPlan verify_plan(int R, int N, int V)
 {
-    // as many parts as give 2048 workgroups, of 4096 logits or 1024 raced ones at least (a race
-    // is all latency: parts of 4096 took 8.6 us where those of 1024 take 6.3, 12 rows of 100003)
+    // As many parts as give 2048 workgroups, of 4096 logits or 1024 raced ones at least: less than an
+    // unrolled step of a workgroup's loads (8192 bf16 logits) and, raced in bf16, half a step, since few
+    // rows are all latency.  12 rows of 100003 fp32 logits: the race 6.3 us in parts of 1024, 8.6 in parts of 4096.
+    // Replayed calls for one row of 40003: fp32 16.7 us, 17.4 with raced parts of 2048, bf16 15.4 and
+    // 15.7; with statistics in parts of 8192 bf16 16.5 (over 131072 14.8 for 15.2).
     const auto cut = [V](long rows, long limit, int least, int &parts, int &part) {
         const long most = (V + least - 1) / least;
         long n = (2048 + rows - 1) / rows;
