@@ -433,7 +433,8 @@ int bdgdn_accept_states(const bdgdn_serve_desc_t *desc, float *state_pool, const
  * (fp32); else BDGDN_ERR_UNSUPPORTED.  The token tensors may be NULL when B*T == 0.
  * Results are deterministic.
  */
-typedef enum { BDGDN_ACT_NONE = 0, BDGDN_ACT_SILU = 1 } bdgdn_act_t;
+/* (the ShortConv takes the first two) */
+typedef enum { BDGDN_ACT_NONE = 0, BDGDN_ACT_SILU = 1, BDGDN_ACT_SIGMOID = 2 } bdgdn_act_t;
 
 typedef struct {
     int32_t batch;      /* B sequences; must be 1 when packed (num_seqs > 0)           */
@@ -714,6 +715,232 @@ int bdgdn_cache_compact(const bdgdn_cache_desc_t *cache, const bdgdn_cache_table
  * negative: 0, which frees the slot) and gives back the pages that they no longer use. */
 int bdgdn_cache_truncate(const bdgdn_cache_desc_t *cache, const bdgdn_cache_tables_t *tables, int32_t num_req,
                          const int32_t *slot, const int32_t *length, void *stream);
+
+/*
+ * ------------------------------------------------------------------------------------
+ * Around the mixers.  What a hybrid layer does with its rows before and behind the Gated
+ * DeltaNet and the attention, and with the logits before bdgdn_verify: rotary positions
+ * (bdgdn_rope), the norms behind and in front of a mixer with gate, scale and residual
+ * (bdgdn_norm_fwd, bdgdn_norm_bwd), projections in 8-bit integers (bdgdn_quant_rows,
+ * bdgdn_quant_matmul), penalties, biases and grammar masks (bdgdn_logits, bdgdn_history_add).
+ *
+ * Tensors of these calls have contiguous innermost rows and otherwise the strides (elements,
+ * not negative) of the descriptor, so they may be parts of the rows of one projection; they
+ * are aligned to an element, and run fastest where addresses and strides are multiples of 16
+ * bytes.  Rows of an output share no memory (BDGDN_ERR_INVALID_ARG).  Where a call may work in
+ * place, the output is the input: the same address and the same strides.
+ */
+typedef enum {
+    BDGDN_ROPE_HALF = 0,    /* element i of the rotated ones turns with element i + rot / 2 */
+    BDGDN_ROPE_PAIRS = 1    /* element 2 i turns with element 2 i + 1                       */
+} bdgdn_rope_layout_t;
+
+typedef enum {
+    BDGDN_ROPE_PLAIN = 0,   /* w_i = base^(-2 i / rot)                                      */
+    BDGDN_ROPE_LINEAR = 1,  /* w_i / factor: positions pressed together                     */
+    BDGDN_ROPE_NTK = 2,     /* base factor^(rot / (rot - 2)) for base                       */
+    BDGDN_ROPE_PARTS = 3    /* pairs that turn more than `fast` times over `original` positions
+                               keep w_i, those of fewer than `slow` turns take w_i / factor,
+                               those between a mixture of both, linear in the turns         */
+} bdgdn_rope_scaling_t;
+
+typedef struct {
+    int32_t rot;            /* rotated elements of a head, even                             */
+    int32_t scaling;        /* bdgdn_rope_scaling_t                                         */
+    double base, factor;    /* base >= 1, factor > 0                                        */
+    double original, slow, fast;   /* BDGDN_ROPE_PARTS: original > 0, 0 <= slow < fast      */
+} bdgdn_rope_freq_t;
+
+/* Fills turns_host[0 .. rot/2 - 1] (host memory) with the pairs' turns a position,
+ * w_i / (2 pi), as fractions in units of 2^-64 (whole turns left out).  A position's angle is
+ * then an integer product modulo 2^64: exact for every position, near or far. */
+int bdgdn_rope_freqs(const bdgdn_rope_freq_t *freq, uint64_t *turns_host);
+
+typedef struct {
+    int64_t req, row, head;          /* elements between requests, rows, heads              */
+} bdgdn_heads_t;
+
+typedef struct {
+    int32_t num_req, nodes;          /* R requests (or sequences) of N rows                 */
+    int32_t h_q, h_k;                /* heads of q and of k (0: q alone)                    */
+    int32_t d, rot;                  /* head dimension (at most 4096), rotated elements     */
+    int32_t layout;                  /* bdgdn_rope_layout_t                                 */
+    int32_t dtype;                   /* bdgdn_dtype_t of q, k and the outputs               */
+    int32_t inverse;                 /* turn back: the gradient of the rotation             */
+    int32_t n_slots;                 /* entries of seq_len                                  */
+    float scale;                     /* multiplies the rotated elements                     */
+    bdgdn_heads_t q, k, q_out, k_out;
+} bdgdn_rope_desc_t;
+
+/*
+ * Rotary positions.  The first rot elements of every head of row n of request r turn by the
+ * position p = seq_len[slot[r]] + pos[r][n]: a pair (a, b) becomes
+ *     scale (a cos t - b sin t),  scale (a sin t + b cos t),   t = 2 pi turns[i] p / 2^64
+ * the other elements stay.  inverse turns by -t: for an upstream gradient of the rotated rows
+ * it gives the gradient of the rows.
+ *   q, k        [R][N][heads][d] (k NULL where h_k is 0)
+ *   turns       [rot / 2] 64-bit words of bdgdn_rope_freqs, on the device
+ *   pos         [R][N] int32, or NULL for n (a tree's depths: bdgdn_tree_mask's depth)
+ *   seq_len     [n_slots] int32 cached tokens (negative: 0), or NULL for 0
+ *   slot        [R] int32, or NULL for slot[r] = r (then R <= n_slots); a slot outside
+ *               [0, n_slots) is an empty sequence
+ *   count       [R] int32 rows of each request, or NULL for N; rows behind them are not read
+ *               and their outputs left as they were
+ *   q_out, k_out  as q, k; may be q, k
+ * Angles are exact to 2^-33 of a turn, cos and sin to 2^-23; results are rounded once.
+ */
+int bdgdn_rope(const bdgdn_rope_desc_t *desc, const void *q, const void *k, const uint64_t *turns,
+               const int32_t *pos, const int32_t *seq_len, const int32_t *slot, const int32_t *count,
+               void *q_out, void *k_out, void *stream);
+
+typedef struct {
+    int64_t outer, inner;            /* elements between rows [a][b] in a and in b          */
+} bdgdn_rows_t;
+
+typedef struct {
+    int32_t outer, inner;            /* rows [outer][inner] (tokens and heads; inner 1)     */
+    int32_t d;                       /* elements of a row, 1 .. 16384                       */
+    int32_t x_dtype, r_dtype, dtype; /* bdgdn_dtype_t of x; of r and r_out; of z and y      */
+    int32_t post, pre;               /* 1: normalise behind the mixer, in front of the next */
+    int32_t act;                     /* bdgdn_act_t of the gate                             */
+    float scale, eps;
+    bdgdn_rows_t x, z, r, r_out, y;
+    bdgdn_rows_t dx, dz, dr, dr_out, dy;   /* the backward's                                */
+} bdgdn_norm_desc_t;
+
+/*
+ * The norms around a mixer, its gate, scale and residual, a row at a time:
+ *     n  = post ? x / rms(x) * w_post : x,          rms(x) = sqrt(mean x^2 + eps)
+ *     u  = z ? n act(z) : n
+ *     r' = r + scale layer_scale u
+ *     y  = pre ? r' / rms(r') * w_pre : r'
+ * With x alone and post it is an RMS norm, with z the gated norm of a Gated DeltaNet's heads.
+ *   x           mixer's output; z its gate or NULL; r the residual or NULL for 0
+ *   w_post, w_pre, layer_scale   [d] fp32, or NULL for 1
+ *   r_out       r', of r's type, may be r; or NULL
+ *   y           of dtype, or NULL (not both)
+ * Sums and statistics are fp32; y comes from the unrounded r'; each result is rounded once.
+ * Types: x, r, dtype bf16 or fp32, with dtype fp32 only if x and r are.  r_dtype counts also
+ * where there is no r.
+ */
+int bdgdn_norm_fwd(const bdgdn_norm_desc_t *desc, const void *x, const void *z, const void *r,
+                   const float *w_post, const float *w_pre, const float *layer_scale, void *r_out,
+                   void *y, void *stream);
+
+/* Bytes of device workspace bdgdn_norm_bwd needs, 0 for a descriptor that it rejects. */
+size_t bdgdn_norm_bwd_workspace(const bdgdn_norm_desc_t *desc);
+
+/*
+ * Its backward, for upstream gradients dy of y and dr_out of r'.
+ *   x, z, w_post, w_pre, layer_scale   what the forward took
+ *   r_out       the forward's r' (as stored); NULL only where it took no r: then r' is computed
+ *               again
+ *   dy          of dtype, dr_out of r_dtype; either NULL for 0
+ *   dx, dz, dr  of x's, z's and r's type, or NULL (dr may be dr_out)
+ *   dw_post, dw_pre, dlayer_scale   [d] fp32 sums over the rows, or NULL.  They need post, pre
+ *               and nothing; deterministic
+ *   workspace   256-byte aligned, owned by the call until the stream passes it
+ */
+int bdgdn_norm_bwd(const bdgdn_norm_desc_t *desc, const void *x, const void *z, const void *r_out,
+                   const float *w_post, const float *w_pre, const float *layer_scale, const void *dy,
+                   const void *dr_out, void *dx, void *dz, void *dr, float *dw_post, float *dw_pre,
+                   float *dlayer_scale, void *workspace, size_t workspace_bytes, void *stream);
+
+typedef struct {
+    int32_t num_req, nodes;          /* R requests of N nodes (the anchor and drafts), 1 .. 64 */
+    int32_t vocab;
+    int32_t dtype, out_dtype;        /* bdgdn_dtype_t of logits and out                     */
+    int32_t n_slots;                 /* rows of history                                     */
+    int32_t n_bias;                  /* entries of bias of each request                     */
+    int64_t req_stride, row_stride;            /* of logits                                 */
+    int64_t out_req_stride, out_row_stride;
+    int64_t history_stride;                    /* words between the slots' rows             */
+    int64_t allow_req_stride, allow_row_stride;   /* words; 0 for what all share            */
+} bdgdn_logits_desc_t;
+
+/*
+ * Logits as the requests ask for them, in front of bdgdn_verify (and for plain sampling with
+ * N = 1).  Row n of request r holds the logits after node n.  For token t, c is how often t has
+ * been generated, in the history of slot[r] or by a node that n's mask word names, and t is
+ * seen where c > 0 or the prompt holds it:
+ *     x = seen ? (x > 0 ? x / repetition : x repetition) : x
+ *     x = x - (c > 0 ? presence : 0) - frequency c
+ *     x = x + bias,   -inf where the grammar does not allow t
+ *   logits       [R][N][V] of dtype (rows contiguous)
+ *   history      [n_slots][V] int32: generated occurrences, + 2^30 where the prompt holds the
+ *                token (bdgdn_history_add); NULL for none
+ *   slot         [R] int32, or NULL for slot[r] = r (then R <= n_slots); a slot outside
+ *                [0, n_slots) has no history
+ *   token        [R][N] int32 the nodes' tokens, or NULL where they do not count; a token
+ *                outside [0, V) counts for nothing
+ *   mask         [R][N] 64-bit words of bdgdn_tree_mask (bit j: node j is n or its ancestor),
+ *                or NULL for chains
+ *   count        [R] int32 nodes of each request, or NULL for N; rows behind them are not read,
+ *                and left as they were
+ *   repetition, presence, frequency   [R] fp32, or NULL for 1, 0, 0; a repetition that is not
+ *                above zero counts as 1
+ *   bias_token, bias   [R][n_bias] int32 and fp32; entries outside [0, V) count for nothing, of
+ *                entries with one token the last one counts
+ *   allow        bit t % 32 of word t / 32 of the row: t is allowed; NULL: all are
+ *   out          [R][N][V] of out_dtype, may be logits where the types are the same
+ * fp32 arithmetic, rounded once.  (dtype, out_dtype): (bf16, bf16), (bf16, fp32), (fp32, fp32).
+ */
+int bdgdn_logits(const bdgdn_logits_desc_t *desc, const void *logits, const int32_t *history,
+                 const int32_t *slot, const int32_t *token, const uint64_t *mask, const int32_t *count,
+                 const float *repetition, const float *presence, const float *frequency,
+                 const int32_t *bias_token, const float *bias, const uint32_t *allow, void *out, void *stream);
+
+/*
+ * Adds tokens to histories: token[r][path[r][j]], j < count[r], of request r to the history of
+ * slot[r], as generated ones (one more each) or, with prompt 1, as the prompt's (bit 30 set).
+ *   history     [n_slots][vocab] int32 with history_stride between the slots
+ *   token       [R][N] int32 (outside [0, vocab): left out); path [R][N] int32 (bdgdn_verify's
+ *               path; a node outside [0, N) is left out) or NULL for rows in order
+ *   count       [R] int32 (clamped to 0 .. N), or NULL for N;  slot as for bdgdn_logits
+ * Slots may repeat.  A token may have been generated fewer than 2^30 times.
+ */
+int bdgdn_history_add(int32_t num_req, int32_t nodes, int32_t vocab, int32_t n_slots, int64_t history_stride,
+                      int32_t *history, const int32_t *slot, const int32_t *token, const int32_t *path,
+                      const int32_t *count, int32_t prompt, void *stream);
+
+typedef struct {
+    int32_t rows, cols;              /* of x                                                */
+    int32_t width;                   /* of q: cols filled up to a multiple of 128           */
+    int32_t dtype;                   /* bdgdn_dtype_t of x                                  */
+    int64_t x_stride, q_stride;      /* elements between rows                               */
+} bdgdn_quant_desc_t;
+
+/*
+ * 8-bit integers with a scale for each row (a token's activations, a channel's weights):
+ *     scale = max |x| / 127,  q = x / scale rounded to the nearest integer (of two the even one)
+ * with fp32 quotients.  Columns cols .. width - 1 of q are zeros.  A row of zeros has scale 0;
+ * a row that holds a NaN or an infinity scale NaN; q is 0 in both.
+ *   x  [rows][cols];  q  [rows][width] int8, 16-byte aligned, q_stride a multiple of 16
+ *   scale  [rows] fp32
+ */
+int bdgdn_quant_rows(const bdgdn_quant_desc_t *desc, const void *x, int8_t *q, float *scale, void *stream);
+
+typedef struct {
+    int32_t m, n, k;                 /* out [m][n]; k a multiple of 128, at most 130944     */
+    int32_t out_dtype;
+    int64_t a_stride, w_stride, out_stride;   /* elements between rows; a's and w's multiples of 16 */
+} bdgdn_quant_matmul_desc_t;
+
+/* Bytes of device workspace bdgdn_quant_matmul needs (0 also where it needs none). */
+size_t bdgdn_quant_matmul_workspace(const bdgdn_quant_matmul_desc_t *desc);
+
+/*
+ * The product of rows of 8-bit integers with scales for each token and channel:
+ *     out[i][j] = a_scale[i] w_scale[j] sum_k a[i][k] w[j][k] + bias[j]
+ *   a  [m][k] int8, w  [n][k] int8, 16-byte aligned (bdgdn_quant_rows fills k up with zeros)
+ *   a_scale [m], w_scale [n], bias [n] (or NULL) fp32;  out [m][n] of out_dtype
+ *   workspace   256-byte aligned, owned by the call until the stream passes it
+ * Sums are 32-bit integers and exact; the result is rounded to fp32 three times and to out's
+ * type once.  Deterministic.
+ */
+int bdgdn_quant_matmul(const bdgdn_quant_matmul_desc_t *desc, const int8_t *a, const float *a_scale,
+                       const int8_t *w, const float *w_scale, const float *bias, void *out, void *workspace,
+                       size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

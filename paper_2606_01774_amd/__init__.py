@@ -32,6 +32,10 @@ __all__ = [
     "BDGDN_CACHE_NO_ROOM", "BDGDN_CACHE_BAD_SLOT", "BDGDN_CACHE_BAD_KEEP", "CacheTables", "make_cache_tables",
     "bdgdn_tree_attn_workspace", "bdgdn_tree_attn", "bdgdn_tree_mask", "bdgdn_verify_workspace", "bdgdn_verify",
     "bdgdn_cache_workspace", "bdgdn_cache_append", "bdgdn_cache_fork", "bdgdn_cache_compact", "bdgdn_cache_truncate",
+    "BDGDN_ROPE_HALF", "BDGDN_ROPE_PAIRS", "BDGDN_ROPE_PLAIN", "BDGDN_ROPE_LINEAR", "BDGDN_ROPE_NTK", "BDGDN_ROPE_PARTS",
+    "BDGDN_ACT_SIGMOID", "BDGDN_HISTORY_PROMPT", "make_rope_turns", "bdgdn_rope", "bdgdn_norm_fwd",
+    "bdgdn_norm_bwd_workspace", "bdgdn_norm_bwd", "bdgdn_logits", "bdgdn_history_add", "bdgdn_quant_rows",
+    "bdgdn_quant_matmul_workspace", "bdgdn_quant_matmul",
 ]
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -64,7 +68,9 @@ EXPORTED_SYMBOLS = ("bdgdn_version", "bdgdn_status_string", "bdgdn_fwd_train_wor
                     "bdgdn_shortconv_bwd_noalloc", "bdgdn_bwd_train_workspace_segmented",
                     "bdgdn_tree_attn_workspace", "bdgdn_tree_attn", "bdgdn_tree_mask", "bdgdn_verify_workspace",
                     "bdgdn_verify", "bdgdn_cache_workspace", "bdgdn_cache_append", "bdgdn_cache_fork",
-                    "bdgdn_cache_compact", "bdgdn_cache_truncate")
+                    "bdgdn_cache_compact", "bdgdn_cache_truncate", "bdgdn_rope_freqs", "bdgdn_rope", "bdgdn_norm_fwd",
+                    "bdgdn_norm_bwd_workspace", "bdgdn_norm_bwd", "bdgdn_logits", "bdgdn_history_add",
+                    "bdgdn_quant_rows", "bdgdn_quant_matmul_workspace", "bdgdn_quant_matmul")
 
 
 class FwdDesc(ctypes.Structure):
@@ -165,6 +171,7 @@ def load_library():
     lib.bdgdn_shortconv_bwd_noalloc.argtypes = [ctypes.POINTER(ConvDesc)] + [P] * 13
     lib.bdgdn_shortconv_bwd_noalloc.restype = ctypes.c_int
     rounds.bind(lib)
+    layers.bind(lib)
     _lib = lib
     return lib
 
@@ -739,3 +746,10 @@ from .rounds import (  # noqa: E402
     BDGDN_MASK_BITS, BDGDN_MASK_CAUSAL, BDGDN_MASK_FULL, CacheTables, bdgdn_cache_append, bdgdn_cache_compact,
     bdgdn_cache_fork, bdgdn_cache_truncate, bdgdn_cache_workspace, bdgdn_tree_attn, bdgdn_tree_attn_workspace,
     bdgdn_tree_mask, bdgdn_verify, bdgdn_verify_workspace, make_cache_tables)
+
+# ------------------------------------------------------------------ around the mixers
+from . import layers  # noqa: E402
+from .layers import (  # noqa: E402
+    BDGDN_ACT_SIGMOID, BDGDN_HISTORY_PROMPT, BDGDN_ROPE_HALF, BDGDN_ROPE_LINEAR, BDGDN_ROPE_NTK, BDGDN_ROPE_PAIRS,
+    BDGDN_ROPE_PARTS, BDGDN_ROPE_PLAIN, bdgdn_history_add, bdgdn_logits, bdgdn_norm_bwd, bdgdn_norm_bwd_workspace,
+    bdgdn_norm_fwd, bdgdn_quant_matmul, bdgdn_quant_matmul_workspace, bdgdn_quant_rows, bdgdn_rope, make_rope_turns)

@@ -19,7 +19,8 @@ SOURCES = ["api.hip", "fwd_kernels.hip", "fwd_scan_kernels.hip", "fused_kernels.
            "split_kernels.hip", "conv_kernels.hip", "bwd_kernels.hip", "chunked_kernels.hip",
            "bwd_generic.hip", "bwd_steps.hip", "bwd_scan.hip", "attn_kernels.hip", "attn_staged_kernels.hip",
            "verify_kernels.hip",
-           "cache_kernels.hip", "round_api.hip"]
+           "cache_kernels.hip", "round_api.hip", "rope_kernels.hip", "norm_kernels.hip", "norm_bwd_kernels.hip",
+           "logits_kernels.hip", "quant_kernels.hip", "layer_api.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-I" + INCLUDE, "-I" + CSRC,
          # no packed-fp32 instructions in the device code

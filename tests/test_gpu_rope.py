@@ -1,0 +1,165 @@
+"""bdgdn_rope against the rotation in 64 bits.
+
+Tolerance.  The angle is the integer product rounded to 2^-32 of a turn: off by 2^-33 turns, under
+2^-30 radians.  cos and sin: the reduced angle (a rounding, and the constant's, of a number below 0.79:
+2^-23.3 x 0.79 at most), the series (2e-9) and four roundings of sums below 1 give under 2^-22.  The
+products and the sum with scale add three roundings of 2^-24 each of scale (|a| + |b|).  So each
+result is within 2^-21 scale (|a| + |b|) of the exact one, and half a step of its type.
+"""
+import math
+from fractions import Fraction
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2606_01774_amd as bd
+
+pytestmark = pytest.mark.gpu
+
+STEP = {torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}
+
+
+def reference(x, turns, pos, layout, scale, inverse):
+    """x [R, N, h, d] in 64 bits, turned by pos [R, N] (Python integers); also |a| + |b| of each element's pair."""
+    y, size = x.double().clone(), torch.zeros(x.shape, dtype=torch.float64)
+    rot = 2 * len(turns)
+    for i, F in enumerate(turns):
+        a, b = (i, i + rot // 2) if layout == "half" else (2 * i, 2 * i + 1)
+        part = [[(p * F) % (1 << 64) for p in row] for row in pos]
+        t = torch.tensor([[float(Fraction(w, 1 << 64)) for w in row] for row in part], dtype=torch.float64) * 2 * math.pi
+        c, s = torch.cos(t)[..., None] * scale, torch.sin(t)[..., None] * (-scale if inverse else scale)
+        xa, xb = x[..., a].double(), x[..., b].double()
+        y[..., a], y[..., b] = xa * c - xb * s, xa * s + xb * c
+        size[..., a] = size[..., b] = (xa.abs() + xb.abs()) * abs(scale)
+    return y, size
+
+
+def check(got, x, turns, pos, layout, scale, inverse):
+    want, size = reference(x.cpu(), [int(t) % (1 << 64) for t in turns.tolist()], pos, layout, scale, inverse)
+    err = (got.cpu().double() - want).abs()
+    assert (err <= 2.0 ** -21 * size + STEP[x.dtype] * want.abs()).all(), float((err / (size + 1e-30)).max())
+
+
+def positions(R, N, seq_len, slot, pos):
+    base = [0] * R if seq_len is None else [max(seq_len[s], 0) if 0 <= s < len(seq_len) else 0
+                                            for s in (slot if slot is not None else range(R))]
+    return [[base[r] + (n if pos is None else pos[r][n]) for n in range(N)] for r in range(R)]
+
+
+CASES = [  # R, N, h_q, h_k, d, rot
+    (1, 1, 32, 8, 128, 128), (1, 1, 1, 0, 64, 64), (3, 5, 4, 2, 128, 32), (2, 33, 6, 2, 80, 40), (2, 7, 3, 1, 256, 64),
+    (1, 70, 5, 5, 100, 10), (4, 3, 2, 1, 33, 6), (2, 2, 1, 1, 2, 2), (1, 3, 2, 1, 1024, 1024), (1, 2, 70, 3, 64, 16),
+    (2, 3, 2, 2, 4096, 4094),
+]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("layout", ["half", "pairs"])
+@pytest.mark.parametrize("R,N,h_q,h_k,d,rot", CASES)
+def test_rotation(R, N, h_q, h_k, d, rot, layout, dtype):
+    g = torch.Generator().manual_seed(d + rot)
+    q = torch.randn(R, N, h_q, d, generator=g).to(dtype).cuda()
+    k = torch.randn(R, N, h_k, d, generator=g).to(dtype).cuda() if h_k else None
+    turns, scale = bd.make_rope_turns(rot, scaling="parts" if rot > 2 else None, factor=4.0, original=4096)
+    out = bd.bdgdn_rope(q, turns, k, layout=layout, scale=scale)
+    pos = positions(R, N, None, None, None)
+    for got, x in zip(out if h_k else (out,), (q, k)):
+        check(got, x, turns, pos, layout, scale, False)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("layout", ["half", "pairs"])
+@pytest.mark.parametrize("d,rot", [(64, 32), (64, 64), (37, 6)])
+def test_positions_of_a_round(d, rot, layout, dtype):
+    """Depths of trees behind the cached tokens of slots, some not there, some far; rows behind a
+    request's nodes left as they were; forwards and back, in place and out of place."""
+    R, N, h_q, h_k = 5, 6, 3, 1
+    g = torch.Generator().manual_seed(7)
+    rows = torch.randn(R, N, h_q + 2 * h_k, d, generator=g).to(dtype).cuda()   # q, k, v of one projection
+    q, k = rows[:, :, :h_q], rows[:, :, h_q:h_q + h_k]
+    seq_len, slot = [3, 100000, -4, 2 ** 31 - 1, 77, 0], [1, 3, 9, 2, -1]
+    pos = torch.randint(-3, 12, (R, N), generator=g, dtype=torch.int32)
+    pos[1] = 2 ** 31 - 1
+    count = [6, 1, 0, 9, 3]
+    ints = lambda v: torch.tensor(v, dtype=torch.int32).cuda()  # noqa: E731
+    turns, _ = bd.make_rope_turns(rot, 500000.0)
+    want = positions(R, N, seq_len, slot, pos.tolist())
+    for inverse in (False, True):
+        kw = dict(pos=pos.cuda(), seq_len=ints(seq_len), slot=ints(slot), layout=layout, scale=0.7, inverse=inverse)
+        for got, x in zip(bd.bdgdn_rope(q, turns, k, **kw), (q, k)):
+            check(got, x, turns, want, layout, 0.7, inverse)
+        before = rows.clone()
+        out = torch.full_like(before, 5.0)
+        bd.bdgdn_rope(q, turns, k, count=ints(count), q_out=out[:, :, :h_q], k_out=out[:, :, h_q:h_q + h_k], **kw)
+        inside = before.clone()
+        bd.bdgdn_rope(inside[:, :, :h_q], turns, inside[:, :, h_q:h_q + h_k], count=ints(count),
+                      q_out=inside[:, :, :h_q], k_out=inside[:, :, h_q:h_q + h_k], **kw)
+        for r in range(R):
+            n = min(max(count[r], 0), N)
+            assert (out[r, n:] == 5).all() and torch.equal(inside[r, n:], before[r, n:])
+            for part, x in ((slice(0, h_q), q), (slice(h_q, h_q + h_k), k)):
+                check(out[r:r + 1, :n, part], x[r:r + 1, :n], turns, [want[r][:n]], layout, 0.7, inverse)
+                assert torch.equal(inside[r, :n, part], out[r, :n, part])
+        assert (out[:, :, h_q + h_k:] == 5).all() and torch.equal(inside[:, :, h_q + h_k:], before[:, :, h_q + h_k:])
+
+
+@pytest.mark.parametrize("offset,order", [(1, "thd"), (0, "htd"), (4, "htd")])
+def test_strides_and_addresses(offset, order):
+    """Heads before rows, addresses and strides that are no multiples of 16 bytes."""
+    R, N, h, d, rot = 2, 9, 3, 32, 16
+    pad = d + (3 if offset == 1 else 0)
+    shape = (R, N, h, pad) if order == "thd" else (R, h, N, pad)
+    flat = torch.randn(R * N * h * pad + 8, generator=torch.Generator().manual_seed(3)).bfloat16().cuda()
+    x = flat[offset:offset + R * N * h * pad].view(shape)
+    x = x[..., :d] if order == "thd" else x.transpose(1, 2)[..., :d]
+    turns, _ = bd.make_rope_turns(rot)
+    got = bd.bdgdn_rope(x, turns, layout="half")
+    check(got, x, turns, positions(R, N, None, None, None), "half", 1.0, False)
+    y = torch.zeros_like(flat)
+    view = y[offset:offset + R * N * h * pad].view(shape)
+    view = view[..., :d] if order == "thd" else view.transpose(1, 2)[..., :d]
+    bd.bdgdn_rope(x, turns, layout="half", q_out=view)
+    assert torch.equal(view, got) and int((y != 0).sum()) == int((got != 0).sum())
+
+
+def test_many_rows_take_the_same_values():
+    """What one row gives does not depend on how many rows and heads there are (the cut of the work)."""
+    turns, _ = bd.make_rope_turns(128)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    q = torch.empty(2, 5001, 32, 128, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    k = torch.empty(2, 5001, 8, 128, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    qo, ko = bd.bdgdn_rope(q, turns, k)
+    for n in (0, 1, 2500, 5000):
+        pos = torch.full((2, 1), n, dtype=torch.int32, device="cuda")
+        q1, k1 = bd.bdgdn_rope(q[:, n:n + 1], turns, k[:, n:n + 1], pos=pos)
+        assert torch.equal(q1, qo[:, n:n + 1]) and torch.equal(k1, ko[:, n:n + 1])
+    check(qo[:, -2:, ::16], q[:, -2:, ::16], turns, [[4999, 5000]] * 2, "half", 1.0, False)
+
+
+def test_gradient_is_the_inverse_rotation():
+    """Differences of <rotation(x), u> against the inverse rotation of u (the rotation is linear, so
+    central differences are exact up to rounding: 2^-21 of the sums' magnitudes)."""
+    R, N, h, d, rot = 1, 3, 2, 16, 8
+    g = torch.Generator().manual_seed(11)
+    x, u = (torch.randn(R, N, h, d, generator=g).cuda() for _ in range(2))
+    turns, _ = bd.make_rope_turns(rot)
+    pos = torch.tensor([[5, 900, 70000]], dtype=torch.int32).cuda()
+    for layout in ("half", "pairs"):
+        grad = bd.bdgdn_rope(u, turns, pos=pos, layout=layout, scale=1.5, inverse=True)
+        for n, hh, e in ((0, 0, 0), (1, 1, 7), (2, 0, 4), (2, 1, 12)):
+            step = torch.zeros_like(x)
+            step[0, n, hh, e] = 1.0
+            lo, hi = (bd.bdgdn_rope(x + s * step, turns, pos=pos, layout=layout, scale=1.5) for s in (-1.0, 1.0))
+            diff = float(((hi.double() - lo.double()) / 2 * u.double()).sum())
+            assert abs(diff - float(grad[0, n, hh, e])) < 2.0 ** -18 * 30
+
+
+def test_nothing_to_turn():
+    turns, _ = bd.make_rope_turns(8)
+    assert bd.bdgdn_rope(torch.zeros(0, 4, 2, 8, device="cuda"), turns).shape == (0, 4, 2, 8)
+    q, k = bd.bdgdn_rope(torch.zeros(2, 0, 2, 8, device="cuda"), turns, torch.zeros(2, 0, 1, 8, device="cuda"))
+    assert q.numel() == k.numel() == 0
+    x = torch.tensor([[[[float("nan"), 1.0, float("inf"), 2.0, 3.0, 4.0, 5.0, 6.0, 9.0]]]], device="cuda")
+    y = bd.bdgdn_rope(x, turns, layout="pairs", pos=torch.full((1, 1), 3, dtype=torch.int32, device="cuda"))
+    assert not y[..., :4].isfinite().any() and y[..., 4:].isfinite().all() and y[..., 8] == 9   # each pair by itself
