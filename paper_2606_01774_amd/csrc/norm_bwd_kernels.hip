@@ -14,119 +14,198 @@ namespace bdgdn {
 
 namespace {
 
-constexpr int kThreads = 1024;
+constexpr int kThreads = 512;
+constexpr int kMostGroups = 256;   // a workgroup to a compute unit
+
+// A lane's parts of the five rows that a row's gradients come from.
+template <typename X, typename R, typename Y, int LANES, int C, bool WIDE> struct BwdRows {
+    Ahead<WIDE, LANES, C, X> x;
+    Ahead<WIDE, LANES, C, Y> z, dy;
+    Ahead<WIDE, LANES, C, R> sum_r, g;
+    __device__ __forceinline__ void load(const NormArgs &a, unsigned row, int lane)
+    {
+        const int d = row < (unsigned)a.rows ? a.d : 0;
+        const int ra = d ? row / (unsigned)a.inner : 0, rb = d ? row - ra * (unsigned)a.inner : 0;
+        x.load(row_at<X>(a.x, a.sx, ra, rb), d, lane);
+        if (a.pre && a.r) sum_r.load(row_at<R>(a.r, a.sro, ra, rb), d, lane);
+        dy.load(row_at<Y>(a.dy, a.sdy, ra, rb), a.dy ? d : 0, lane);
+        if (a.z) z.load(row_at<Y>(a.z, a.sz, ra, rb), d, lane);
+        g.load(row_at<R>(a.dr_out, a.sdro, ra, rb), a.dr_out ? d : 0, lane);
+    }
+};
 
 template <typename X, typename R, typename Y, int LANES, int C, bool WIDE>
 __global__ void __launch_bounds__(kThreads) bdgdn_norm_bwd_kernel(NormArgs a)
 {
+    // One or two chunks to a lane stay in registers, and beside one the next row's, loaded ahead; of more
+    // each is read again (from the caches) where it is used.
+    constexpr bool ONE = C == 1, HOLD = C <= 2;
+    constexpr int H = HOLD ? C : 1;
+    constexpr auto at = [](int c) { return HOLD ? c : 0; };
     constexpr int ROWS = kThreads / LANES;
     constexpr int UNITS = LANES < 64 ? kThreads / 64 : ROWS;   // that hold sums of the same elements
-    __shared__ float lds[3 * (kThreads / 64)];
+    __shared__ float lds[2 * 3 * (kThreads / 64)];
+    RowSum<LANES, kThreads, 3> row_sum(lds);
     __shared__ float meet[UNITS > 1 ? UNITS * LANES * 8 : 1];
     const int lane = threadIdx.x % LANES;
-    float wp[C][8], wq[C][8], ls[C][8];
-    if (a.w_post) load_row<WIDE, LANES>(wp, a.w_post, a.d, lane);
-    if (a.w_pre) load_row<WIDE, LANES>(wq, a.w_pre, a.d, lane);
-    if (a.ls) load_row<WIDE, LANES>(ls, a.ls, a.d, lane);
-#pragma unroll
-    for (int c = 0; c < C; ++c)
+    float wp[H][8], wq[H][8], ls[H][8];
+    auto weights = [&](int c) {
+        if (a.w_post) load_chunk<WIDE, LANES>(wp[at(c)], a.w_post, c, a.d, lane);
+        if (a.w_pre) load_chunk<WIDE, LANES>(wq[at(c)], a.w_pre, c, a.d, lane);
+        if (a.ls) load_chunk<WIDE, LANES>(ls[at(c)], a.ls, c, a.d, lane);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            if (!a.w_post) wp[c][i] = 1.f;
-            if (!a.w_pre) wq[c][i] = 1.f;
-            ls[c][i] = a.ls ? a.scale * ls[c][i] : a.scale;
+            if (!a.w_post) wp[at(c)][i] = 1.f;
+            if (!a.w_pre) wq[at(c)][i] = 1.f;
+            ls[at(c)][i] = a.ls ? a.scale * ls[at(c)][i] : a.scale;
         }
+    };
+    if (ONE) weights(0);
+    // the gate and its slope
+    auto gate = [&](float z, float &act, float &slope) {
+        const float e = a.act ? sigmoid(z) : z;
+        act = a.act == kActSilu ? z * e : e;
+        slope = a.act == kActSilu ? e * (1.f + z * (1.f - e)) : a.act ? e * (1.f - e) : 1.f;
+    };
     float acc[3][C][8] = {};   // of w_post, w_pre, layer_scale
 
-    for (unsigned row0 = blockIdx.x * ROWS; row0 < (unsigned)a.rows; row0 += gridDim.x * ROWS) {
-        const unsigned row = row0 + threadIdx.x / LANES;
+    const unsigned stride = gridDim.x * ROWS, mine = row_of<LANES>();
+    BwdRows<X, R, Y, LANES, H, WIDE> next;
+    if (ONE) next.load(a, blockIdx.x * ROWS + mine, lane);
+    for (unsigned row0 = blockIdx.x * ROWS; row0 < (unsigned)a.rows; row0 += stride) {
+        const unsigned row = row0 + mine;
         const bool there = row < (unsigned)a.rows;   // (sums meet at barriers)
         const int d = there ? a.d : 0, ra = there ? row / (unsigned)a.inner : 0, rb = there ? row - ra * (unsigned)a.inner : 0;
-        float x[C][8], z[C][8], sum_r[C][8], dy[C][8], g[C][8];
-        load_row<WIDE, LANES>(x, row_at<X>(a.x, a.sx, ra, rb), d, lane);
-        if (a.z) load_row<WIDE, LANES>(z, row_at<Y>(a.z, a.sz, ra, rb), d, lane);
-        if (a.r) load_row<WIDE, LANES>(sum_r, row_at<R>(a.r, a.sro, ra, rb), d, lane);
-        load_row<WIDE, LANES>(dy, row_at<Y>(a.dy, a.sdy, ra, rb), a.dy ? d : 0, lane);
-        load_row<WIDE, LANES>(g, row_at<R>(a.dr_out, a.sdro, ra, rb), a.dr_out ? d : 0, lane);
-        float s1 = 1.f, s2 = 1.f, mean_t = 0.f;
         const bool joint = a.pre && a.r;
+        float x[H][8], z[H][8], sum_r[H][8], dy[H][8], g[H][8], t[C][8];
+        auto read_x = [&](int c) { load_chunk<WIDE, LANES>(x[at(c)], row_at<X>(a.x, a.sx, ra, rb), c, d, lane); };
+        auto read_z = [&](int c) { load_chunk<WIDE, LANES>(z[at(c)], row_at<Y>(a.z, a.sz, ra, rb), c, d, lane); };
+        auto read_r = [&](int c) { load_chunk<WIDE, LANES>(sum_r[at(c)], row_at<R>(a.r, a.sro, ra, rb), c, d, lane); };
+        auto read_dy = [&](int c) { load_chunk<WIDE, LANES>(dy[at(c)], row_at<Y>(a.dy, a.sdy, ra, rb), c, a.dy ? d : 0, lane); };
+        auto read_g = [&](int c) { load_chunk<WIDE, LANES>(g[at(c)], row_at<R>(a.dr_out, a.sdro, ra, rb), c, a.dr_out ? d : 0, lane); };
+        if (HOLD) {
+            if (!ONE) {
+                next.load(a, row, lane);
+#pragma unroll
+                for (int c = 0; c < C; ++c) weights(c);
+            }
+            next.x.get(x);
+            next.dy.get(dy);
+            next.g.get(g);
+            if (a.z) next.z.get(z);
+            if (joint) next.sum_r.get(sum_r);
+            if (ONE) next.load(a, row + stride, lane);
+        }
+        float s1 = 1.f, s2 = 1.f, mean_t = 0.f;
         if (a.post || joint) {
             float sum[3] = {0.f, 0.f, 0.f};
 #pragma unroll
-            for (int c = 0; c < C; ++c)
+            for (int c = 0; c < C; ++c) {
+                if (!HOLD && joint) weights(c);
+                if (!HOLD) {
+                    read_x(c);
+                    if (joint) {
+                        read_r(c);
+                        read_dy(c);
+                    }
+                    asm volatile("" ::: "memory");
+                }
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    sum[0] = fmaf(x[c][i], x[c][i], sum[0]);
+                    sum[0] = fmaf(x[at(c)][i], x[at(c)][i], sum[0]);
                     if (joint) {
-                        sum[1] = fmaf(sum_r[c][i], sum_r[c][i], sum[1]);
-                        sum[2] = fmaf(dy[c][i] * wq[c][i], sum_r[c][i], sum[2]);
+                        sum[1] = fmaf(sum_r[at(c)][i], sum_r[at(c)][i], sum[1]);
+                        sum[2] = fmaf(dy[at(c)][i] * wq[at(c)][i], sum_r[at(c)][i], sum[2]);
                     }
                 }
-            row_sum<LANES, kThreads>(sum, lds);
+            }
+            row_sum(sum);
             if (a.post) s1 = 1.f / sqrtf(fmaf(sum[0], a.inv_d, a.eps));
             if (joint) {
                 s2 = 1.f / sqrtf(fmaf(sum[1], a.inv_d, a.eps));
                 mean_t = sum[2] * s2 * a.inv_d;
             }
         }
-        if (a.pre && !a.r) {   // r' = s l u
+        // r' = s l u where there is no residual
+        auto sum_again = [&](int c, int i) {
+            float act = 1.f, slope;
+            if (a.z) gate(z[at(c)][i], act, slope);
+            sum_r[at(c)][i] = (a.post ? x[at(c)][i] * s1 * wp[at(c)][i] : x[at(c)][i]) * act * ls[at(c)][i];
+        };
+        if (a.pre && !a.r) {
             float sum[2] = {0.f, 0.f};
 #pragma unroll
-            for (int c = 0; c < C; ++c)
+            for (int c = 0; c < C; ++c) {
+                if (!HOLD) weights(c);
+                if (!HOLD) {
+                    read_x(c);
+                    read_dy(c);
+                    if (a.z) read_z(c);
+                    asm volatile("" ::: "memory");
+                }
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    float u = a.post ? x[c][i] * s1 * wp[c][i] : x[c][i];
-                    if (a.z) {
-                        const float e = a.act ? sigmoid(z[c][i]) : z[c][i];
-                        u *= a.act == kActSilu ? z[c][i] * e : e;
-                    }
-                    sum_r[c][i] = u * ls[c][i];
-                    sum[0] = fmaf(sum_r[c][i], sum_r[c][i], sum[0]);
-                    sum[1] = fmaf(dy[c][i] * wq[c][i], sum_r[c][i], sum[1]);
+                    sum_again(c, i);
+                    sum[0] = fmaf(sum_r[at(c)][i], sum_r[at(c)][i], sum[0]);
+                    sum[1] = fmaf(dy[at(c)][i] * wq[at(c)][i], sum_r[at(c)][i], sum[1]);
                 }
-            row_sum<LANES, kThreads>(sum, lds);
+            }
+            row_sum(sum);
             s2 = 1.f / sqrtf(fmaf(sum[0], a.inv_d, a.eps));
             mean_t = sum[1] * s2 * a.inv_d;
         }
         float sum[1] = {0.f};
 #pragma unroll
-        for (int c = 0; c < C; ++c)
+        for (int c = 0; c < C; ++c) {
+            if (!HOLD) weights(c);
+            if (!HOLD) {
+                read_x(c);
+                read_dy(c);
+                read_g(c);
+                if (a.z) read_z(c);
+                if (joint) read_r(c);
+                asm volatile("" ::: "memory");
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 if (a.pre) {
-                    const float h = sum_r[c][i] * s2;
-                    if (there) acc[1][c][i] = fmaf(dy[c][i], h, acc[1][c][i]);
-                    g[c][i] += s2 * (dy[c][i] * wq[c][i] - h * mean_t);
+                    if (!HOLD && !a.r) sum_again(c, i);
+                    const float h = sum_r[at(c)][i] * s2;
+                    if (there) acc[1][c][i] = fmaf(dy[at(c)][i], h, acc[1][c][i]);
+                    g[at(c)][i] += s2 * (dy[at(c)][i] * wq[at(c)][i] - h * mean_t);
                 } else {
-                    g[c][i] += dy[c][i];
+                    g[at(c)][i] += dy[at(c)][i];
                 }
-                const float xh = a.post ? x[c][i] * s1 : x[c][i], n = a.post ? xh * wp[c][i] : xh;
+                const float xh = a.post ? x[at(c)][i] * s1 : x[at(c)][i], n = a.post ? xh * wp[at(c)][i] : xh;
                 float act = 1.f, slope = 0.f;
-                if (a.z) {
-                    const float e = a.act ? sigmoid(z[c][i]) : z[c][i];
-                    act = a.act == kActSilu ? z[c][i] * e : e;
-                    slope = a.act == kActSilu ? e * (1.f + z[c][i] * (1.f - e)) : a.act ? e * (1.f - e) : 1.f;
-                }
-                if (there) acc[2][c][i] = fmaf(a.scale * g[c][i], n * act, acc[2][c][i]);
-                const float du = ls[c][i] * g[c][i], dn = du * act;
-                z[c][i] = du * n * slope;
+                if (a.z) gate(z[at(c)][i], act, slope);
+                if (there) acc[2][c][i] = fmaf(a.scale * g[at(c)][i], n * act, acc[2][c][i]);
+                const float du = ls[at(c)][i] * g[at(c)][i], dn = du * act;
+                z[at(c)][i] = du * n * slope;
                 if (there) acc[0][c][i] = fmaf(dn, xh, acc[0][c][i]);
-                x[c][i] = xh;
-                dy[c][i] = a.post ? dn * wp[c][i] : dn;
-                sum[0] = fmaf(dy[c][i], xh, sum[0]);
+                x[at(c)][i] = xh;
+                t[c][i] = a.post ? dn * wp[at(c)][i] : dn;
+                sum[0] = fmaf(t[c][i], xh, sum[0]);
             }
-        if (a.dr) store_row<WIDE, LANES>(row_at<R>(a.dr, a.sdr, ra, rb), g, d, lane);
-        if (a.dz) store_row<WIDE, LANES>(row_at<Y>(a.dz, a.sdz, ra, rb), z, d, lane);
+            if (a.dr) store_chunk<WIDE, LANES>(row_at<R>(a.dr, a.sdr, ra, rb), g[at(c)], c, d, lane);
+            if (a.dz) store_chunk<WIDE, LANES>(row_at<Y>(a.dz, a.sdz, ra, rb), z[at(c)], c, d, lane);
+        }
         if (!a.dx) continue;
         if (a.post) {
-            row_sum<LANES, kThreads>(sum, lds);
+            row_sum(sum);
             const float mean = sum[0] * a.inv_d;
 #pragma unroll
-            for (int c = 0; c < C; ++c)
+            for (int c = 0; c < C; ++c) {
+                if (!HOLD) {
+                    read_x(c);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) dy[c][i] = s1 * (dy[c][i] - x[c][i] * mean);
+                    for (int i = 0; i < 8; ++i) x[at(c)][i] *= s1;
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) t[c][i] = s1 * (t[c][i] - x[at(c)][i] * mean);
+            }
         }
-        store_row<WIDE, LANES>(row_at<X>(a.dx, a.sdx, ra, rb), dy, d, lane);
+        store_row<WIDE, LANES>(row_at<X>(a.dx, a.sdx, ra, rb), t, d, lane);
     }
 
     // the workgroup's sums
@@ -164,8 +243,11 @@ __global__ void __launch_bounds__(1024) bdgdn_norm_weights_kernel(NormArgs a)
     const int k = blockIdx.y, e = blockIdx.x * 64 + (threadIdx.x & 63), u = threadIdx.x >> 6;
     if (!a.dw[k]) return;
     float v = 0.f;
-    if (e < a.d)
-        for (int p = u; p < a.groups; p += 16) v += a.part[((long)p * 3 + k) * a.d + e];
+#pragma unroll
+    for (int i = 0; i < kMostGroups / 16; ++i) {   // (all of them in flight)
+        const int p = u + 16 * i;
+        v += p < a.groups && e < a.d ? a.part[((long)p * 3 + k) * a.d + e] : 0.f;
+    }
     lds[u][threadIdx.x & 63] = v;
     __syncthreads();
     if (u == 0 && e < a.d) {
@@ -187,8 +269,8 @@ template <typename X, typename R, typename Y> hipError_t sized(const NormArgs &a
         else if (a.d <= 512) launch<X, R, Y, 64, 1>(a, s);
         else if (a.d <= 2048) launch<X, R, Y, 256, 1>(a, s);
         else if (a.d <= 4096) launch<X, R, Y, 512, 1>(a, s);
-        else if (a.d <= 8192) launch<X, R, Y, 1024, 1>(a, s);
-        else launch<X, R, Y, 1024, 2>(a, s);
+        else if (a.d <= 8192) launch<X, R, Y, 512, 2>(a, s);
+        else launch<X, R, Y, 512, 4>(a, s);
     }
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && (a.dw[0] || a.dw[1] || a.dw[2])) {
@@ -202,9 +284,9 @@ template <typename X, typename R, typename Y> hipError_t sized(const NormArgs &a
 
 int norm_bwd_groups(int rows, int d)
 {
-    const int lanes = d <= 128 ? 16 : d <= 512 ? 64 : d <= 2048 ? 256 : d <= 4096 ? 512 : 1024, in_one = kThreads / lanes;
+    const int lanes = d <= 128 ? 16 : d <= 512 ? 64 : d <= 2048 ? 256 : 512, in_one = kThreads / lanes;
     const int groups = (int)(((long)rows + in_one - 1) / in_one);
-    return groups < 512 ? groups : 512;
+    return groups < kMostGroups ? groups : kMostGroups;
 }
 
 hipError_t launch_norm_bwd(bool xf, bool rf, bool yf, NormArgs &a, hipStream_t s)

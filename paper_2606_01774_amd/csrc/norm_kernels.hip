@@ -12,23 +12,30 @@ template <typename X, typename R, typename Y, int LANES, int C, bool WIDE>
 __global__ void __launch_bounds__(LANES > 256 ? LANES : 256) bdgdn_norm_fwd_kernel(NormArgs a)
 {
     constexpr int THREADS = LANES > 256 ? LANES : 256;
-    __shared__ float lds[THREADS / 64];
+    __shared__ float lds[2 * (THREADS / 64)];
+    RowSum<LANES, THREADS, 1> row_sum(lds);
     const int lane = threadIdx.x % LANES;
     for (unsigned row0 = blockIdx.x * (THREADS / LANES); row0 < (unsigned)a.rows; row0 += gridDim.x * (THREADS / LANES)) {
-        const unsigned row = row0 + threadIdx.x / LANES;
+        const unsigned row = row0 + row_of<LANES>();
         const bool there = row < (unsigned)a.rows;   // (sums meet at barriers)
         const int d = there ? a.d : 0, ra = there ? row / (unsigned)a.inner : 0, rb = there ? row - ra * (unsigned)a.inner : 0;
         float x[C][8], z[C][8], r[C][8];
-        load_row<WIDE, LANES>(x, row_at<X>(a.x, a.sx, ra, rb), d, lane);
-        if (a.z) load_row<WIDE, LANES>(z, row_at<Y>(a.z, a.sz, ra, rb), d, lane);
-        if (a.r) load_row<WIDE, LANES>(r, row_at<R>(a.r, a.sr, ra, rb), d, lane);
+        Ahead<WIDE, LANES, C, X> ax;
+        Ahead<WIDE, LANES, C, Y> az;
+        Ahead<WIDE, LANES, C, R> ar;
+        ax.load(row_at<X>(a.x, a.sx, ra, rb), d, lane);
+        if (a.z) az.load(row_at<Y>(a.z, a.sz, ra, rb), d, lane);
+        if (a.r) ar.load(row_at<R>(a.r, a.sr, ra, rb), d, lane);
+        ax.get(x);
+        if (a.z) az.get(z);
+        if (a.r) ar.get(r);
         if (a.post) {
             float sum[1] = {0.f};
 #pragma unroll
             for (int c = 0; c < C; ++c)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sum[0] = fmaf(x[c][i], x[c][i], sum[0]);
-            row_sum<LANES, THREADS>(sum, lds);
+            row_sum(sum);
             const float s1 = 1.f / sqrtf(fmaf(sum[0], a.inv_d, a.eps));
             float w[C][8];
             if (a.w_post) load_row<WIDE, LANES>(w, a.w_post, d, lane);
@@ -65,7 +72,7 @@ __global__ void __launch_bounds__(LANES > 256 ? LANES : 256) bdgdn_norm_fwd_kern
             for (int c = 0; c < C; ++c)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sum[0] = fmaf(x[c][i], x[c][i], sum[0]);
-            row_sum<LANES, THREADS>(sum, lds);
+            row_sum(sum);
             const float s2 = 1.f / sqrtf(fmaf(sum[0], a.inv_d, a.eps));
             float w[C][8];
             if (a.w_pre) load_row<WIDE, LANES>(w, a.w_pre, d, lane);
