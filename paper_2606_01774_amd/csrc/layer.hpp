@@ -20,9 +20,9 @@ struct RopeArgs {
     float scale, sine;         // sine: +-scale
     // how the work is cut: 2^item_log lanes to the pieces of a head, 2^sub_log head-lanes to a row of
     // a workgroup, 2^row_log rows to a workgroup
-    int items, item_log, sub_log, row_log;
+    int items, turned, item_log, sub_log, row_log;   // items: pieces, of which the first `turned` turn
 };
-hipError_t launch_rope(bool bf16, bool pairs, bool wide, RopeArgs &a, hipStream_t s);
+hipError_t launch_rope(bool bf16, bool pairs, RopeArgs &a, hipStream_t s);
 
 // ------------------------------------------------------------------ norms (norm_kernels.hip, norm_bwd_kernels.hip)
 struct RowStride {
@@ -40,7 +40,7 @@ struct NormArgs {
     int rows, inner, d;
     int post, pre, act;
     float scale, eps, inv_d;
-    int vec, groups;
+    int groups;
 };
 // Types of x, of the residual, of the gate and y: fp32 (true) or bf16.
 hipError_t launch_norm_fwd(bool xf, bool rf, bool yf, NormArgs &a, hipStream_t s);

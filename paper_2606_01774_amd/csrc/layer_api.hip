@@ -41,13 +41,6 @@ bool disjoint(int64_t inner, int n, const int64_t *size, const int64_t *stride)
     return true;
 }
 
-bool multiples(int64_t unit, int n, const int64_t *size, const int64_t *stride)
-{
-    for (int i = 0; i < n; ++i)
-        if (size[i] > 1 && stride[i] % unit) return false;
-    return true;
-}
-
 // ------------------------------------------------------------------ rotary positions
 int check_rope(const bdgdn_rope_desc_t *d)
 {
@@ -102,25 +95,19 @@ struct NormTensor {
     bool out;
 };
 
-// Checks the tensors that are there, and whether all of them and the weights can be read 16 bytes at a time.
-int check_tensors(const bdgdn_norm_desc_t *d, const NormTensor *t, int n, const float *const *weights, int n_weights, int &vec)
+// Checks the tensors that are there.
+int check_tensors(const bdgdn_norm_desc_t *d, const NormTensor *t, int n, const float *const *weights, int n_weights)
 {
-    vec = d->d % 8 == 0;
     for (int i = 0; i < n; ++i) {
         if (!t[i].p) continue;
         const int st = check_rows(d, *t[i].s, t[i].out);
         if (st != BDGDN_OK) return st;
-        const int size = size_of(t[i].dtype);
-        if (!aligned(t[i].p, size)) return BDGDN_ERR_INVALID_ARG;
-        const int64_t sizes[2] = {d->outer, d->inner}, stride[2] = {t[i].s->outer, t[i].s->inner};
-        if (!aligned(t[i].p, 16) || !multiples(16 / size, 2, sizes, stride)) vec = 0;
+        if (!aligned(t[i].p, size_of(t[i].dtype))) return BDGDN_ERR_INVALID_ARG;
         t[i].to->outer = t[i].s->outer;
         t[i].to->inner = t[i].s->inner;
     }
-    for (int i = 0; i < n_weights; ++i) {
+    for (int i = 0; i < n_weights; ++i)
         if (!aligned(weights[i], 4)) return BDGDN_ERR_INVALID_ARG;
-        if (!aligned(weights[i], 16)) vec = 0;
-    }
     return BDGDN_OK;
 }
 
@@ -242,16 +229,10 @@ int bdgdn_rope(const bdgdn_rope_desc_t *desc, const void *q, const void *k, cons
     a.y[0] = static_cast<unsigned char *>(q_out);
     a.y[1] = static_cast<unsigned char *>(k_out);
     const bdgdn_heads_t *s[2][2] = {{&desc->q, &desc->q_out}, {&desc->k, &desc->k_out}};
-    const int64_t unit = 16 / size;
-    // 16 bytes at a time: all addresses, strides and parts of a head in whole pieces
-    bool wide = desc->d % unit == 0 && desc->rot % (desc->layout == BDGDN_ROPE_HALF ? 2 * unit : unit) == 0;
     for (int w = 0; w <= (with_k ? 1 : 0); ++w) {
         for (int o = 0; o < 2; ++o) {
-            const int64_t sizes[3] = {desc->num_req, desc->nodes, w ? desc->h_k : desc->h_q};
             const int64_t stride[3] = {s[w][o]->req, s[w][o]->row, s[w][o]->head};
-            long *to = o ? a.ys[w] : a.xs[w];
-            for (int i = 0; i < 3; ++i) to[i] = stride[i] * (long)size;
-            wide = wide && multiples(unit, 3, sizes, stride) && aligned(o ? a.y[w] : a.x[w], 16);
+            for (int i = 0; i < 3; ++i) (o ? a.ys : a.xs)[w][i] = stride[i] * (long)size;
         }
     }
     a.turns = turns; a.pos = pos; a.len = seq_len; a.slot = slot; a.count = count;
@@ -260,7 +241,7 @@ int bdgdn_rope(const bdgdn_rope_desc_t *desc, const void *q, const void *k, cons
     a.in_place = q == q_out && (!with_k || k == k_out);
     a.scale = desc->scale;
     a.sine = desc->inverse ? -desc->scale : desc->scale;
-    return status_of(launch_rope(desc->dtype == BDGDN_BF16, desc->layout == BDGDN_ROPE_PAIRS, wide, a, static_cast<hipStream_t>(stream)));
+    return status_of(launch_rope(desc->dtype == BDGDN_BF16, desc->layout == BDGDN_ROPE_PAIRS, a, static_cast<hipStream_t>(stream)));
 }
 
 int bdgdn_norm_fwd(const bdgdn_norm_desc_t *desc, const void *x, const void *z, const void *r,
@@ -277,7 +258,7 @@ int bdgdn_norm_fwd(const bdgdn_norm_desc_t *desc, const void *x, const void *z, 
                              {r, &desc->r, &a.sr, desc->r_dtype, false}, {r_out, &desc->r_out, &a.sro, desc->r_dtype, true},
                              {y, &desc->y, &a.sy, desc->dtype, true}};
     const float *weights[3] = {a.w_post, a.w_pre, a.ls};
-    st = check_tensors(desc, t, 5, weights, 3, a.vec);
+    st = check_tensors(desc, t, 5, weights, 3);
     if (st != BDGDN_OK) return st;
     a.x = x; a.z = z; a.r = r; a.r_out = r_out; a.y = y;
     return status_of(launch_norm_fwd(desc->x_dtype == BDGDN_F32, desc->r_dtype == BDGDN_F32, desc->dtype == BDGDN_F32, a,
@@ -309,7 +290,7 @@ int bdgdn_norm_bwd(const bdgdn_norm_desc_t *desc, const void *x, const void *z, 
                                  {dr_out, &desc->dr_out, &a.sdro, desc->r_dtype, false}, {dx, &desc->dx, &a.sdx, desc->x_dtype, true},
                                  {dz, &desc->dz, &a.sdz, desc->dtype, true}, {dr, &desc->dr, &a.sdr, desc->r_dtype, true}};
         const float *weights[3] = {a.w_post, a.w_pre, a.ls};
-        st = check_tensors(desc, t, 8, weights, 3, a.vec);
+        st = check_tensors(desc, t, 8, weights, 3);
         if (st != BDGDN_OK) return st;
         if (sums) {
             if (!aligned(workspace, 256)) return BDGDN_ERR_INVALID_ARG;

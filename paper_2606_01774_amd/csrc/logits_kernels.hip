@@ -6,7 +6,7 @@
 // and the biases of a lane's tokens stay in registers, each row of logits is read and written once.
 // What a tile holds beside its history, a request's biases and the nodes' own tokens, is found
 // once a tile: an LDS word for every token names its bias and says whether a node carries it.
-#include "common.hpp"
+#include "anywhere.hpp"
 #include "layer.hpp"
 
 namespace bdgdn {
@@ -18,49 +18,6 @@ constexpr int kPer = 8;                       // tokens of a lane
 constexpr int kTile = kThreads * kPer;
 constexpr int32_t kPrompt = 1 << 30;
 constexpr uint32_t kNode = 0x80000000u;       // a node of the block carries the token
-
-typedef u32x4 u32x4_e2 __attribute__((aligned(2)));
-typedef u32x4 u32x4_e4 __attribute__((aligned(4)));
-
-// Eight logits at any element.
-__device__ __forceinline__ void load8(float (&v)[8], const __bf16 *p)
-{
-    const u32x4 w = *reinterpret_cast<const u32x4_e2 *>(p);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(w[i] << 16);
-        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-}
-__device__ __forceinline__ void load8(float (&v)[8], const float *p)
-{
-    const u32x4 a = *reinterpret_cast<const u32x4_e4 *>(p), b = *reinterpret_cast<const u32x4_e4 *>(p + 4);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        v[i] = __uint_as_float(a[i]);
-        v[4 + i] = __uint_as_float(b[i]);
-    }
-}
-__device__ __forceinline__ void store8(__bf16 *p, const float (&v)[8])
-{
-    bf16x8 w;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = (__bf16)v[i];
-    u32x4 u;
-    __builtin_memcpy(&u, &w, 16);
-    *reinterpret_cast<u32x4_e2 *>(p) = u;
-}
-__device__ __forceinline__ void store8(float *p, const float (&v)[8])
-{
-    u32x4 a, b;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        a[i] = __float_as_uint(v[i]);
-        b[i] = __float_as_uint(v[4 + i]);
-    }
-    *reinterpret_cast<u32x4_e4 *>(p) = a;
-    *reinterpret_cast<u32x4_e4 *>(p + 4) = b;
-}
 
 template <typename X, typename Y> __global__ void __launch_bounds__(kThreads) bdgdn_logits_kernel(LogitsArgs a)
 {

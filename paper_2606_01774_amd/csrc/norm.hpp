@@ -1,132 +1,95 @@
 // norm.hpp -- what the forward and the backward of the norms around a mixer share: a row's elements
 // in the registers of its lanes, the gate, sums over a row.
 //
-// A row belongs to LANES lanes, each with C chunks of 8 of its elements in registers, so that a
-// row is read once however many sums it needs.  WIDE: a chunk is 8 neighbouring elements (16 or
-// 32 bytes); else (odd sizes, addresses or strides) elements LANES apart, one load each.
+// A row belongs to LANES lanes, each with C chunks of 8 neighbouring elements of it, so that a row is
+// read once however many sums it needs.  Chunks are 16 or 32 bytes at any element's address.  WHOLE:
+// d is a multiple of 8; else the last chunk is read and written an element at a time.
 #pragma once
 
-#include "common.hpp"
+#include "anywhere.hpp"
 #include "layer.hpp"
 
 namespace bdgdn {
 
 constexpr int kActSilu = 1, kActSigmoid = 2;
 
-// The element of place i of chunk c of this lane.
-template <bool WIDE, int LANES> __device__ __forceinline__ int element(int c, int i, int lane)
-{
-    return WIDE ? (c * LANES + lane) * 8 + i : (c * 8 + i) * LANES + lane;
-}
+// The first element of chunk c of this lane.
+template <int LANES> __device__ __forceinline__ int element(int c, int lane) { return (c * LANES + lane) * 8; }
 
-__device__ __forceinline__ void load8(float (&v)[8], const __bf16 *p)
-{
-    const u32x4 w = *reinterpret_cast<const u32x4 *>(p);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(w[i] << 16);
-        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-}
-__device__ __forceinline__ void load8(float (&v)[8], const float *p)
-{
-    const f32x4 a = *reinterpret_cast<const f32x4 *>(p), b = *reinterpret_cast<const f32x4 *>(p + 4);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        v[i] = a[i];
-        v[4 + i] = b[i];
-    }
-}
-__device__ __forceinline__ void store8(__bf16 *p, const float (&v)[8])
-{
-    bf16x8 w;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = (__bf16)v[i];
-    *reinterpret_cast<bf16x8 *>(p) = w;
-}
-__device__ __forceinline__ void store8(float *p, const float (&v)[8])
-{
-    *reinterpret_cast<f32x4 *>(p) = f32x4{v[0], v[1], v[2], v[3]};
-    *reinterpret_cast<f32x4 *>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
-}
-
-// Chunk c of a lane's part of a row of d elements; zeros beyond its end.
-template <bool WIDE, int LANES, typename E> __device__ __forceinline__ void load_chunk(float (&v)[8], const E *row, int c, int d, int lane)
-{
-    if constexpr (WIDE) {
-        const int e = element<WIDE, LANES>(c, 0, lane);
-        if (e < d) load8(v, row + e);
-        else
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = 0.f;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int e = element<WIDE, LANES>(c, i, lane);
-            v[i] = e < d ? to_f(row[e]) : 0.f;
-        }
-    }
-}
-template <bool WIDE, int LANES, typename E>
-__device__ __forceinline__ void store_chunk(E *row, const float (&v)[8], int c, int d, int lane)
-{
-    if constexpr (WIDE) {
-        const int e = element<WIDE, LANES>(c, 0, lane);
-        if (e < d) store8(row + e, v);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int e = element<WIDE, LANES>(c, i, lane);
-            if (e < d) row[e] = to_e<E>(v[i]);
-        }
-    }
-}
-
-// C chunks of a lane's part of a row as they lie in memory: loads that nothing waits for until get().
-template <bool WIDE, int LANES, int C, typename E> struct Ahead {
+// C chunks of a lane's part of a row of d elements as they lie in memory (zeros beyond its end): loads that
+// nothing waits for until get().
+template <bool WHOLE, int LANES, int C, typename E> struct Ahead {
     static constexpr int N = sizeof(E) / 2;   // 16-byte parts of a chunk
-    u32x4 w[WIDE ? C * N : 1];
-    E v[WIDE ? 1 : C * 8];
+    u32x4 w[C * N];
+    E v[WHOLE ? 1 : 8];                       // the elements of a last chunk that is not whole
     __device__ __forceinline__ void load(const E *row, int d, int lane)
     {
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            if constexpr (WIDE) {
-                const int e = element<WIDE, LANES>(c, 0, lane);
+            const int e = element<LANES>(c, lane);
 #pragma unroll
-                for (int i = 0; i < N; ++i) w[c * N + i] = e < d ? reinterpret_cast<const u32x4 *>(row + e)[i] : u32x4{0, 0, 0, 0};
-            } else {
+            for (int i = 0; i < N; ++i)
+                w[c * N + i] = (WHOLE ? e : e + 7) < d ? reinterpret_cast<const typename AnyPlace<E>::type *>(row + e)[i] : u32x4{0, 0, 0, 0};
+        }
+        if constexpr (!WHOLE) {
+            const int e = last(d, lane);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int e = element<WIDE, LANES>(c, i, lane);
-                    v[c * 8 + i] = e < d ? row[e] : to_e<E>(0.f);
-                }
-            }
+            for (int i = 0; i < 8; ++i) v[i] = e + i < d ? row[e + i] : to_e<E>(0.f);
         }
     }
-    __device__ __forceinline__ void get(float (&to)[C][8]) const
+    // The first element of this lane's chunk that is not whole, d if it has none.
+    static __device__ __forceinline__ int last(int d, int lane)
+    {
+        const int chunk = d >> 3;
+        return (d & 7) && chunk % LANES == lane ? chunk * 8 : d;
+    }
+    __device__ __forceinline__ void get(float (&to)[C][8], int d, int lane) const
     {
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                if constexpr (!WIDE) to[c][i] = to_f(v[c * 8 + i]);
-                else if constexpr (N == 1) to[c][i] = __uint_as_float(i & 1 ? w[c][i >> 1] & 0xffff0000u : w[c][i >> 1] << 16);
+                if constexpr (N == 1) to[c][i] = __uint_as_float(i & 1 ? w[c][i >> 1] & 0xffff0000u : w[c][i >> 1] << 16);
                 else to[c][i] = __uint_as_float(w[c * N + (i >> 2)][i & 3]);
+                if (!WHOLE && element<LANES>(c, lane) + 7 >= d) to[c][i] = element<LANES>(c, lane) < d ? to_f(v[i]) : 0.f;
             }
     }
 };
 
-// All chunks.
-template <bool WIDE, int LANES, int C, typename E> __device__ __forceinline__ void load_row(float (&v)[C][8], const E *row, int d, int lane)
+// Chunk c of a lane's part of a row of d elements.
+template <bool WHOLE, int LANES, typename E> __device__ __forceinline__ void load_chunk(float (&v)[8], const E *row, int c, int d, int lane)
 {
+    const int e = element<LANES>(c, lane);
+    if ((WHOLE ? e : e + 7) < d) {
+        load8(v, row + e);
+    } else {
 #pragma unroll
-    for (int c = 0; c < C; ++c) load_chunk<WIDE, LANES>(v[c], row, c, d, lane);
+        for (int i = 0; i < 8; ++i) v[i] = !WHOLE && e + i < d ? to_f(row[e + i]) : 0.f;
+    }
 }
-template <bool WIDE, int LANES, int C, typename E> __device__ __forceinline__ void store_row(E *row, const float (&v)[C][8], int d, int lane)
+template <bool WHOLE, int LANES, typename E>
+__device__ __forceinline__ void store_chunk(E *row, const float (&v)[8], int c, int d, int lane)
+{
+    const int e = element<LANES>(c, lane);
+    if (e + 8 <= d) {
+        store8(row + e, v);
+    } else if (!WHOLE) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (e + i < d) row[e + i] = to_e<E>(v[i]);
+    }
+}
+
+// All chunks.
+template <bool WHOLE, int LANES, int C, typename E> __device__ __forceinline__ void load_row(float (&v)[C][8], const E *row, int d, int lane)
 {
 #pragma unroll
-    for (int c = 0; c < C; ++c) store_chunk<WIDE, LANES>(row, v[c], c, d, lane);
+    for (int c = 0; c < C; ++c) load_chunk<WHOLE, LANES>(v[c], row, c, d, lane);
+}
+template <bool WHOLE, int LANES, int C, typename E> __device__ __forceinline__ void store_row(E *row, const float (&v)[C][8], int d, int lane)
+{
+#pragma unroll
+    for (int c = 0; c < C; ++c) store_chunk<WHOLE, LANES>(row, v[c], c, d, lane);
 }
 
 // 1 / (1 + exp(-z)); a large -z gives exp = inf and the result 0.

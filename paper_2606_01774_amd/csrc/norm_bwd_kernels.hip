@@ -18,10 +18,10 @@ constexpr int kThreads = 512;
 constexpr int kMostGroups = 256;   // a workgroup to a compute unit
 
 // A lane's parts of the five rows that a row's gradients come from.
-template <typename X, typename R, typename Y, int LANES, int C, bool WIDE> struct BwdRows {
-    Ahead<WIDE, LANES, C, X> x;
-    Ahead<WIDE, LANES, C, Y> z, dy;
-    Ahead<WIDE, LANES, C, R> sum_r, g;
+template <typename X, typename R, typename Y, int LANES, int C, bool WHOLE> struct BwdRows {
+    Ahead<WHOLE, LANES, C, X> x;
+    Ahead<WHOLE, LANES, C, Y> z, dy;
+    Ahead<WHOLE, LANES, C, R> sum_r, g;
     __device__ __forceinline__ void load(const NormArgs &a, unsigned row, int lane)
     {
         const int d = row < (unsigned)a.rows ? a.d : 0;
@@ -34,7 +34,7 @@ template <typename X, typename R, typename Y, int LANES, int C, bool WIDE> struc
     }
 };
 
-template <typename X, typename R, typename Y, int LANES, int C, bool WIDE>
+template <typename X, typename R, typename Y, int LANES, int C, bool WHOLE>
 __global__ void __launch_bounds__(kThreads) bdgdn_norm_bwd_kernel(NormArgs a)
 {
     // One or two chunks to a lane stay in registers, and beside one the next row's, loaded ahead; of more
@@ -50,9 +50,9 @@ __global__ void __launch_bounds__(kThreads) bdgdn_norm_bwd_kernel(NormArgs a)
     const int lane = threadIdx.x % LANES;
     float wp[H][8], wq[H][8], ls[H][8];
     auto weights = [&](int c) {
-        if (a.w_post) load_chunk<WIDE, LANES>(wp[at(c)], a.w_post, c, a.d, lane);
-        if (a.w_pre) load_chunk<WIDE, LANES>(wq[at(c)], a.w_pre, c, a.d, lane);
-        if (a.ls) load_chunk<WIDE, LANES>(ls[at(c)], a.ls, c, a.d, lane);
+        if (a.w_post) load_chunk<WHOLE, LANES>(wp[at(c)], a.w_post, c, a.d, lane);
+        if (a.w_pre) load_chunk<WHOLE, LANES>(wq[at(c)], a.w_pre, c, a.d, lane);
+        if (a.ls) load_chunk<WHOLE, LANES>(ls[at(c)], a.ls, c, a.d, lane);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             if (!a.w_post) wp[at(c)][i] = 1.f;
@@ -70,7 +70,7 @@ __global__ void __launch_bounds__(kThreads) bdgdn_norm_bwd_kernel(NormArgs a)
     float acc[3][C][8] = {};   // of w_post, w_pre, layer_scale
 
     const unsigned stride = gridDim.x * ROWS, mine = row_of<LANES>();
-    BwdRows<X, R, Y, LANES, H, WIDE> next;
+    BwdRows<X, R, Y, LANES, H, WHOLE> next;
     if (ONE) next.load(a, blockIdx.x * ROWS + mine, lane);
     for (unsigned row0 = blockIdx.x * ROWS; row0 < (unsigned)a.rows; row0 += stride) {
         const unsigned row = row0 + mine;
@@ -78,22 +78,22 @@ __global__ void __launch_bounds__(kThreads) bdgdn_norm_bwd_kernel(NormArgs a)
         const int d = there ? a.d : 0, ra = there ? row / (unsigned)a.inner : 0, rb = there ? row - ra * (unsigned)a.inner : 0;
         const bool joint = a.pre && a.r;
         float x[H][8], z[H][8], sum_r[H][8], dy[H][8], g[H][8], t[C][8];
-        auto read_x = [&](int c) { load_chunk<WIDE, LANES>(x[at(c)], row_at<X>(a.x, a.sx, ra, rb), c, d, lane); };
-        auto read_z = [&](int c) { load_chunk<WIDE, LANES>(z[at(c)], row_at<Y>(a.z, a.sz, ra, rb), c, d, lane); };
-        auto read_r = [&](int c) { load_chunk<WIDE, LANES>(sum_r[at(c)], row_at<R>(a.r, a.sro, ra, rb), c, d, lane); };
-        auto read_dy = [&](int c) { load_chunk<WIDE, LANES>(dy[at(c)], row_at<Y>(a.dy, a.sdy, ra, rb), c, a.dy ? d : 0, lane); };
-        auto read_g = [&](int c) { load_chunk<WIDE, LANES>(g[at(c)], row_at<R>(a.dr_out, a.sdro, ra, rb), c, a.dr_out ? d : 0, lane); };
+        auto read_x = [&](int c) { load_chunk<WHOLE, LANES>(x[at(c)], row_at<X>(a.x, a.sx, ra, rb), c, d, lane); };
+        auto read_z = [&](int c) { load_chunk<WHOLE, LANES>(z[at(c)], row_at<Y>(a.z, a.sz, ra, rb), c, d, lane); };
+        auto read_r = [&](int c) { load_chunk<WHOLE, LANES>(sum_r[at(c)], row_at<R>(a.r, a.sro, ra, rb), c, d, lane); };
+        auto read_dy = [&](int c) { load_chunk<WHOLE, LANES>(dy[at(c)], row_at<Y>(a.dy, a.sdy, ra, rb), c, a.dy ? d : 0, lane); };
+        auto read_g = [&](int c) { load_chunk<WHOLE, LANES>(g[at(c)], row_at<R>(a.dr_out, a.sdro, ra, rb), c, a.dr_out ? d : 0, lane); };
         if (HOLD) {
             if (!ONE) {
                 next.load(a, row, lane);
 #pragma unroll
                 for (int c = 0; c < C; ++c) weights(c);
             }
-            next.x.get(x);
-            next.dy.get(dy);
-            next.g.get(g);
-            if (a.z) next.z.get(z);
-            if (joint) next.sum_r.get(sum_r);
+            next.x.get(x, d, lane);
+            next.dy.get(dy, d, lane);
+            next.g.get(g, d, lane);
+            if (a.z) next.z.get(z, d, lane);
+            if (joint) next.sum_r.get(sum_r, d, lane);
             if (ONE) next.load(a, row + stride, lane);
         }
         float s1 = 1.f, s2 = 1.f, mean_t = 0.f;
@@ -187,8 +187,8 @@ __global__ void __launch_bounds__(kThreads) bdgdn_norm_bwd_kernel(NormArgs a)
                 t[c][i] = a.post ? dn * wp[at(c)][i] : dn;
                 sum[0] = fmaf(t[c][i], xh, sum[0]);
             }
-            if (a.dr) store_chunk<WIDE, LANES>(row_at<R>(a.dr, a.sdr, ra, rb), g[at(c)], c, d, lane);
-            if (a.dz) store_chunk<WIDE, LANES>(row_at<Y>(a.dz, a.sdz, ra, rb), z[at(c)], c, d, lane);
+            if (a.dr) store_chunk<WHOLE, LANES>(row_at<R>(a.dr, a.sdr, ra, rb), g[at(c)], c, d, lane);
+            if (a.dz) store_chunk<WHOLE, LANES>(row_at<Y>(a.dz, a.sdz, ra, rb), z[at(c)], c, d, lane);
         }
         if (!a.dx) continue;
         if (a.post) {
@@ -205,7 +205,7 @@ __global__ void __launch_bounds__(kThreads) bdgdn_norm_bwd_kernel(NormArgs a)
                 for (int i = 0; i < 8; ++i) t[c][i] = s1 * (t[c][i] - x[at(c)][i] * mean);
             }
         }
-        store_row<WIDE, LANES>(row_at<X>(a.dx, a.sdx, ra, rb), t, d, lane);
+        store_row<WHOLE, LANES>(row_at<X>(a.dx, a.sdx, ra, rb), t, d, lane);
     }
 
     // the workgroup's sums
@@ -214,7 +214,7 @@ __global__ void __launch_bounds__(kThreads) bdgdn_norm_bwd_kernel(NormArgs a)
         if (!a.dw[k]) continue;
         float *part = a.part + ((long)blockIdx.x * 3 + k) * a.d;
         if constexpr (UNITS == 1) {
-            store_row<WIDE, LANES>(part, acc[k], a.d, lane);
+            store_row<WHOLE, LANES>(part, acc[k], a.d, lane);
         } else {
             static_assert(C == 1, "several rows to a workgroup have one chunk to a lane");
             const int unit = LANES < 64 ? threadIdx.x >> 6 : threadIdx.x / LANES;
@@ -224,7 +224,7 @@ __global__ void __launch_bounds__(kThreads) bdgdn_norm_bwd_kernel(NormArgs a)
                 float v = acc[k][0][i];
 #pragma unroll
                 for (int o = LANES; o < 64; o <<= 1) v += __shfl_xor(v, o);
-                if (LANES >= 64 || (threadIdx.x & 63) < LANES) meet[unit * LANES * 8 + element<WIDE, LANES>(0, i, lane)] = v;
+                if (LANES >= 64 || (threadIdx.x & 63) < LANES) meet[unit * LANES * 8 + element<LANES>(0, lane) + i] = v;
             }
             __syncthreads();
             for (int e = threadIdx.x; e < a.d; e += kThreads) {
@@ -258,7 +258,7 @@ __global__ void __launch_bounds__(1024) bdgdn_norm_weights_kernel(NormArgs a)
 
 template <typename X, typename R, typename Y, int LANES, int C> void launch(const NormArgs &a, hipStream_t s)
 {
-    if (a.vec) bdgdn_norm_bwd_kernel<X, R, Y, LANES, C, true><<<a.groups, kThreads, 0, s>>>(a);
+    if (a.d % 8 == 0) bdgdn_norm_bwd_kernel<X, R, Y, LANES, C, true><<<a.groups, kThreads, 0, s>>>(a);
     else bdgdn_norm_bwd_kernel<X, R, Y, LANES, C, false><<<a.groups, kThreads, 0, s>>>(a);
 }
 

@@ -6,29 +6,50 @@ namespace bdgdn {
 
 namespace {
 
-constexpr unsigned kMostGroups = 1u << 21;   // (a launch has 2^32 threads)
+// Threads of a workgroup whose rows have LANES lanes, and of a compute unit, which keeps them for many rows
+// (so the weights are read once, and the next row while this one is worked on).
+constexpr int threads_of(int lanes) { return lanes < 256 ? 256 : lanes; }
+constexpr int kPerUnit = 1024;
 
-template <typename X, typename R, typename Y, int LANES, int C, bool WIDE>
-__global__ void __launch_bounds__(LANES > 256 ? LANES : 256) bdgdn_norm_fwd_kernel(NormArgs a)
+template <typename X, typename R, typename Y, int LANES, int C, bool WHOLE> struct FwdRows {
+    Ahead<WHOLE, LANES, C, X> x;
+    Ahead<WHOLE, LANES, C, Y> z;
+    Ahead<WHOLE, LANES, C, R> r;
+    __device__ __forceinline__ void load(const NormArgs &a, unsigned row, int lane)
+    {
+        const int d = row < (unsigned)a.rows ? a.d : 0;
+        const int ra = d ? row / (unsigned)a.inner : 0, rb = d ? row - ra * (unsigned)a.inner : 0;
+        x.load(row_at<X>(a.x, a.sx, ra, rb), d, lane);
+        if (a.z) z.load(row_at<Y>(a.z, a.sz, ra, rb), d, lane);
+        if (a.r) r.load(row_at<R>(a.r, a.sr, ra, rb), d, lane);
+    }
+};
+
+template <typename X, typename R, typename Y, int LANES, int C, bool WHOLE>
+__global__ void __launch_bounds__(threads_of(LANES)) bdgdn_norm_fwd_kernel(NormArgs a)
 {
-    constexpr int THREADS = LANES > 256 ? LANES : 256;
+    constexpr int THREADS = threads_of(LANES), ROWS = THREADS / LANES;
+    constexpr bool AHEAD = C == 1;   // the next row loaded ahead
     __shared__ float lds[2 * (THREADS / 64)];
     RowSum<LANES, THREADS, 1> row_sum(lds);
     const int lane = threadIdx.x % LANES;
-    for (unsigned row0 = blockIdx.x * (THREADS / LANES); row0 < (unsigned)a.rows; row0 += gridDim.x * (THREADS / LANES)) {
-        const unsigned row = row0 + row_of<LANES>();
+    const unsigned stride = gridDim.x * ROWS, mine = row_of<LANES>();
+    FwdRows<X, R, Y, LANES, C, WHOLE> next;
+    next.load(a, blockIdx.x * ROWS + mine, lane);
+    float w_post[C][8], w_pre[C][8], ls[C][8];
+    if (a.w_post) load_row<WHOLE, LANES>(w_post, a.w_post, a.d, lane);
+    if (a.ls) load_row<WHOLE, LANES>(ls, a.ls, a.d, lane);
+    if (a.w_pre) load_row<WHOLE, LANES>(w_pre, a.w_pre, a.d, lane);
+    for (unsigned row0 = blockIdx.x * ROWS; row0 < (unsigned)a.rows; row0 += stride) {
+        const unsigned row = row0 + mine;
         const bool there = row < (unsigned)a.rows;   // (sums meet at barriers)
         const int d = there ? a.d : 0, ra = there ? row / (unsigned)a.inner : 0, rb = there ? row - ra * (unsigned)a.inner : 0;
         float x[C][8], z[C][8], r[C][8];
-        Ahead<WIDE, LANES, C, X> ax;
-        Ahead<WIDE, LANES, C, Y> az;
-        Ahead<WIDE, LANES, C, R> ar;
-        ax.load(row_at<X>(a.x, a.sx, ra, rb), d, lane);
-        if (a.z) az.load(row_at<Y>(a.z, a.sz, ra, rb), d, lane);
-        if (a.r) ar.load(row_at<R>(a.r, a.sr, ra, rb), d, lane);
-        ax.get(x);
-        if (a.z) az.get(z);
-        if (a.r) ar.get(r);
+        next.x.get(x, d, lane);
+        if (a.z) next.z.get(z, d, lane);
+        if (a.r) next.r.get(r, d, lane);
+        if (AHEAD) next.load(a, row + stride, lane);
+        float s1 = 1.f, s2 = 1.f;
         if (a.post) {
             float sum[1] = {0.f};
 #pragma unroll
@@ -36,60 +57,46 @@ __global__ void __launch_bounds__(LANES > 256 ? LANES : 256) bdgdn_norm_fwd_kern
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sum[0] = fmaf(x[c][i], x[c][i], sum[0]);
             row_sum(sum);
-            const float s1 = 1.f / sqrtf(fmaf(sum[0], a.inv_d, a.eps));
-            float w[C][8];
-            if (a.w_post) load_row<WIDE, LANES>(w, a.w_post, d, lane);
-#pragma unroll
-            for (int c = 0; c < C; ++c)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[c][i] *= a.w_post ? s1 * w[c][i] : s1;
+            s1 = 1.f / sqrtf(fmaf(sum[0], a.inv_d, a.eps));
         }
-        if (a.z) {
+        float sum[1] = {0.f};
 #pragma unroll
-            for (int c = 0; c < C; ++c)
+        for (int c = 0; c < C; ++c)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < 8; ++i) {
+                float u = a.post ? x[c][i] * s1 : x[c][i];
+                if (a.w_post) u *= w_post[c][i];
+                if (a.z) {
                     const float g = a.act ? sigmoid(z[c][i]) : z[c][i];
-                    x[c][i] *= a.act == kActSilu ? z[c][i] * g : g;
+                    u *= a.act == kActSilu ? z[c][i] * g : g;
                 }
+                u *= a.scale;
+                if (a.ls) u *= ls[c][i];
+                if (a.r) u += r[c][i];
+                x[c][i] = u;
+                sum[0] = fmaf(u, u, sum[0]);
+            }
+        if (a.r_out) store_row<WHOLE, LANES>(row_at<R>(a.r_out, a.sro, ra, rb), x, d, lane);
+        if (a.y) {
+            if (a.pre) {
+                row_sum(sum);
+                s2 = 1.f / sqrtf(fmaf(sum[0], a.inv_d, a.eps));
+#pragma unroll
+                for (int c = 0; c < C; ++c)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[c][i] *= a.w_pre ? s2 * w_pre[c][i] : s2;
+            }
+            store_row<WHOLE, LANES>(row_at<Y>(a.y, a.sy, ra, rb), x, d, lane);
         }
-        {
-            float w[C][8];
-            if (a.ls) load_row<WIDE, LANES>(w, a.ls, d, lane);
-#pragma unroll
-            for (int c = 0; c < C; ++c)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    x[c][i] *= a.ls ? a.scale * w[c][i] : a.scale;
-                    if (a.r) x[c][i] += r[c][i];
-                }
-        }
-        if (a.r_out) store_row<WIDE, LANES>(row_at<R>(a.r_out, a.sro, ra, rb), x, d, lane);
-        if (!a.y) continue;
-        if (a.pre) {
-            float sum[1] = {0.f};
-#pragma unroll
-            for (int c = 0; c < C; ++c)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) sum[0] = fmaf(x[c][i], x[c][i], sum[0]);
-            row_sum(sum);
-            const float s2 = 1.f / sqrtf(fmaf(sum[0], a.inv_d, a.eps));
-            float w[C][8];
-            if (a.w_pre) load_row<WIDE, LANES>(w, a.w_pre, d, lane);
-#pragma unroll
-            for (int c = 0; c < C; ++c)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[c][i] *= a.w_pre ? s2 * w[c][i] : s2;
-        }
-        store_row<WIDE, LANES>(row_at<Y>(a.y, a.sy, ra, rb), x, d, lane);
+        if (!AHEAD) next.load(a, row + stride, lane);
     }
 }
 
 template <typename X, typename R, typename Y, int LANES, int C> hipError_t launch(const NormArgs &a, hipStream_t s)
 {
-    constexpr int THREADS = LANES > 256 ? LANES : 256, ROWS = THREADS / LANES;
-    const unsigned groups = ((unsigned)a.rows + ROWS - 1) / ROWS, grid = groups < kMostGroups ? groups : kMostGroups;
-    if (a.vec) bdgdn_norm_fwd_kernel<X, R, Y, LANES, C, true><<<grid, THREADS, 0, s>>>(a);
+    constexpr int THREADS = threads_of(LANES), ROWS = THREADS / LANES, MOST = 256 * kPerUnit / THREADS;
+    const unsigned groups = ((unsigned)a.rows + ROWS - 1) / ROWS, grid = groups < MOST ? groups : MOST;
+    if (a.d % 8 == 0) bdgdn_norm_fwd_kernel<X, R, Y, LANES, C, true><<<grid, THREADS, 0, s>>>(a);
     else bdgdn_norm_fwd_kernel<X, R, Y, LANES, C, false><<<grid, THREADS, 0, s>>>(a);
     return hipGetLastError();
 }
@@ -98,8 +105,9 @@ template <typename X, typename R, typename Y> hipError_t sized(const NormArgs &a
 {
     if (a.d <= 128) return launch<X, R, Y, 16, 1>(a, s);
     if (a.d <= 512) return launch<X, R, Y, 64, 1>(a, s);
+    if (a.d <= 1024) return launch<X, R, Y, 128, 1>(a, s);
     if (a.d <= 2048) return launch<X, R, Y, 256, 1>(a, s);
-    if (a.d <= 4096) return launch<X, R, Y, 256, 2>(a, s);
+    if (a.d <= 4096) return launch<X, R, Y, 512, 1>(a, s);
     if (a.d <= 8192) return launch<X, R, Y, 1024, 1>(a, s);
     return launch<X, R, Y, 1024, 2>(a, s);
 }

@@ -5,7 +5,7 @@
 // p F modulo 2^64 is one integer product and exact, so far positions lose nothing.  cos and
 // sin of a head's pairs are the same in every head: a thread computes those of its pairs once
 // and takes them through several heads.
-#include "common.hpp"
+#include "anywhere.hpp"
 #include "layer.hpp"
 
 namespace bdgdn {
@@ -30,46 +30,44 @@ __device__ __forceinline__ void turn(uint64_t w, float &c, float &s)
     s = quarter & 2 ? -b : b;
 }
 
-// CH consecutive elements, 16 bytes of them at once.
-template <typename E, int CH> struct Chunk {
+// 16 bytes of consecutive elements, of which the first n are there.
+template <typename E> struct Chunk {
+    static constexpr int CH = 16 / sizeof(E);
     E e[CH];
-    template <int N = CH> __device__ __forceinline__ void load(const unsigned char *p)
+    template <bool RAGGED> __device__ __forceinline__ void load(const unsigned char *p, int n)
     {
-        if constexpr (N * sizeof(E) == 16) {
-            const u32x4 w = *reinterpret_cast<const u32x4 *>(p);
+        if (!RAGGED || n >= CH) {
+            const u32x4 w = *reinterpret_cast<const typename AnyPlace<E>::type *>(p);
             __builtin_memcpy(e, &w, 16);
         } else {
 #pragma unroll
-            for (int i = 0; i < N; ++i) e[i] = reinterpret_cast<const E *>(p)[i];
+            for (int i = 0; i < CH; ++i)
+                if (i < n) e[i] = reinterpret_cast<const E *>(p)[i];
         }
     }
-    template <int N = CH> __device__ __forceinline__ void store(unsigned char *p) const
+    template <bool RAGGED> __device__ __forceinline__ void store(unsigned char *p, int n) const
     {
-        if constexpr (N * sizeof(E) == 16) {
+        if (!RAGGED || n >= CH) {
             u32x4 w;
             __builtin_memcpy(&w, e, 16);
-            *reinterpret_cast<u32x4 *>(p) = w;
+            *reinterpret_cast<typename AnyPlace<E>::type *>(p) = w;
         } else {
 #pragma unroll
-            for (int i = 0; i < N; ++i) reinterpret_cast<E *>(p)[i] = e[i];
+            for (int i = 0; i < CH; ++i)
+                if (i < n) reinterpret_cast<E *>(p)[i] = e[i];
         }
     }
 };
 
-// Elements that stay, to a piece.
-template <typename E, int CH> constexpr int staying() { return CH * sizeof(E) == 16 ? CH : 1; }
-
-// A piece of a head: HALF: CH elements and their partners; PAIRS: CH elements, CH / 2 pairs; behind
-// the rotated ones some elements that stay.
-template <typename E, bool PAIRS, int CH> __global__ void __launch_bounds__(kThreads) bdgdn_rope_kernel(RopeArgs a)
+// A piece of a head is two chunks: HALF: elements and their partners; PAIRS, and behind the rotated
+// elements those that stay: neighbours.  RAGGED: some chunks are not whole.
+template <typename E, bool PAIRS, bool RAGGED> __global__ void __launch_bounds__(kThreads) bdgdn_rope_kernel(RopeArgs a)
 {
-    constexpr int P = PAIRS ? CH / 2 : CH, S = staying<E, CH>();   // pairs of a piece
-    constexpr int U = 2;                                           // heads in flight
+    constexpr int CH = Chunk<E>::CH, U = 2;   // pairs of a piece; heads in flight
     const int row_l = threadIdx.x >> (a.item_log + a.sub_log);
     const int sub = (threadIdx.x >> a.item_log) & ((1 << a.sub_log) - 1);
     const int first = sub + (blockIdx.y << a.sub_log), step = gridDim.y << a.sub_log;
-    const int turned = a.rot / (PAIRS ? CH : 2 * CH);
-    const long half = (a.rot >> 1) * (long)sizeof(E);
+    const int half = a.rot >> 1;
     const unsigned rows = (unsigned)a.R * (unsigned)a.N;
     for (unsigned row = (blockIdx.x << a.row_log) + row_l; row < rows; row += gridDim.x << a.row_log) {
         const int r = row / (unsigned)a.N, n = row - r * (unsigned)a.N;
@@ -80,50 +78,55 @@ template <typename E, bool PAIRS, int CH> __global__ void __launch_bounds__(kThr
             if ((unsigned)slot < (unsigned)a.n_slots) p += max(a.len[slot], 0);
         }
         for (int item = threadIdx.x & ((1 << a.item_log) - 1); item < a.items; item += 1 << a.item_log) {
-            const bool stays = item >= turned;
-            const long e0 = (stays ? a.rot + (item - turned) * S : item * CH) * (long)sizeof(E);
-            float c[P], s[P];
+            const bool stays = item >= a.turned;
+            // the elements of the two chunks, and how many there are
+            int e0 = stays ? a.rot + (item - a.turned) * 2 * CH : PAIRS ? item * 2 * CH : item * CH;
+            int e1 = stays || PAIRS ? e0 + CH : e0 + half;
+            const int end = stays ? a.d : PAIRS ? a.rot : half;
+            if (stays && a.d - a.rot >= CH) {   // (what lies past the end is moved back: copied twice)
+                e0 = min(e0, a.d - CH);
+                e1 = min(e1, a.d - CH);
+            }
+            const int n0 = end - e0, n1 = stays ? end - e1 : PAIRS ? n0 - CH : n0;
+            float c[CH], s[CH];
             if (!stays) {
 #pragma unroll
-                for (int i = 0; i < P; ++i) {
-                    turn((uint64_t)p * a.turns[item * P + i], c[i], s[i]);
+                for (int i = 0; i < CH; ++i) {
+                    const int pair = item * CH + i;
+                    turn((uint64_t)p * a.turns[RAGGED ? min(pair, half - 1) : pair], c[i], s[i]);
                     c[i] *= a.scale;
                     s[i] *= a.sine;
                 }
             }
             for (int h0 = first; h0 < a.h; h0 += U * step) {
-                Chunk<E, CH> lo[U], hi[U];
+                Chunk<E> lo[U], hi[U];
                 unsigned char *to[U];
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     const int h = h0 + u * step;
                     if (h >= a.h) break;
                     const int w = h >= a.h_q, hh = w ? h - a.h_q : h;
-                    const unsigned char *from = a.x[w] + r * a.xs[w][0] + n * a.xs[w][1] + hh * a.xs[w][2] + e0;
-                    to[u] = a.y[w] + r * a.ys[w][0] + n * a.ys[w][1] + hh * a.ys[w][2] + e0;
-                    if (stays) {
-                        lo[u].template load<S>(from);
-                    } else {
-                        lo[u].load(from);
-                        if (!PAIRS) hi[u].load(from + half);
-                    }
+                    const unsigned char *from = a.x[w] + r * a.xs[w][0] + n * a.xs[w][1] + hh * a.xs[w][2];
+                    to[u] = a.y[w] + r * a.ys[w][0] + n * a.ys[w][1] + hh * a.ys[w][2];
+                    lo[u].template load<RAGGED>(from + e0 * (int)sizeof(E), n0);
+                    if (!RAGGED || n1 > 0) hi[u].template load<RAGGED>(from + e1 * (int)sizeof(E), n1);
                 }
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     if (h0 + u * step >= a.h) break;
-                    if (stays) {
-                        lo[u].template store<S>(to[u]);
-                        continue;
-                    }
+                    if (!stays) {
 #pragma unroll
-                    for (int i = 0; i < P; ++i) {
-                        E &ea = lo[u].e[PAIRS ? 2 * i : i], &eb = PAIRS ? lo[u].e[PAIRS ? 2 * i + 1 : 0] : hi[u].e[i];
-                        const float x = to_f(ea), y = to_f(eb);
-                        ea = to_e<E>(x * c[i] - y * s[i]);
-                        eb = to_e<E>(x * s[i] + y * c[i]);
+                        for (int i = 0; i < CH; ++i) {
+                            // PAIRS: the first half of a piece's pairs lies in lo, the second in hi
+                            E &ea = !PAIRS ? lo[u].e[i] : i < CH / 2 ? lo[u].e[2 * i % CH] : hi[u].e[2 * i % CH];
+                            E &eb = !PAIRS ? hi[u].e[i] : i < CH / 2 ? lo[u].e[(2 * i + 1) % CH] : hi[u].e[(2 * i + 1) % CH];
+                            const float x = to_f(ea), y = to_f(eb);
+                            ea = to_e<E>(x * c[i] - y * s[i]);
+                            eb = to_e<E>(x * s[i] + y * c[i]);
+                        }
                     }
-                    lo[u].store(to[u]);
-                    if (!PAIRS) hi[u].store(to[u] + half);
+                    lo[u].template store<RAGGED>(to[u] + e0 * (int)sizeof(E), n0);
+                    if (!RAGGED || n1 > 0) hi[u].template store<RAGGED>(to[u] + e1 * (int)sizeof(E), n1);
                 }
             }
         }
@@ -137,35 +140,36 @@ int log_up(int x)
     return l;
 }
 
-template <typename E, bool PAIRS, int CH> hipError_t launch(RopeArgs &a, hipStream_t s)
+template <typename E, bool PAIRS> hipError_t launch(RopeArgs &a, hipStream_t s)
 {
-    const int piece = PAIRS ? CH : 2 * CH;
-    a.items = a.rot / piece + (a.in_place ? 0 : (a.d - a.rot) / staying<E, CH>());
+    constexpr int CH = Chunk<E>::CH;
+    const int half = a.rot / 2, stay = a.in_place ? 0 : a.d - a.rot;
+    a.turned = (half + CH - 1) / CH;   // (of either layout: a piece has CH pairs)
+    a.items = a.turned + (stay + 2 * CH - 1) / (2 * CH);
     a.item_log = log_up(a.items);
     if (a.item_log > 8) a.item_log = 8;
     const unsigned rows = (unsigned)a.R * (unsigned)a.N;
-    // head-lanes: all heads at once, fewer as long as the chip stays full
+    // head-lanes: all heads at once, fewer as long as there are four lanes to every place the chip has
+    // for one.  q and k of 16384 tokens (40 heads of 128, bf16): 84 us with one, 69 with four, 72 with eight,
+    // 93 with all heads at once
     int heads_log = log_up(a.h);
-    while (heads_log > 0 && ((long)rows << (a.item_log + heads_log - 1)) >= 524288) --heads_log;
+    while (heads_log > 0 && ((long)rows << (a.item_log + heads_log - 1)) >= 4 * 524288) --heads_log;
     a.sub_log = heads_log < 8 - a.item_log ? heads_log : 8 - a.item_log;
     a.row_log = 8 - a.item_log - a.sub_log;
     const unsigned blocks = (rows + (1u << a.row_log) - 1) >> a.row_log;
     const unsigned parts = 1u << (heads_log - a.sub_log);
     const dim3 grid(blocks * (long)parts < kMostBlocks ? blocks : kMostBlocks / parts, parts);
-    bdgdn_rope_kernel<E, PAIRS, CH><<<grid, kThreads, 0, s>>>(a);
+    if (half % CH || (stay && stay < CH)) bdgdn_rope_kernel<E, PAIRS, true><<<grid, kThreads, 0, s>>>(a);
+    else bdgdn_rope_kernel<E, PAIRS, false><<<grid, kThreads, 0, s>>>(a);
     return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_rope(bool bf16, bool pairs, bool wide, RopeArgs &a, hipStream_t s)
+hipError_t launch_rope(bool bf16, bool pairs, RopeArgs &a, hipStream_t s)
 {
-    if (bf16) {
-        if (pairs) return wide ? launch<__bf16, true, 8>(a, s) : launch<__bf16, true, 2>(a, s);
-        return wide ? launch<__bf16, false, 8>(a, s) : launch<__bf16, false, 1>(a, s);
-    }
-    if (pairs) return wide ? launch<float, true, 4>(a, s) : launch<float, true, 2>(a, s);
-    return wide ? launch<float, false, 4>(a, s) : launch<float, false, 1>(a, s);
+    if (bf16) return pairs ? launch<__bf16, true>(a, s) : launch<__bf16, false>(a, s);
+    return pairs ? launch<float, true>(a, s) : launch<float, false>(a, s);
 }
 
 }  // namespace bdgdn
