@@ -12,6 +12,7 @@ typedef u32x4 u32x4_e4 __attribute__((aligned(4)));
 template <typename E> struct AnyPlace;
 template <> struct AnyPlace<__bf16> { typedef u32x4_e2 type; };
 template <> struct AnyPlace<float> { typedef u32x4_e4 type; };
+template <> struct AnyPlace<int32_t> { typedef u32x4_e4 type; };
 
 // Eight elements.
 __device__ __forceinline__ void load8(float (&v)[8], const __bf16 *p)
