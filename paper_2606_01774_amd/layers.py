@@ -16,7 +16,7 @@ import math
 
 import torch
 
-from . import _DT, _F32, _I32, _Tensor, _check, _p, _stream, load_library
+from . import _DT, _F32, _I32, _Tensor, _check, _p, _raw_stream, _stream, load_library
 from .rounds import _empty, _scratch, _vector
 
 BDGDN_ROPE_HALF = 0
@@ -33,6 +33,7 @@ _SCALINGS = {None: BDGDN_ROPE_PLAIN, "none": BDGDN_ROPE_PLAIN, "linear": BDGDN_R
              "parts": BDGDN_ROPE_PARTS}
 _ACTS = {None: 0, "none": 0, "silu": 1, "sigmoid": BDGDN_ACT_SIGMOID}
 _I64, _I8 = torch.int64, torch.int8
+_get_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _fields(ctype, *names):
@@ -95,16 +96,23 @@ def bind(lib):
 
 
 # ------------------------------------------------------------------ marshalling
-def _here(stream, **tensors):
-    """The tensors are on the device that the call runs on."""
-    at = torch.cuda.current_device() if stream is None else stream.device_index
-    for name, t in tensors.items():
-        if t is None:
-            continue
-        if not isinstance(t, _Tensor) or not t.is_cuda:
-            raise ValueError(f"{name} must be a device tensor")
-        if t.get_device() != at:
+def _here(stream, names, *tensors):
+    """The tensors are on the device that the call runs on; its raw stream.  (A small call costs what its
+    marshalling does: what is usual is one comparison a tensor.)"""
+    at = _current_device() if stream is None else stream.device_index
+    if tensors[0] is None:
+        raise ValueError(f"{names.split()[0]} must be a device tensor")
+    for t in tensors:
+        if t is not None and not (isinstance(t, _Tensor) and t.is_cuda and t.get_device() == at):
+            name = names.split()[[i for i, u in enumerate(tensors) if u is t][0]]
+            if not isinstance(t, _Tensor) or not t.is_cuda:
+                raise ValueError(f"{name} must be a device tensor")
             raise ValueError(f"{name} is on device {t.get_device()}, the call runs on device {at}")
+    return _stream(stream) if stream is not None or _raw_stream is None else _raw_stream(at)
+
+
+def _current_device():
+    return _get_device() if torch.cuda.is_initialized() else torch.cuda.current_device()
 
 
 def _like(t, name, shape, dtype):
@@ -158,7 +166,8 @@ def bdgdn_rope(q, turns, k=None, *, pos=None, seq_len=None, slot=None, count=Non
     inverse turns back (the gradient).  q_out and k_out may be q and k; rows n >= count[r] are left
     out.  Returns q_out, or (q_out, k_out)."""
     lib = load_library()
-    _here(stream, q=q, turns=turns, k=k, pos=pos, seq_len=seq_len, slot=slot, count=count, q_out=q_out, k_out=k_out)
+    here = _here(stream, "q turns k pos seq_len slot count q_out k_out",
+                 q, turns, k, pos, seq_len, slot, count, q_out, k_out)
     dt, shape = q.dtype, q.shape
     if k is None and k_out is not None:
         raise ValueError("k_out without k")
@@ -181,7 +190,7 @@ def bdgdn_rope(q, turns, k=None, *, pos=None, seq_len=None, slot=None, count=Non
         pk, pko = _at(k), _at(k_out)
     st = lib.bdgdn_rope(desc, q.data_ptr(), pk, _p(turns, "turns", _I64), _vector(pos, "pos", R * N),
                         _p(seq_len, "seq_len", _I32), _vector(slot, "slot", R), _vector(count, "count", R),
-                        q_out.data_ptr(), pko, _stream(stream))
+                        q_out.data_ptr(), pko, here)
     _check(st, "bdgdn_rope")
     return q_out if k_out is None else (q_out, k_out)
 
@@ -224,7 +233,8 @@ def bdgdn_norm_fwd(x, *, z=None, r=None, w_post=None, w_pre=None, layer_scale=No
     or [tokens, heads, d]; weights [d] fp32 or None for ones; act "silu", "sigmoid" or "none".  y has
     out_dtype (z's type, or else x's).  Returns (y, r'), None for r' where there is neither r nor r_out."""
     lib = load_library()
-    _here(stream, x=x, z=z, r=r, w_post=w_post, w_pre=w_pre, layer_scale=layer_scale, r_out=r_out, y=y)
+    here = _here(stream, "x z r w_post w_pre layer_scale r_out y",
+                 x, z, r, w_post, w_pre, layer_scale, r_out, y)
     shape = x.shape
     dt = z.dtype if z is not None else y.dtype if y is not None else x.dtype if out_dtype is None else out_dtype
     if out_dtype is not None and out_dtype is not dt:
@@ -240,7 +250,7 @@ def bdgdn_norm_fwd(x, *, z=None, r=None, w_post=None, w_pre=None, layer_scale=No
         r_out = _empty(shape, rt, x.device, stream)
     st = lib.bdgdn_norm_fwd(desc, x.data_ptr(), _at(z), _at(r),
                             *_weights(shape[-1], w_post=w_post, w_pre=w_pre, layer_scale=layer_scale), _at(r_out),
-                            y.data_ptr(), _stream(stream))
+                            y.data_ptr(), here)
     _check(st, "bdgdn_norm_fwd")
     return y, r_out
 
@@ -256,8 +266,8 @@ def bdgdn_norm_bwd(x, dy, *, z=None, r_out=None, dr_out=None, w_post=None, w_pre
     None).  r_out is the forward's r', to be given where it took a residual.  Returns (dx, dz, dr,
     dw_post, dw_pre, dlayer_scale); dr where r_out or dr_out is given, the weights' where they are."""
     lib = load_library()
-    _here(stream, x=x, dy=dy, z=z, r_out=r_out, dr_out=dr_out, w_post=w_post, w_pre=w_pre, layer_scale=layer_scale, dx=dx,
-          dz=dz, dr=dr, dw_post=dw_post, dw_pre=dw_pre, dlayer_scale=dlayer_scale, workspace=workspace)
+    here = _here(stream, "x dy z r_out dr_out w_post w_pre layer_scale dx dz dr dw_post dw_pre dlayer_scale workspace",
+                 x, dy, z, r_out, dr_out, w_post, w_pre, layer_scale, dx, dz, dr, dw_post, dw_pre, dlayer_scale, workspace)
     shape, d = x.shape, x.shape[-1]
     dt = z.dtype if z is not None else dy.dtype if dy is not None else x.dtype
     rt = r_out.dtype if r_out is not None else dr_out.dtype if dr_out is not None else dr.dtype if dr is not None else x.dtype
@@ -287,7 +297,7 @@ def bdgdn_norm_bwd(x, dy, *, z=None, r_out=None, dr_out=None, w_post=None, w_pre
                             *_weights(d, w_post=w_post, w_pre=w_pre, layer_scale=layer_scale), _at(dy), _at(dr_out),
                             dx.data_ptr(), _at(dz), _at(dr),
                             *_weights(d, dw_post=dw_post, dw_pre=dw_pre, dlayer_scale=dlayer_scale),
-                            workspace.data_ptr(), size, _stream(stream))
+                            workspace.data_ptr(), size, here)
     _check(st, "bdgdn_norm_bwd")
     return dx, dz, dr, dw_post, dw_pre, dlayer_scale
 
@@ -325,8 +335,8 @@ def bdgdn_logits(logits, *, token=None, mask=None, count=None, history=None, slo
     t % 32 of word t // 32 set where token t is allowed.  out may be logits.  Returns out (out_dtype:
     that of logits)."""
     lib = load_library()
-    _here(stream, logits=logits, token=token, mask=mask, count=count, history=history, slot=slot, repetition=repetition,
-          presence=presence, frequency=frequency, bias_token=bias_token, bias=bias, allow=allow, out=out)
+    here = _here(stream, "logits token mask count history slot repetition presence frequency bias_token bias allow out",
+                 logits, token, mask, count, history, slot, repetition, presence, frequency, bias_token, bias, allow, out)
     dt, shape = logits.dtype, logits.shape
     if out is not None:
         if out_dtype is not None and out_dtype is not out.dtype:
@@ -354,7 +364,7 @@ def bdgdn_logits(logits, *, token=None, mask=None, count=None, history=None, slo
                           _vector(mask, "mask", R * N, _I64), _vector(count, "count", R),
                           _vector(repetition, "repetition", R, _F32), _vector(presence, "presence", R, _F32),
                           _vector(frequency, "frequency", R, _F32), _vector(bias_token, "bias_token", n),
-                          _vector(bias, "bias", n, _F32), _at(allow), out.data_ptr(), _stream(stream))
+                          _vector(bias, "bias", n, _F32), _at(allow), out.data_ptr(), here)
     _check(st, "bdgdn_logits")
     return out
 
@@ -364,7 +374,8 @@ def bdgdn_history_add(history, token, *, slot=None, path=None, count=None, promp
     in order; count None: all): one more occurrence each or, with prompt, the mark of a prompt's token
     (BDGDN_HISTORY_PROMPT)."""
     lib = load_library()
-    _here(stream, history=history, token=token, slot=slot, path=path, count=count)
+    here = _here(stream, "history token slot path count",
+                 history, token, slot, path, count)
     if history.dim() != 2 or history.dtype is not _I32 or (history.shape[1] > 1 and history.stride(1) != 1):
         raise ValueError("history must be [n_slots, V] int32 with contiguous rows")
     if token.dim() != 2:
@@ -372,7 +383,7 @@ def bdgdn_history_add(history, token, *, slot=None, path=None, count=None, promp
     R, N = token.shape
     st = lib.bdgdn_history_add(R, N, history.shape[1], history.shape[0], history.stride(0), history.data_ptr(),
                                _vector(slot, "slot", R), _p(token, "token", _I32), _vector(path, "path", R * N),
-                               _vector(count, "count", R), int(bool(prompt)), _stream(stream))
+                               _vector(count, "count", R), int(bool(prompt)), here)
     _check(st, "bdgdn_history_add")
 
 
@@ -389,7 +400,8 @@ def bdgdn_quant_rows(x, *, q=None, scale=None, stream=None):
     rounded to the nearest integer.  q is int8 [rows, columns filled up with zeros to a multiple of
     128].  Returns (q, scale)."""
     lib = load_library()
-    _here(stream, x=x, q=q, scale=scale)
+    here = _here(stream, "x q scale",
+                 x, q, scale)
     if x.dim() != 2:
         raise ValueError("x must be [rows, columns]")
     rows, width = x.shape[0], (x.shape[1] + 127) // 128 * 128
@@ -402,7 +414,7 @@ def bdgdn_quant_rows(x, *, q=None, scale=None, stream=None):
     if scale is None:
         scale = _empty(rows, _F32, x.device, stream)
     desc = _quant_plan(x.shape, x.stride(), x.dtype, width, q.stride(0))
-    st = lib.bdgdn_quant_rows(desc, x.data_ptr(), q.data_ptr(), _vector(scale, "scale", rows, _F32), _stream(stream))
+    st = lib.bdgdn_quant_rows(desc, x.data_ptr(), q.data_ptr(), _vector(scale, "scale", rows, _F32), here)
     _check(st, "bdgdn_quant_rows")
     return q, scale
 
@@ -424,7 +436,8 @@ def bdgdn_quant_matmul(a, a_scale, w, w_scale, *, bias=None, out=None, out_dtype
     of 128) with scales a_scale [m] for each token and w_scale [n] for each channel: a_scale[i]
     w_scale[j] sum_k a[i, k] w[j, k] + bias[j], exact in its integer sums."""
     lib = load_library()
-    _here(stream, a=a, a_scale=a_scale, w=w, w_scale=w_scale, bias=bias, out=out, workspace=workspace)
+    here = _here(stream, "a a_scale w w_scale bias out workspace",
+                 a, a_scale, w, w_scale, bias, out, workspace)
     if a.dtype is not _I8 or w.dtype is not _I8:
         raise ValueError(f"a and w must be {_I8}")
     if out is not None:
@@ -443,6 +456,6 @@ def bdgdn_quant_matmul(a, a_scale, w, w_scale, *, bias=None, out=None, out_dtype
         size = 0
     st = lib.bdgdn_quant_matmul(desc, a.data_ptr(), _vector(a_scale, "a_scale", m, _F32), w.data_ptr(),
                                 _vector(w_scale, "w_scale", n, _F32), _vector(bias, "bias", n, _F32), out.data_ptr(),
-                                _at(workspace) if need else None, size, _stream(stream))
+                                _at(workspace) if need else None, size, here)
     _check(st, "bdgdn_quant_matmul")
     return out
