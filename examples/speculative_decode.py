@@ -8,10 +8,14 @@ drafts a chain behind each request's last token, runs the block through the laye
 (bdgdn_accept_states, bdgdn_cache_append); nothing of it waits for the host.  Prompts are forked
 several ways (bdgdn_cache_fork), a window keeps the caches short (bdgdn_cache_compact), and
 finished sequences give their pages back (bdgdn_cache_truncate).  A model without "g" layers
-can also draft trees (bdgdn_tree_mask).
+can also draft trees (bdgdn_tree_mask).  The residual and its norms are bdgdn_norm_fwd's; on request the
+attention layers turn their queries and keys by their positions (bdgdn_rope), the projections are in 8-bit
+integers (bdgdn_quant_rows, bdgdn_quant_matmul), and repeated tokens are penalised (bdgdn_logits,
+bdgdn_history_add).
 
     python examples/speculative_decode.py --prompts 8 --ways 4 --rounds 64
     python examples/speculative_decode.py --layers aa --tree 3,2,1 --temperature 0
+    python examples/speculative_decode.py --rotary 10000 --eight-bit --repetition 1.1
 """
 import argparse
 import os
@@ -47,10 +51,12 @@ def parents_of(branches):
 
 
 class Decoder:
-    """The model with the states and caches of `slots` sequences of up to max_len tokens."""
+    """The model with the states and caches of `slots` sequences of up to max_len tokens.  rotary: the
+    base of the attention layers' positions (None: they have none); eight_bit: projections in 8-bit
+    integers; penalties: (repetition, presence, frequency) of tokens that a sequence holds already."""
 
     def __init__(self, layers="gaga", vocab=512, width=256, slots=32, page=16, max_len=1024, pages=None, seed=0,
-                 device="cuda"):
+                 device="cuda", rotary=None, eight_bit=False, penalties=None):
         gen = torch.Generator().manual_seed(seed)
 
         def weight(rows, cols):
@@ -64,6 +70,13 @@ class Decoder:
         back = {"g": GDN_HEADS * GDN_DIM, "a": HEADS * DIM}
         self.w_in = [weight(width, qkv[x]) for x in layers]
         self.w_out = [weight(back[x], width) for x in layers]
+        # rows of integers with a scale for each channel
+        self.eight_bit = [[bd.bdgdn_quant_rows(w.T.contiguous()) for w in ws] for ws in (self.w_in, self.w_out)] if eight_bit else None
+        self.turns = None if rotary is None else bd.make_rope_turns(DIM, rotary, device=device)[0]
+        # tokens that a sequence has taken in (a window shortens its cache, not its positions)
+        self.taken = torch.zeros(slots, dtype=torch.int32, device=device)
+        self.penalties = penalties
+        self.history = torch.zeros(slots, vocab, dtype=torch.int32, device=device) if penalties else None
         self.drafter = self.logits(self.embed.float())   # [V, V]: after each token
         self.states = [torch.zeros(slots, GDN_HEADS, GDN_DIM, GDN_DIM, device=device) if x == "g" else None
                        for x in layers]
@@ -76,15 +89,23 @@ class Decoder:
     def logits(self, x):
         return (norm(x).to(torch.bfloat16) @ self.out).float()
 
-    def forward(self, token, slot, mask="causal", n_record=0):
+    def project(self, x, out, i):
+        """Rows [R * N, .] through the projection in front of layer i, or behind it (out 1)."""
+        if self.eight_bit is None:
+            return x @ (self.w_in, self.w_out)[out][i]
+        return bd.bdgdn_quant_matmul(*bd.bdgdn_quant_rows(x), *self.eight_bit[out][i])
+
+    def forward(self, token, slot, mask="causal", depth=None, n_record=0):
         """Logits [R, N, V] of a block of tokens behind the sequences in `slot`, the attention
         layers' new rows, and with n_record the recorded states of the "g" layers.  The "g"
-        layers' states go forward by the whole block, the caches stay as they are."""
+        layers' states go forward by the whole block, the caches stay as they are.  depth: the
+        nodes' positions behind the sequence (None: 0, 1, ...)."""
         R, N = token.shape
-        x = self.embed[token.long()].float()
+        x = self.embed[token.long()].float().view(R * N, -1)
+        z, _ = bd.bdgdn_norm_fwd(x, pre=True, out_dtype=torch.bfloat16)
         rows, recorded, a = [], [], 0
         for i, kind in enumerate(self.layers):
-            y = norm(x).to(torch.bfloat16) @ self.w_in[i]
+            y = self.project(z, 0, i).view(R, N, -1)
             if kind == "g":
                 q, k, v, rest = y.split([GDN_HEADS * GDN_DIM] * 3 + [2 * GDN_HEADS], dim=-1)
                 q, k, v = (t.reshape(R, N, GDN_HEADS, GDN_DIM) for t in (q, k, v))
@@ -102,15 +123,18 @@ class Decoder:
             else:
                 y = y.view(R, N, HEADS + 2 * KV_HEADS, DIM)   # q, k and v as parts of its rows
                 q, k, v = y.split([HEADS, KV_HEADS, KV_HEADS], dim=2)
+                if self.turns is not None:
+                    q, k = bd.bdgdn_rope(q, self.turns, k, pos=depth, seq_len=self.taken, slot=slot, q_out=q, k_out=k)
                 o, _ = bd.bdgdn_tree_attn(q, k, v, self.pools[a], self.pools[a + 1], self.tables.page_table,
                                           self.tables.seq_len, mask=mask, slot=slot)
                 rows += [k, v]
                 recorded.append(None)
                 a += 2
-            x = x + (o.reshape(R, N, -1) @ self.w_out[i]).float()
-        return self.logits(x), rows, recorded
+            z, x = bd.bdgdn_norm_fwd(self.project(o.reshape(R * N, -1), 1, i), r=x, pre=True, r_out=x)
+        return (z @ self.out).float().view(R, N, -1), rows, recorded
 
     def append(self, rows, slot, count, path=None):
+        self.taken.index_add_(0, slot.long(), count)
         if rows:
             return bd.bdgdn_cache_append(self.tables, self.pools, rows, slot, count, path=path)
         return torch.zeros_like(count)
@@ -118,6 +142,8 @@ class Decoder:
     def prefill(self, prompt, slot, block=32):
         """Takes in prompt [R, T] but its last token, which is the first round's anchor."""
         status = torch.zeros_like(slot)
+        if self.penalties:
+            bd.bdgdn_history_add(self.history, prompt[:, :-1].contiguous(), slot=slot, prompt=True)
         for t in range(0, prompt.shape[1] - 1, block):
             part = prompt[:, t:min(t + block, prompt.shape[1] - 1)]
             _, rows, _ = self.forward(part, slot)
@@ -128,6 +154,9 @@ class Decoder:
         for s in self.states:
             if s is not None:
                 s[dst.long()] = s[src.long()]
+        self.taken[dst.long()] = self.taken[src.long()]
+        if self.penalties:
+            self.history[dst.long()] = self.history[src.long()]
         return bd.bdgdn_cache_fork(self.tables, src, dst)
 
     def _draft(self, logits, temperature):
@@ -136,12 +165,19 @@ class Decoder:
         p = torch.softmax(logits / temperature, -1)
         return (p / torch.empty_like(p).exponential_()).argmax(-1)
 
-    def _verify(self, target, token, temperature, **kw):
+    def _verify(self, target, token, slot, temperature, mask=None, **kw):
         R, N, V = target.shape
+        if self.penalties:
+            repetition, presence, frequency = (torch.full((R,), float(p), device=self.device) for p in self.penalties)
+            bd.bdgdn_logits(target, token=token, mask=mask, history=self.history, slot=slot, repetition=repetition,
+                            presence=presence, frequency=frequency, out=target)
         u = torch.rand(R, N, device=self.device)
         noise = torch.empty(R, V, device=self.device).exponential_()
         T = torch.full((R,), float(temperature), device=self.device)
-        return bd.bdgdn_verify(target, token, u, noise, temperature=T, want_n_path=True, **kw)
+        out = bd.bdgdn_verify(target, token, u, noise, temperature=T, want_n_path=True, **kw)
+        if self.penalties:
+            bd.bdgdn_history_add(self.history, token, slot=slot, path=out[1], count=out[3])
+        return out
 
     def round(self, anchor, slot, drafts=7, temperature=1.0):
         """One round with a drafted chain.  Returns (tokens [R, 1 + drafts] of the block,
@@ -152,7 +188,7 @@ class Decoder:
         token = torch.stack(token, 1)
         draft = self.drafter[token[:, :-1].long()]
         target, rows, recorded = self.forward(token, slot, n_record=drafts)
-        n_accept, path, anchor, n_path = self._verify(target, token, temperature, draft=draft)
+        n_accept, path, anchor, n_path = self._verify(target, token, slot, temperature, draft=draft)
         for state, kept in zip(self.states, recorded):
             if kept is not None:
                 bd.bdgdn_accept_states(state, kept, n_accept, block=token.shape[1], slot=slot)
@@ -170,8 +206,9 @@ class Decoder:
             token.append(likely[token[p].long(), j])
         token = torch.stack(token, 1)
         parents = torch.tensor([parent] * len(slot), dtype=torch.int32, device=self.device)
-        target, rows, _ = self.forward(token, slot, mask=bd.bdgdn_tree_mask(parents))
-        n_accept, path, anchor, n_path = self._verify(target, token, temperature, parent=parents)
+        mask, depth = bd.bdgdn_tree_mask(parents, want_depth=True)
+        target, rows, _ = self.forward(token, slot, mask=mask, depth=depth)
+        n_accept, path, anchor, n_path = self._verify(target, token, slot, temperature, mask=mask, parent=parents)
         status = self.append(rows, slot, n_path, path)
         return token.gather(1, path.clamp(min=0).long()), n_accept, anchor, status
 
@@ -184,6 +221,9 @@ class Decoder:
         return bd.bdgdn_cache_compact(self.tables, self.pools, slot, keep.contiguous(), count)
 
     def finish(self, slot):
+        self.taken[slot.long()] = 0
+        if self.penalties:
+            self.history[slot.long()] = 0
         bd.bdgdn_cache_truncate(self.tables, slot)
 
 
@@ -205,7 +245,13 @@ def main():
     ap.add_argument("--tree", help="children of a node at each depth, as 3,2,1: draft trees")
     ap.add_argument("--temperature", type=float, default=1.0)
     ap.add_argument("--window", type=int, default=256, help="cached tokens kept, from twice as many on")
+    ap.add_argument("--rotary", type=float, help="base of the attention layers' rotary positions")
+    ap.add_argument("--eight-bit", action="store_true", help="projections in 8-bit integers")
+    ap.add_argument("--repetition", type=float, default=1.0)
+    ap.add_argument("--presence", type=float, default=0.0)
+    ap.add_argument("--frequency", type=float, default=0.0)
     args = ap.parse_args()
+    penalties = (args.repetition, args.presence, args.frequency)
     torch.manual_seed(0)
     R, ways = args.prompts, args.ways
     branches = [int(x) for x in args.tree.split(",")] if args.tree else []
@@ -213,7 +259,8 @@ def main():
     every = max(1, args.window // grows)            # rounds from one shortening to the next
     max_len = max(args.length, args.window) + (every + 1) * grows
     # (twice the pages: a shortened sequence's tokens move before their old pages are free)
-    model = Decoder(args.layers, slots=R * ways, max_len=max_len, pages=2 * R * ways * -(-max_len // 16))
+    model = Decoder(args.layers, slots=R * ways, max_len=max_len, pages=2 * R * ways * -(-max_len // 16),
+                    rotary=args.rotary, eight_bit=args.eight_bit, penalties=penalties if penalties != (1, 0, 0) else None)
     slot = torch.arange(R * ways, dtype=torch.int32, device=model.device)
     prompt = torch.randint(model.vocab, (R, args.length), dtype=torch.int32, device=model.device)
     anchor, status = model.prefill(prompt, slot[:R])
