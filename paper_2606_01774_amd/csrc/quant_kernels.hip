@@ -66,7 +66,7 @@ template <typename E, int LANES, int HELD> __global__ void __launch_bounds__(kQu
     look(x, min(cols, SPAN));
     top = row_top<LANES>(top, lds);
     const bool bad = top > 0x7f7fffffu;
-    const float scale = bad ? __uint_as_float(0x7fc00000u) : __uint_as_float(top) / 127.f;
+    const float scale = bad ? __uint_as_float(0x7fc00000u) : __uint_as_float(top) * (1.f / 127.f);
     if (cols && lane == 0) a.scale[row] = scale;
     int8_t *q = a.q + row * a.qs;
     for (int at = 0; at < width; at += SPAN) {

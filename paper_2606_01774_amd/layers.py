@@ -396,8 +396,8 @@ def _quant_plan(shape, s, dtype, width, q_stride):
 
 
 def bdgdn_quant_rows(x, *, q=None, scale=None, stream=None):
-    """8-bit integers and a scale for each row of x [rows, columns]: scale = max |x| / 127, q = x / scale
-    rounded to the nearest integer.  q is int8 [rows, columns filled up with zeros to a multiple of
+    """8-bit integers and a scale for each row of x [rows, columns]: scale = max |x| (1 / 127), q =
+    x / scale rounded to the nearest integer, in fp32.  q is int8 [rows, columns filled up with zeros to a multiple of
     128].  Returns (q, scale)."""
     lib = load_library()
     here = _here(stream, "x q scale",

@@ -1,7 +1,7 @@
 """bdgdn_quant_rows and bdgdn_quant_matmul.
 
-quant_rows is held to its definition bit for bit: max |x| / 127 and the quotients are single correctly
-rounded fp32 operations, which numpy's are too.  The product's integer sums are exact; a_scale w_scale,
+quant_rows is held to its definition bit for bit: the product max |x| (1 / 127) and the quotients are single
+correctly rounded fp32 operations, which numpy's are too.  The product's integer sums are exact; a_scale w_scale,
 the sum as fp32, its product with the scales and the bias's sum are rounded once each (the last two
 together): 3 x 2^-24 of |sum scales| + |bias|, and half a step of the result's type.
 """
@@ -20,7 +20,7 @@ B, F = torch.bfloat16, torch.float32
 def quantised(x):
     x = x.float().cpu().numpy()
     top = np.abs(x).max(-1, keepdims=True)
-    scale = (top / np.float32(127)).astype(np.float32)
+    scale = (top * (np.float32(1) / np.float32(127))).astype(np.float32)
     with np.errstate(all="ignore"):
         q = np.clip(np.rint(np.where(scale > 0, x / scale, 0)), -127, 127)
     return torch.from_numpy(q.astype(np.int8)), torch.from_numpy(scale[:, 0])
