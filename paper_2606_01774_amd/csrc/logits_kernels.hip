@@ -19,6 +19,34 @@ constexpr int kTile = kThreads * kPer;
 constexpr int32_t kPrompt = 1 << 30;
 constexpr uint32_t kNode = 0x80000000u;       // a node of the block carries the token
 
+// A lane's logits of one row, and its bits of the grammar's words, as they lie in memory.
+template <typename X> struct Row {
+    u32x4 w[sizeof(X) / 2];
+    uint32_t bits;
+    __device__ __forceinline__ void load(const X *x, const uint8_t *allow, int left)
+    {
+        if (left <= 0) return;
+        if (left >= kPer) {
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(X) / 2; ++i) w[i] = reinterpret_cast<const typename AnyPlace<X>::type *>(x)[i];
+        } else {
+            X v[kPer];
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) v[i] = i < left ? x[i] : to_e<X>(0.f);
+            __builtin_memcpy(w, v, sizeof(w));
+        }
+        bits = allow ? *allow : 0xffu;
+    }
+    __device__ __forceinline__ void get(float (&l)[kPer]) const
+    {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            if constexpr (sizeof(X) == 2) l[i] = __uint_as_float(i & 1 ? w[0][i >> 1] & 0xffff0000u : w[0][i >> 1] << 16);
+            else l[i] = __uint_as_float(w[i >> 2][i & 3]);
+        }
+    }
+};
+
 template <typename X, typename Y> __global__ void __launch_bounds__(kThreads) bdgdn_logits_kernel(LogitsArgs a)
 {
     __shared__ uint32_t s_mark[kTile];        // entry of bias + 1, kNode
@@ -36,16 +64,34 @@ template <typename X, typename Y> __global__ void __launch_bounds__(kThreads) bd
     const bool with_history = penal && a.history && (unsigned)slot < (unsigned)a.n_slots;
     const bool with_nodes = penal && a.token;
 
-    int32_t word[kPer];
+    // (what comes from memory is on its way while the tile's marks are set)
+    const X *x = static_cast<const X *>(a.x) + r * a.x_req + v;
+    const uint8_t *allow = a.allow ? reinterpret_cast<const uint8_t *>(a.allow + r * a.a_req) + (v >> 3) : nullptr;
+    auto grammar = [&](int n) { return allow ? allow + 4 * n * a.a_row : nullptr; };
+    Row<X> next;
+    next.load(x + n0 * a.x_row, grammar(n0), left);
+    int32_t word[kPer] = {};
+    if (with_history && left > 0) {
+        const int32_t *from = a.history + slot * a.h_row + v;
+        if (left >= kPer) {
+            const u32x4 lo = reinterpret_cast<const u32x4_e4 *>(from)[0], hi = reinterpret_cast<const u32x4_e4 *>(from)[1];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) word[i] = with_history && i < left ? a.history[slot * a.h_row + v + i] : 0;
+            for (int i = 0; i < 4; ++i) {
+                word[i] = (int32_t)lo[i];
+                word[4 + i] = (int32_t)hi[i];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) word[i] = i < left ? from[i] : 0;
+        }
+    }
     uint32_t mark[kPer] = {};
     float bias[kPer] = {};
     if (with_nodes || a.n_bias) {
         if (tid == 0) s_nodes = s_marks = 0;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) s_mark[i * kThreads + tid] = 0;
-        __syncthreads();
+        lds_barrier();
         for (int j = tid; j < a.n_bias; j += kThreads) {
             const unsigned t = (unsigned)a.bias_token[(long)r * a.n_bias + j] - (unsigned)v0;
             if (t < (unsigned)kTile) {
@@ -53,7 +99,7 @@ template <typename X, typename Y> __global__ void __launch_bounds__(kThreads) bd
                 s_marks = 1;
             }
         }
-        __syncthreads();
+        lds_barrier();
         if (with_nodes && tid < nodes) {
             const int t = a.token[(long)r * a.N + tid];
             if ((unsigned)t - (unsigned)v0 < (unsigned)kTile && (unsigned)t < (unsigned)a.V) {
@@ -64,7 +110,7 @@ template <typename X, typename Y> __global__ void __launch_bounds__(kThreads) bd
                 s_marks = 1;
             }
         }
-        __syncthreads();
+        lds_barrier();
         if (s_marks) {
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
@@ -79,15 +125,12 @@ template <typename X, typename Y> __global__ void __launch_bounds__(kThreads) bd
     for (int i = 0; i < kPer; ++i) any |= mark[i] & kNode;
     if (left <= 0) return;
 
-    const X *x = static_cast<const X *>(a.x) + r * a.x_req + v;
     Y *y = static_cast<Y *>(a.y) + r * a.y_req + v;
-    const uint8_t *allow = a.allow ? reinterpret_cast<const uint8_t *>(a.allow + r * a.a_req) + (v >> 3) : nullptr;
     for (int n = n0; n < n1; ++n) {
         float l[kPer];
-        if (left == kPer) load8(l, x + n * a.x_row);
-        else
-            for (int i = 0; i < kPer; ++i) l[i] = i < left ? to_f((x + n * a.x_row)[i]) : 0.f;
-        const uint32_t bits = allow ? allow[4 * n * a.a_row] : 0xffu;
+        next.get(l);
+        const uint32_t bits = next.bits;
+        if (n + 1 < n1) next.load(x + (n + 1) * a.x_row, grammar(n + 1), left);
         const uint64_t path = a.mask ? a.mask[(long)r * a.N + n] : (2ull << n) - 1;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
@@ -103,7 +146,7 @@ template <typename X, typename Y> __global__ void __launch_bounds__(kThreads) bd
             t += bias[i];
             l[i] = (bits >> i) & 1 ? t : -INFINITY;
         }
-        if (left == kPer) store8(y + n * a.y_row, l);
+        if (left >= kPer) store8(y + n * a.y_row, l);
         else
             for (int i = 0; i < left; ++i) (y + n * a.y_row)[i] = to_e<Y>(l[i]);
     }
