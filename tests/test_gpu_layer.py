@@ -156,6 +156,49 @@ def test_tensors_the_calls_refuse():
             call()
 
 
+def test_offsets_beyond_32_bits():
+    """The last rows of tensors of more than 2^32 bytes, as calls of their own give them."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+
+    def normal(*shape, dtype=torch.bfloat16):
+        return torch.empty(shape, dtype=dtype, device="cuda").normal_(generator=g)
+
+    turns, _ = bd.make_rope_turns(64)
+    q = normal(1, 9000, 2000, 128)
+    out = bd.bdgdn_rope(q, turns)
+    pos = torch.tensor([[8998, 8999]], dtype=torch.int32, device="cuda")
+    assert q.numel() > 2 ** 31 and torch.equal(bd.bdgdn_rope(q[:, -2:], turns, pos=pos), out[:, -2:])
+    del q, out
+    x, w = normal(300000, 8000), torch.ones(8000, device="cuda")
+    kw = dict(w_post=w, post=True)
+    y, _ = bd.bdgdn_norm_fwd(x, **kw)
+    assert x.numel() > 2 ** 31 and torch.equal(bd.bdgdn_norm_fwd(x[-3:], **kw)[0], y[-3:])
+    dx = bd.bdgdn_norm_bwd(x, y, **kw)[0]
+    assert torch.equal(bd.bdgdn_norm_bwd(x[-3:], y[-3:], **kw)[0], dx[-3:])
+    del y, dx
+    a, sa = bd.bdgdn_quant_rows(x)
+    few, few_s = bd.bdgdn_quant_rows(x[-300:])
+    assert a.numel() > 2 ** 31 and torch.equal(a[-300:], few) and torch.equal(sa[-300:], few_s)
+    wide = bd.bdgdn_quant_matmul(few, few_s, a, sa)            # [300, 300000]
+    tall = bd.bdgdn_quant_matmul(a, sa, a[:8000], sa[:8000])   # [300000, 8000]
+    assert tall.numel() > 2 ** 31
+    assert torch.equal(wide[:, -300:], bd.bdgdn_quant_matmul(few, few_s, few, few_s))
+    assert torch.equal(tall[-300:], bd.bdgdn_quant_matmul(few, few_s, a[:8000], sa[:8000]))
+    del a, x, wide, tall
+    R, N, V = 40, 60, 1000003
+    logits, history = normal(R, N, V), torch.zeros(2200, V, dtype=torch.int32, device="cuda")
+    assert logits.numel() > 2 ** 31 and history.numel() > 2 ** 31
+    token = torch.full((R, N), V - 1, dtype=torch.int32, device="cuda")
+    slot = torch.arange(2160, 2200, dtype=torch.int32, device="cuda")
+    bd.bdgdn_history_add(history, token, slot=slot)
+    assert (history[2160:, -1] == N).all() and not history[:2160].any() and not history[:, :-1].any()
+    kw = dict(frequency=torch.full((R,), 0.01, device="cuda"))
+    out = bd.bdgdn_logits(logits, token=token, history=history, slot=slot, **kw)
+    last = bd.bdgdn_logits(logits[-1:], token=token[-1:], history=history[-1:], frequency=kw["frequency"][:1])
+    assert torch.equal(out[-1], last[0]) and torch.equal(out[-1, -1, :-1], logits[-1, -1, :-1])
+    assert float(out[-1, -1, -1]) != float(logits[-1, -1, -1])
+
+
 # ------------------------------------------------------------------ rounds of a model
 def _np(t):
     return t.double().cpu().numpy()
