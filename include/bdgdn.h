@@ -915,7 +915,7 @@ typedef struct {
  *     scale = max |x| (1 / 127),  q = x / scale rounded to the nearest integer (of two the even one)
  * where 1 / 127, the product and the quotient are fp32 numbers.  Columns cols .. width - 1 of q are
  * zeros.  A row of zeros has scale 0; a row that holds a NaN or an infinity scale NaN; q is 0 in
- * both.  At most 2^24 rows.
+ * both.  Fewer than 2^24 rows.
  *   x  [rows][cols];  q  [rows][width] int8, 16-byte aligned, q_stride a multiple of 16
  *   scale  [rows] fp32
  */

@@ -161,7 +161,7 @@ int check_quant(const bdgdn_quant_desc_t *d)
 {
     if (!d) return BDGDN_ERR_INVALID_ARG;
     if (d->rows < 0 || d->cols <= 0 || d->width <= 0 || !stride_ok(d->x_stride) || !stride_ok(d->q_stride)) return BDGDN_ERR_INVALID_ARG;
-    if (d->cols > 0x40000000 || d->rows > (1 << 24)) return BDGDN_ERR_UNSUPPORTED;   // (a launch has 2^32 threads)
+    if (d->cols > 0x40000000 || d->rows >= (1 << 24)) return BDGDN_ERR_UNSUPPORTED;   // (a launch has 2^32 threads)
     if (d->width != (d->cols + 127) / 128 * 128 || d->q_stride % 16 || (d->rows > 1 && d->q_stride < d->width)) return BDGDN_ERR_INVALID_ARG;
     return type_ok(d->dtype) ? BDGDN_OK : BDGDN_ERR_UNSUPPORTED;
 }

@@ -8,7 +8,7 @@
 // once a tile: an LDS word for every token names its bias and says whether a node carries it.
 //
 // Bound by memory: 64 requests of 8 nodes over 131072 bf16 logits with history, 300 biases and a grammar
-// 56 us, 310 MB at 5.5 TB/s; one node each 17 us, 68 MB at 4.0; one request of 8 nodes over 32001 4.5 us.
+// 57 us, 310 MB at 5.4 TB/s; one node each 17 us, 68 MB at 4.0; one request of 8 nodes over 32001 4.5 us.
 #include "anywhere.hpp"
 #include "layer.hpp"
 

@@ -162,6 +162,7 @@ template <typename E, bool PAIRS> hipError_t launch(RopeArgs &a, hipStream_t s)
     if (4 * a.h <= 3 << heads_log && ((long)rows << (a.item_log + heads_log - 1)) >= 524288) --heads_log;
     a.sub_log = heads_log < 8 - a.item_log ? heads_log : 8 - a.item_log;
     a.row_log = 8 - a.item_log - a.sub_log;
+    if (heads_log > a.sub_log + 15) heads_log = a.sub_log + 15;   // (a grid's second dimension)
     const unsigned blocks = (rows + (1u << a.row_log) - 1) >> a.row_log;
     const unsigned parts = 1u << (heads_log - a.sub_log);
     const dim3 grid(blocks * (long)parts < kMostBlocks ? blocks : kMostBlocks / parts, parts);

@@ -5,8 +5,7 @@ and grammar masks.
 Bindings of the C entry points of the same names (``include/bdgdn.h``), re-exported by the
 package.  Like the others they only marshal arguments.  Rows have contiguous elements and otherwise
 any strides, so tensors may be parts of one projection's rows; outputs that are not given are
-contiguous.  All tensors of a call are on the device that it runs on, the current one or that of
-``stream``.
+contiguous.  All tensors of a call, and ``stream``, are on the current device.
 """
 from __future__ import annotations
 
@@ -99,7 +98,9 @@ def bind(lib):
 def _here(stream, names, *tensors):
     """The tensors are on the device that the call runs on; its raw stream.  (A small call costs what its
     marshalling does: what is usual is one comparison a tensor.)"""
-    at = _current_device() if stream is None else stream.device_index
+    at = _current_device()
+    if stream is not None and stream.device_index != at:
+        raise ValueError(f"the stream is on device {stream.device_index}, the call runs on device {at}")
     if tensors[0] is None:
         raise ValueError(f"{names.split()[0]} must be a device tensor")
     for t in tensors:

@@ -50,7 +50,7 @@ def positions(R, N, seq_len, slot, pos):
 CASES = [  # R, N, h_q, h_k, d, rot
     (1, 1, 32, 8, 128, 128), (1, 1, 1, 0, 64, 64), (3, 5, 4, 2, 128, 32), (2, 33, 6, 2, 80, 40), (2, 7, 3, 1, 256, 64),
     (1, 70, 5, 5, 100, 10), (4, 3, 2, 1, 33, 6), (2, 2, 1, 1, 2, 2), (1, 3, 2, 1, 1024, 1024), (1, 2, 70, 3, 64, 16),
-    (2, 3, 2, 2, 4096, 4094),
+    (2, 3, 2, 2, 4096, 4094), (1, 1, 60000, 40000, 2, 2),
 ]
 
 

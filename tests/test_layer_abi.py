@@ -232,7 +232,7 @@ def test_quant_rows_rejects():
     for kw in (dict(rows=-1), dict(cols=0), dict(width=0), dict(width=100), dict(width=256), dict(x_stride=-1), dict(q_stride=112),
                dict(q_stride=136), dict(x=None), dict(q=None), dict(scale=None), dict(x=0x1002), dict(q=0x1008), dict(scale=0x1002)):
         assert call(**kw) == INV, kw
-    assert call(dtype=2) == UNS and call(cols=(1 << 30) + 1) == UNS and call(rows=0, x=None) == OK
+    assert call(dtype=2) == UNS and call(cols=(1 << 30) + 1) == UNS and call(rows=1 << 24) == UNS and call(rows=0, x=None) == OK
 
 
 def test_quant_matmul_rejects():
@@ -267,6 +267,24 @@ def test_the_binding_refuses_what_is_not_on_the_device(monkeypatch):
                  lambda: bd.bdgdn_quant_rows(x), lambda: bd.bdgdn_quant_matmul(x.to(torch.int8), x, x.to(torch.int8), x)):
         with pytest.raises(ValueError, match="must be a device tensor"):
             call()
+
+
+def test_the_binding_refuses_other_devices(monkeypatch):
+    class Elsewhere(torch.Tensor):
+        is_cuda = True
+
+        def get_device(self):
+            return 1
+
+    class Stream:
+        device_index, cuda_stream = 1, 0
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    x = torch.zeros(2, 8).as_subclass(Elsewhere)
+    with pytest.raises(ValueError, match="x is on device 1, the call runs on device 0"):
+        bd.bdgdn_norm_fwd(x)
+    with pytest.raises(ValueError, match="the stream is on device 1"):
+        bd.bdgdn_norm_fwd(x, stream=Stream())
 
 
 def test_kept_plans_follow_shapes_and_strides():
