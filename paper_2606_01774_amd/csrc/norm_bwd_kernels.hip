@@ -10,7 +10,8 @@
 // in a second kernel, in order.
 //
 // Bound by memory: 16384 rows of 4096 with gate and fp32 residual 273 us, 1476 MB at 5.4 TB/s, and 4.6 for the
-// weights' sums (12.6 MB); 16384 x 16 heads of 128 with their gate 97 us, 470 MB at 4.9.  The 512 lanes of a
+// weights' sums (12.6 MB); 16384 x 16 heads of 128 with their gate 97 us, 470 MB at 4.9;
+// bf16 heads of 64 and 256 3.8.  The 512 lanes of a
 // workgroup take 150 to 180 registers each, so a compute unit has one, and what keeps memory busy is
 // the next row, loaded while this one is worked on (443 us without it, in workgroups of 1024).  Twice the
 // workgroups leave twice the partial sums, and take 293 us.  Rows of 8192 take two chunks to a lane, none
@@ -273,8 +274,11 @@ template <typename X, typename R, typename Y, int LANES, int C> void launch(cons
 template <typename X, typename R, typename Y> hipError_t sized(const NormArgs &a, hipStream_t s)
 {
     if (a.groups > 0) {
-        if (a.d <= 128) launch<X, R, Y, 16, 1>(a, s);
+        if (a.d <= 64) launch<X, R, Y, 8, 1>(a, s);
+        else if (a.d <= 128) launch<X, R, Y, 16, 1>(a, s);
+        else if (a.d <= 256) launch<X, R, Y, 32, 1>(a, s);
         else if (a.d <= 512) launch<X, R, Y, 64, 1>(a, s);
+        else if (a.d <= 1024) launch<X, R, Y, 128, 1>(a, s);
         else if (a.d <= 2048) launch<X, R, Y, 256, 1>(a, s);
         else if (a.d <= 4096) launch<X, R, Y, 512, 1>(a, s);
         else if (a.d <= 8192) launch<X, R, Y, 512, 2>(a, s);
@@ -292,7 +296,7 @@ template <typename X, typename R, typename Y> hipError_t sized(const NormArgs &a
 
 int norm_bwd_groups(int rows, int d)
 {
-    const int lanes = d <= 128 ? 16 : d <= 512 ? 64 : d <= 2048 ? 256 : 512, in_one = kThreads / lanes;
+    const int lanes = d <= 64 ? 8 : d <= 128 ? 16 : d <= 256 ? 32 : d <= 512 ? 64 : d <= 1024 ? 128 : d <= 2048 ? 256 : 512, in_one = kThreads / lanes;
     const int groups = (int)(((long)rows + in_one - 1) / in_one);
     return groups < kMostGroups ? groups : kMostGroups;
 }
