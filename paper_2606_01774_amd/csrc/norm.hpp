@@ -94,6 +94,14 @@ template <bool WHOLE, int LANES, int C, typename E> __device__ __forceinline__ v
 
 // 1 / (1 + exp(-z)); a large -z gives exp = inf and the result 0.
 __device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + fexp2(-kLog2e * z)); }
+// e = sigmoid(z), and 1 - e in 32 bits of its own: the difference cancels where e is near 1 (at z = 12 1 % of it
+// is rounding, from 17 on all), so there it is exp(-z) e.
+__device__ __forceinline__ float sigmoid(float z, float &rest)
+{
+    const float t = fexp2(-kLog2e * z), e = __builtin_amdgcn_rcpf(1.f + t);
+    rest = z > 0.f ? t * e : 1.f - e;
+    return e;
+}
 
 // Sums over the LANES lanes of a row, in every lane of it.  Rows of several waves meet in LDS: two
 // buffers take turns, so that a sum needs one barrier (between a buffer's readers and its next

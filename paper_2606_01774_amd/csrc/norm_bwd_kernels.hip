@@ -72,9 +72,10 @@ __global__ void __launch_bounds__(kThreads) bdgdn_norm_bwd_kernel(NormArgs a)
     if (ONE) weights(0);
     // the gate and its slope
     auto gate = [&](float z, float &act, float &slope) {
-        const float e = a.act ? sigmoid(z) : z;
-        act = a.act == kActSilu ? z * e : e;
-        slope = a.act == kActSilu ? e * (1.f + z * (1.f - e)) : a.act ? e * (1.f - e) : 1.f;
+        float rest;
+        const float e = sigmoid(z, rest);
+        act = a.act == kActSilu ? z * e : a.act ? e : z;
+        slope = a.act == kActSilu ? e * (1.f + z * (1.f - e)) : a.act ? e * rest : 1.f;
     };
     float acc[3][C][8] = {};   // of w_post, w_pre, layer_scale
 
