@@ -277,8 +277,9 @@ def bdgdn_norm_bwd(x, dy, *, z=None, r_out=None, dr_out=None, w_post=None, w_pre
     here = _here(stream, "x dy z r_out dr_out w_post w_pre layer_scale dx dz dr dw_post dw_pre dlayer_scale workspace",
                  x, dy, z, r_out, dr_out, w_post, w_pre, layer_scale, dx, dz, dr, dw_post, dw_pre, dlayer_scale, workspace)
     shape, d = x.shape, x.shape[-1]
-    dt = z.dtype if z is not None else dy.dtype if dy is not None else x.dtype
     rt = r_out.dtype if r_out is not None else dr_out.dtype if dr_out is not None else dr.dtype if dr is not None else x.dtype
+    # (without z and dy nothing is of y's type: bf16 goes with all others)
+    dt = z.dtype if z is not None else dy.dtype if dy is not None else x.dtype if x.dtype is rt else torch.bfloat16
     for t, name, kind in ((dy, "dy", dt), (z, "z", dt), (r_out, "r_out", rt), (dr_out, "dr_out", rt), (dx, "dx", x.dtype),
                           (dz, "dz", dt), (dr, "dr", rt)):
         _like(t, name, shape, kind)
