@@ -53,7 +53,8 @@ def parents_of(branches):
 class Decoder:
     """The model with the states and caches of `slots` sequences of up to max_len tokens.  rotary: the
     base of the attention layers' positions (None: they have none); eight_bit: projections in 8-bit
-    integers; penalties: (repetition, presence, frequency) of tokens that a sequence holds already."""
+    integers; penalties: (repetition, presence, frequency) of tokens that a sequence holds already (the last
+    two: that it has generated)."""
 
     def __init__(self, layers="gaga", vocab=512, width=256, slots=32, page=16, max_len=1024, pages=None, seed=0,
                  device="cuda", rotary=None, eight_bit=False, penalties=None):
@@ -77,6 +78,8 @@ class Decoder:
         self.taken = torch.zeros(slots, dtype=torch.int32, device=device)
         self.penalties = penalties
         self.history = torch.zeros(slots, vocab, dtype=torch.int32, device=device) if penalties else None
+        # sequences whose next anchor is a prompt's token (its last: the model has not taken it in yet)
+        self.prompted = torch.zeros(slots, dtype=torch.bool, device=device)
         self.drafter = self.logits(self.embed.float())   # [V, V]: after each token
         self.states = [torch.zeros(slots, GDN_HEADS, GDN_DIM, GDN_DIM, device=device) if x == "g" else None
                        for x in layers]
@@ -139,11 +142,13 @@ class Decoder:
             return bd.bdgdn_cache_append(self.tables, self.pools, rows, slot, count, path=path)
         return torch.zeros_like(count)
 
-    def prefill(self, prompt, slot, block=32):
-        """Takes in prompt [R, T] but its last token, which is the first round's anchor."""
+    def prefill(self, prompt, slot, block=32, whole=False):
+        """Takes in prompt [R, T] but its last token, which is the first round's anchor.  whole: that token is the
+        prompt's too; else it counts as generated, like the anchors behind it."""
         status = torch.zeros_like(slot)
+        self.prompted[slot.long()] = whole
         if self.penalties:
-            bd.bdgdn_history_add(self.history, prompt[:, :-1].contiguous(), slot=slot, prompt=True)
+            bd.bdgdn_history_add(self.history, (prompt if whole else prompt[:, :-1]).contiguous(), slot=slot, prompt=True)
         for t in range(0, prompt.shape[1] - 1, block):
             part = prompt[:, t:min(t + block, prompt.shape[1] - 1)]
             _, rows, _ = self.forward(part, slot)
@@ -155,6 +160,7 @@ class Decoder:
             if s is not None:
                 s[dst.long()] = s[src.long()]
         self.taken[dst.long()] = self.taken[src.long()]
+        self.prompted[dst.long()] = self.prompted[src.long()]
         if self.penalties:
             self.history[dst.long()] = self.history[src.long()]
         return bd.bdgdn_cache_fork(self.tables, src, dst)
@@ -169,14 +175,17 @@ class Decoder:
         R, N, V = target.shape
         if self.penalties:
             repetition, presence, frequency = (torch.full((R,), float(p), device=self.device) for p in self.penalties)
-            bd.bdgdn_logits(target, token=token, mask=mask, history=self.history, slot=slot, repetition=repetition,
+            generated = token.clone()   # (-1 counts for nothing: the history has marked a prompt's token)
+            generated[:, 0].masked_fill_(self.prompted[slot.long()], -1)
+            bd.bdgdn_logits(target, token=generated, mask=mask, history=self.history, slot=slot, repetition=repetition,
                             presence=presence, frequency=frequency, out=target)
         u = torch.rand(R, N, device=self.device)
         noise = torch.empty(R, V, device=self.device).exponential_()
         T = torch.full((R,), float(temperature), device=self.device)
         out = bd.bdgdn_verify(target, token, u, noise, temperature=T, want_n_path=True, **kw)
         if self.penalties:
-            bd.bdgdn_history_add(self.history, token, slot=slot, path=out[1], count=out[3])
+            bd.bdgdn_history_add(self.history, generated, slot=slot, path=out[1], count=out[3])
+        self.prompted[slot.long()] = False
         return out
 
     def round(self, anchor, slot, drafts=7, temperature=1.0):
@@ -263,7 +272,7 @@ def main():
                     rotary=args.rotary, eight_bit=args.eight_bit, penalties=penalties if penalties != (1, 0, 0) else None)
     slot = torch.arange(R * ways, dtype=torch.int32, device=model.device)
     prompt = torch.randint(model.vocab, (R, args.length), dtype=torch.int32, device=model.device)
-    anchor, status = model.prefill(prompt, slot[:R])
+    anchor, status = model.prefill(prompt, slot[:R], whole=True)
     bad = status.max()
     if ways > 1:
         bad = torch.maximum(bad, model.fork(slot[:R].repeat(ways - 1), slot[R:]).max())

@@ -872,7 +872,8 @@ typedef struct {
  *   slot         [R] int32, or NULL for slot[r] = r (then R <= n_slots); a slot outside
  *                [0, n_slots) has no history
  *   token        [R][N] int32 the nodes' tokens, or NULL where they do not count; a token
- *                outside [0, V) counts for nothing
+ *                outside [0, V) counts for nothing (-1 for an anchor that is the prompt's last
+ *                token: it was not generated, and the history has marked it)
  *   mask         [R][N] 64-bit words of bdgdn_tree_mask (bit j: node j is n or its ancestor),
  *                or NULL for chains
  *   count        [R] int32 nodes of each request, or NULL for N; rows behind them are not read,

@@ -1,0 +1,106 @@
+"""What examples/speculative_decode.py keeps of a sequence beside its cache.  The reference model and its
+tolerances: test_gpu_layer."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2606_01774_amd as bd
+from test_gpu_layer import REL, check, reference, sd
+
+pytestmark = pytest.mark.gpu
+
+
+def prompts(model, R, T, seed=3):
+    return torch.randint(model.vocab, (R, T), dtype=torch.int32, generator=torch.Generator().manual_seed(seed)).cuda()
+
+
+def go_on(sequences, step):
+    token, n_accept, anchor, _ = step
+    for seq, t, n, nxt in zip(sequences, token.tolist(), n_accept.tolist(), anchor.tolist()):
+        seq += t[1:1 + n] + [nxt]
+    return anchor
+
+
+def check_penalties(model, sequences, T, base, penalties):
+    """The prompt is the first T tokens, all of them; what comes behind them was generated."""
+    rho, presence, frequency = penalties
+    for slot, seq in enumerate(sequences):
+        logits, _ = reference(model, np.array(seq[:-1]), base)
+        history, prompt = np.zeros(model.vocab, int), np.zeros(model.vocab, bool)
+        prompt[seq[:T]] = True
+        for t in range(T - 1, len(seq) - 1):
+            if t >= T:
+                history[seq[t]] += 1
+            seen = prompt | (history > 0)
+            row = np.where(seen, np.where(logits[t] > 0, logits[t] / rho, logits[t] * rho), logits[t])
+            row = row - presence * (history > 0) - frequency * history
+            assert row.max() - row[seq[t + 1]] < REL * 2 ** 0.5 * 4 * rho * logits.std(), (slot, t)
+        got = model.history[slot].cpu().numpy()
+        assert (got % (1 << 30) == history).all() and ((got >> 30) == prompt).all()
+
+
+@pytest.mark.parametrize("argv", [["--layers", "gaga"], ["--layers", "aa", "--tree", "2,2"]])
+def test_the_command_penalises_generated_tokens_alone(argv, monkeypatch, capsys):
+    """The last token of a prompt, the first anchor, is the prompt's like the others."""
+    seen, prefill, finish = {}, sd.Decoder.prefill, sd.Decoder.finish
+
+    def keep_prompt(self, prompt, *args, **kw):
+        seen["prompt"] = prompt.cpu()
+        return prefill(self, prompt, *args, **kw)
+
+    def keep_history(self, slot):
+        seen["history"], seen["taken"] = self.history.cpu(), self.taken.cpu()
+        return finish(self, slot)
+
+    monkeypatch.setattr(sd.Decoder, "prefill", keep_prompt)
+    monkeypatch.setattr(sd.Decoder, "finish", keep_history)
+    monkeypatch.setattr("sys.argv", ["speculative_decode.py", "--prompts", "3", "--ways", "2", "--rounds", "4", "--length", "20",
+                                     "--presence", "0.5", *argv])
+    sd.main()
+    assert "tokens a sequence and round" in capsys.readouterr().out
+    prompt, history = seen["prompt"], seen["history"]
+    for s in range(6):
+        marks = torch.zeros(history.shape[1], dtype=torch.bool)
+        marks[prompt[s % 3].long()] = True
+        assert torch.equal(history[s] >= bd.BDGDN_HISTORY_PROMPT, marks)
+        # every token behind the prompt that the sequence has taken in, once
+        assert int((history[s] % bd.BDGDN_HISTORY_PROMPT).sum()) == int(seen["taken"][s]) - prompt.shape[1]
+
+
+def test_generated_tokens_alone_are_penalised():
+    R, ways, T, drafts, penalties, base = 2, 2, 30, 4, (1.2, 1.5, 0.4), 500.0
+    model = sd.Decoder("ga", slots=R * ways, max_len=128, rotary=base, penalties=penalties)
+    slot = torch.arange(R * ways, dtype=torch.int32, device="cuda")
+    prompt = prompts(model, R, T)
+    anchor, status = model.prefill(prompt, slot[:R], whole=True)
+    assert not status.any() and not model.fork(slot[:R].clone(), slot[R:].clone()).any()
+    anchor, sequences = anchor.repeat(ways), [prompt[i % R].tolist() for i in range(R * ways)]
+    for _ in range(6):
+        anchor = go_on(sequences, model.round(anchor, slot, drafts, 0.0))
+    check_penalties(model, sequences, T, base, penalties)
+
+
+def test_an_anchor_that_was_generated_counts():
+    """Without `whole` the first anchor is a token that another program has generated."""
+    R, T, penalties, base = 2, 30, (1.2, 1.5, 0.4), 500.0
+    model = sd.Decoder("ga", slots=R, max_len=128, rotary=base, penalties=penalties)
+    slot = torch.arange(R, dtype=torch.int32, device="cuda")
+    prompt = prompts(model, R, T)
+    anchor, _ = model.prefill(prompt, slot)
+    sequences = prompt.tolist()
+    for _ in range(3):
+        anchor = go_on(sequences, model.round(anchor, slot, 4, 0.0))
+    check(model, sequences, T, base, penalties)
+
+
+def test_trees_penalise_generated_tokens_alone():
+    R, T, penalties, base = 3, 12, (1.1, 1.0, 0.3), 10000.0
+    model = sd.Decoder("aa", slots=R, max_len=64, rotary=base, penalties=penalties)
+    slot = torch.arange(R, dtype=torch.int32, device="cuda")
+    prompt = prompts(model, R, T)
+    anchor, _ = model.prefill(prompt, slot, whole=True)
+    sequences = prompt.tolist()
+    for _ in range(5):
+        token, n_accept, nxt, _ = model.tree_round(anchor, slot, [3, 2], 0.0)
+        anchor = go_on(sequences, (token, n_accept, nxt, None))
+    check_penalties(model, sequences, T, base, penalties)
