@@ -137,14 +137,19 @@ class Decoder:
         return (z @ self.out).float().view(R, N, -1), rows, recorded
 
     def append(self, rows, slot, count, path=None):
-        self.taken.index_add_(0, slot.long(), count)
+        """(status, how many tokens each sequence has taken in: none where the cache has refused them)."""
         if rows:
-            return bd.bdgdn_cache_append(self.tables, self.pools, rows, slot, count, path=path)
-        return torch.zeros_like(count)
+            status = bd.bdgdn_cache_append(self.tables, self.pools, rows, slot, count, path=path)
+        else:
+            status = torch.zeros_like(count)
+        kept = torch.where(status == bd.BDGDN_CACHE_DONE, count, 0)
+        self.taken.index_add_(0, slot.long(), kept)
+        return status, kept
 
     def prefill(self, prompt, slot, block=32, whole=False):
         """Takes in prompt [R, T] but its last token, which is the first round's anchor.  whole: that token is the
-        prompt's too; else it counts as generated, like the anchors behind it."""
+        prompt's too; else it counts as generated, like the anchors behind it.  A request whose status
+        is not BDGDN_CACHE_DONE has taken in a part: it is to be finished."""
         status = torch.zeros_like(slot)
         self.prompted[slot.long()] = whole
         if self.penalties:
@@ -152,7 +157,7 @@ class Decoder:
         for t in range(0, prompt.shape[1] - 1, block):
             part = prompt[:, t:min(t + block, prompt.shape[1] - 1)]
             _, rows, _ = self.forward(part, slot)
-            status |= self.append(rows, slot, torch.full_like(slot, part.shape[1]))
+            status |= self.append(rows, slot, torch.full_like(slot, part.shape[1]))[0]
         return prompt[:, -1], status
 
     def fork(self, src, dst):
@@ -175,33 +180,43 @@ class Decoder:
         R, N, V = target.shape
         if self.penalties:
             repetition, presence, frequency = (torch.full((R,), float(p), device=self.device) for p in self.penalties)
-            generated = token.clone()   # (-1 counts for nothing: the history has marked a prompt's token)
-            generated[:, 0].masked_fill_(self.prompted[slot.long()], -1)
-            bd.bdgdn_logits(target, token=generated, mask=mask, history=self.history, slot=slot, repetition=repetition,
-                            presence=presence, frequency=frequency, out=target)
+            bd.bdgdn_logits(target, token=self._generated(token, slot), mask=mask, history=self.history, slot=slot,
+                            repetition=repetition, presence=presence, frequency=frequency, out=target)
         u = torch.rand(R, N, device=self.device)
         noise = torch.empty(R, V, device=self.device).exponential_()
         T = torch.full((R,), float(temperature), device=self.device)
-        out = bd.bdgdn_verify(target, token, u, noise, temperature=T, want_n_path=True, **kw)
+        return bd.bdgdn_verify(target, token, u, noise, temperature=T, want_n_path=True, **kw)
+
+    def _generated(self, token, slot):
+        """A block's tokens as the penalties count them (-1 counts for nothing: the history has marked a prompt's)."""
+        token = token.clone()
+        token[:, 0].masked_fill_(self.prompted[slot.long()], -1)
+        return token
+
+    def _keep(self, rows, recorded, token, slot, path, n_path):
+        """The sequences take in the accepted path of a block, in their caches, states and histories; those that
+        the cache refuses stay as they were before it, and the block may be tried again."""
+        status, kept = self.append(rows, slot, n_path, path)
+        for state, states in zip(self.states, recorded):
+            if states is not None:
+                bd.bdgdn_accept_states(state, states, kept, block=token.shape[1], slot=slot)
         if self.penalties:
-            bd.bdgdn_history_add(self.history, generated, slot=slot, path=out[1], count=out[3])
-        self.prompted[slot.long()] = False
-        return out
+            bd.bdgdn_history_add(self.history, self._generated(token, slot), slot=slot, path=path, count=kept)
+        self.prompted[slot.long()] &= kept == 0
+        return status
 
     def round(self, anchor, slot, drafts=7, temperature=1.0):
         """One round with a drafted chain.  Returns (tokens [R, 1 + drafts] of the block,
-        n_accept, the next anchor, status)."""
+        n_accept, the next anchor, status); the last anchor stays that of a request whose status is not
+        BDGDN_CACHE_DONE."""
         token = [anchor]
         for _ in range(drafts):
             token.append(self._draft(self.drafter[token[-1].long()], temperature).to(torch.int32))
         token = torch.stack(token, 1)
         draft = self.drafter[token[:, :-1].long()]
-        target, rows, recorded = self.forward(token, slot, n_record=drafts)
+        target, rows, recorded = self.forward(token, slot, n_record=1 + drafts)   # (from the state before the block on)
         n_accept, path, anchor, n_path = self._verify(target, token, slot, temperature, draft=draft)
-        for state, kept in zip(self.states, recorded):
-            if kept is not None:
-                bd.bdgdn_accept_states(state, kept, n_accept, block=token.shape[1], slot=slot)
-        return token, n_accept, anchor, self.append(rows, slot, n_path, path)
+        return token, n_accept, anchor, self._keep(rows, recorded, token, slot, path, n_path)
 
     def tree_round(self, anchor, slot, branches, temperature=1.0):
         """One round with a tree of the drafter's most likely tokens.  Returns (tokens of the
@@ -216,9 +231,9 @@ class Decoder:
         token = torch.stack(token, 1)
         parents = torch.tensor([parent] * len(slot), dtype=torch.int32, device=self.device)
         mask, depth = bd.bdgdn_tree_mask(parents, want_depth=True)
-        target, rows, _ = self.forward(token, slot, mask=mask, depth=depth)
+        target, rows, recorded = self.forward(token, slot, mask=mask, depth=depth)
         n_accept, path, anchor, n_path = self._verify(target, token, slot, temperature, mask=mask, parent=parents)
-        status = self.append(rows, slot, n_path, path)
+        status = self._keep(rows, recorded, token, slot, path, n_path)
         return token.gather(1, path.clamp(min=0).long()), n_accept, anchor, status
 
     def shorten(self, slot, first, last):

@@ -104,3 +104,34 @@ def test_trees_penalise_generated_tokens_alone():
         token, n_accept, nxt, _ = model.tree_round(anchor, slot, [3, 2], 0.0)
         anchor = go_on(sequences, (token, n_accept, nxt, None))
     check_penalties(model, sequences, T, base, penalties)
+
+
+def held(model, s):
+    return [t[s].clone() for t in (model.taken, model.history, model.tables.seq_len, *(x for x in model.states if x is not None))]
+
+
+def test_a_refused_append_leaves_the_sequence_as_it_was():
+    """Five pages of 16: slot 0 fills two, slot 1 a part of its second, slot 2 one.  A round finds no page for
+    slot 0; when slot 2 has ended, the same round goes through."""
+    T, penalties, base = 33, (1.2, 0.3, 0.1), 500.0
+    model = sd.Decoder("gaga", slots=3, max_len=64, pages=5, rotary=base, penalties=penalties)
+    slot = torch.arange(3, dtype=torch.int32, device="cuda")
+    prompt = prompts(model, 3, T)
+    anchors = []
+    for s, n in enumerate((T, 21, 11)):
+        anchor, status = model.prefill(prompt[s:s + 1, :n], slot[s:s + 1])
+        assert not status.any()
+        anchors.append(anchor)
+    before, other = held(model, 0), held(model, 1)
+    *_, status = model.round(torch.cat(anchors[:2]), slot[:2], 5, 0.0)
+    assert status.tolist() == [bd.BDGDN_CACHE_NO_PAGES, bd.BDGDN_CACHE_DONE]
+    for name, a, b in zip(("taken", "history", "seq_len", "state", "state"), before, held(model, 0)):
+        assert torch.equal(a, b), name
+    assert int(model.taken[1]) == int(model.tables.seq_len[1]) > int(other[0])
+    model.finish(slot[2:])
+    sequences, anchor = [prompt[0].tolist()], anchors[0]
+    for _ in range(2):
+        step = model.round(anchor, slot[:1], 5, 0.0)
+        assert not step[3].any()
+        anchor = go_on(sequences, step)
+    check(model, sequences, T, base, penalties)
