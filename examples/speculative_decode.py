@@ -161,14 +161,13 @@ class Decoder:
         return prompt[:, -1], status
 
     def fork(self, src, dst):
-        for s in self.states:
-            if s is not None:
-                s[dst.long()] = s[src.long()]
-        self.taken[dst.long()] = self.taken[src.long()]
-        self.prompted[dst.long()] = self.prompted[src.long()]
-        if self.penalties:
-            self.history[dst.long()] = self.history[src.long()]
-        return bd.bdgdn_cache_fork(self.tables, src, dst)
+        """Gives slots dst the sequences of src; a slot whose status is not BDGDN_CACHE_DONE stays as it was."""
+        status = bd.bdgdn_cache_fork(self.tables, src, dst)
+        done, src, dst = status == bd.BDGDN_CACHE_DONE, src.long(), dst.long()
+        for t in (*self.states, self.taken, self.prompted, self.history):
+            if t is not None:
+                t[dst] = torch.where(done.view(-1, *[1] * (t.dim() - 1)), t[src], t[dst])
+        return status
 
     def _draft(self, logits, temperature):
         if temperature <= 0:

@@ -135,3 +135,16 @@ def test_a_refused_append_leaves_the_sequence_as_it_was():
         assert not step[3].any()
         anchor = go_on(sequences, step)
     check(model, sequences, T, base, penalties)
+
+
+def test_a_refused_fork_leaves_the_sequence_as_it_was():
+    model = sd.Decoder("ga", slots=3, max_len=64, rotary=500.0, penalties=(1.2, 0.3, 0.1))
+    slot = torch.arange(3, dtype=torch.int32, device="cuda")
+    prompt = prompts(model, 2, 20)
+    for s in range(2):
+        model.prefill(prompt[s:s + 1, :20 - 5 * s], slot[s:s + 1])
+    source, taken = held(model, 0), held(model, 1)
+    status = model.fork(slot[:1].repeat(2), slot[1:])   # slot 1 is in use
+    assert status.tolist() == [bd.BDGDN_CACHE_BAD_SLOT, bd.BDGDN_CACHE_DONE]
+    assert all(torch.equal(a, b) for a, b in zip(taken, held(model, 1)))
+    assert all(torch.equal(a, b) for a, b in zip(source, held(model, 2)))
