@@ -244,9 +244,10 @@ class Decoder:
         return bd.bdgdn_cache_compact(self.tables, self.pools, slot, keep.contiguous(), count)
 
     def finish(self, slot):
-        self.taken[slot.long()] = 0
-        if self.penalties:
-            self.history[slot.long()] = 0
+        """The sequences end: their slots may be used again."""
+        for t in (*self.states, self.taken, self.prompted, self.history):
+            if t is not None:
+                t[slot.long()] = 0
         bd.bdgdn_cache_truncate(self.tables, slot)
 
 

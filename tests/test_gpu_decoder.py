@@ -148,3 +148,14 @@ def test_a_refused_fork_leaves_the_sequence_as_it_was():
     assert status.tolist() == [bd.BDGDN_CACHE_BAD_SLOT, bd.BDGDN_CACHE_DONE]
     assert all(torch.equal(a, b) for a, b in zip(taken, held(model, 1)))
     assert all(torch.equal(a, b) for a, b in zip(source, held(model, 2)))
+
+
+def test_a_slot_that_is_used_again():
+    model = sd.Decoder("ga", slots=2, max_len=64, rotary=500.0, penalties=(1.2, 0.3, 0.1))
+    slot = torch.arange(2, dtype=torch.int32, device="cuda")
+    prompt = prompts(model, 2, 20)
+    model.prefill(prompt[:1], slot[:1])
+    model.finish(slot[:1])
+    for s in range(2):   # the same prompt where a sequence has been, and where none has
+        model.prefill(prompt[1:], slot[s:s + 1])
+    assert all(torch.equal(a, b) for a, b in zip(held(model, 0), held(model, 1)))
