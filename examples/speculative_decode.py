@@ -79,7 +79,7 @@ class Decoder:
         self.penalties = penalties
         self.history = torch.zeros(slots, vocab, dtype=torch.int32, device=device) if penalties else None
         # sequences whose next anchor is a prompt's token (its last: the model has not taken it in yet)
-        self.prompted = torch.zeros(slots, dtype=torch.bool, device=device)
+        self.prompted = torch.zeros(slots, dtype=torch.bool, device=device) if penalties else None
         self.drafter = self.logits(self.embed.float())   # [V, V]: after each token
         self.states = [torch.zeros(slots, GDN_HEADS, GDN_DIM, GDN_DIM, device=device) if x == "g" else None
                        for x in layers]
@@ -151,8 +151,8 @@ class Decoder:
         prompt's too; else it counts as generated, like the anchors behind it.  A request whose status
         is not BDGDN_CACHE_DONE has taken in a part: it is to be finished."""
         status = torch.zeros_like(slot)
-        self.prompted[slot.long()] = whole
         if self.penalties:
+            self.prompted[slot.long()] = whole
             bd.bdgdn_history_add(self.history, (prompt if whole else prompt[:, :-1]).contiguous(), slot=slot, prompt=True)
         for t in range(0, prompt.shape[1] - 1, block):
             part = prompt[:, t:min(t + block, prompt.shape[1] - 1)]
@@ -175,12 +175,12 @@ class Decoder:
         p = torch.softmax(logits / temperature, -1)
         return (p / torch.empty_like(p).exponential_()).argmax(-1)
 
-    def _verify(self, target, token, slot, temperature, mask=None, **kw):
+    def _verify(self, target, token, generated, slot, temperature, mask=None, **kw):
         R, N, V = target.shape
         if self.penalties:
             repetition, presence, frequency = (torch.full((R,), float(p), device=self.device) for p in self.penalties)
-            bd.bdgdn_logits(target, token=self._generated(token, slot), mask=mask, history=self.history, slot=slot,
-                            repetition=repetition, presence=presence, frequency=frequency, out=target)
+            bd.bdgdn_logits(target, token=generated, mask=mask, history=self.history, slot=slot, repetition=repetition,
+                            presence=presence, frequency=frequency, out=target)
         u = torch.rand(R, N, device=self.device)
         noise = torch.empty(R, V, device=self.device).exponential_()
         T = torch.full((R,), float(temperature), device=self.device)
@@ -188,20 +188,22 @@ class Decoder:
 
     def _generated(self, token, slot):
         """A block's tokens as the penalties count them (-1 counts for nothing: the history has marked a prompt's)."""
+        if not self.penalties:
+            return None
         token = token.clone()
         token[:, 0].masked_fill_(self.prompted[slot.long()], -1)
         return token
 
-    def _keep(self, rows, recorded, token, slot, path, n_path):
+    def _keep(self, rows, recorded, generated, slot, path, n_path):
         """The sequences take in the accepted path of a block, in their caches, states and histories; those that
         the cache refuses stay as they were before it, and the block may be tried again."""
         status, kept = self.append(rows, slot, n_path, path)
         for state, states in zip(self.states, recorded):
             if states is not None:
-                bd.bdgdn_accept_states(state, states, kept, block=token.shape[1], slot=slot)
+                bd.bdgdn_accept_states(state, states, kept, block=path.shape[1], slot=slot)
         if self.penalties:
-            bd.bdgdn_history_add(self.history, self._generated(token, slot), slot=slot, path=path, count=kept)
-        self.prompted[slot.long()] &= kept == 0
+            bd.bdgdn_history_add(self.history, generated, slot=slot, path=path, count=kept)
+            self.prompted[slot.long()] &= kept == 0
         return status
 
     def round(self, anchor, slot, drafts=7, temperature=1.0):
@@ -214,8 +216,9 @@ class Decoder:
         token = torch.stack(token, 1)
         draft = self.drafter[token[:, :-1].long()]
         target, rows, recorded = self.forward(token, slot, n_record=1 + drafts)   # (from the state before the block on)
-        n_accept, path, anchor, n_path = self._verify(target, token, slot, temperature, draft=draft)
-        return token, n_accept, anchor, self._keep(rows, recorded, token, slot, path, n_path)
+        generated = self._generated(token, slot)
+        n_accept, path, anchor, n_path = self._verify(target, token, generated, slot, temperature, draft=draft)
+        return token, n_accept, anchor, self._keep(rows, recorded, generated, slot, path, n_path)
 
     def tree_round(self, anchor, slot, branches, temperature=1.0):
         """One round with a tree of the drafter's most likely tokens.  Returns (tokens of the
@@ -231,8 +234,9 @@ class Decoder:
         parents = torch.tensor([parent] * len(slot), dtype=torch.int32, device=self.device)
         mask, depth = bd.bdgdn_tree_mask(parents, want_depth=True)
         target, rows, recorded = self.forward(token, slot, mask=mask, depth=depth)
-        n_accept, path, anchor, n_path = self._verify(target, token, slot, temperature, mask=mask, parent=parents)
-        status = self._keep(rows, recorded, token, slot, path, n_path)
+        generated = self._generated(token, slot)
+        n_accept, path, anchor, n_path = self._verify(target, token, generated, slot, temperature, mask=mask, parent=parents)
+        status = self._keep(rows, recorded, generated, slot, path, n_path)
         return token.gather(1, path.clamp(min=0).long()), n_accept, anchor, status
 
     def shorten(self, slot, first, last):
