@@ -129,6 +129,15 @@ __device__ __forceinline__ void stage(const int8_t *p, long ld, int row0, int ro
 // Waits until at most N of this wave's loads are on their way (s_waitcnt vmcnt(N), the others at their maxima).
 template <int N> __device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | (N >> 4) << 14); }
 
+// Between a wave's writes to LDS and its other lanes' reads of them, and back.  The hardware takes a wave's LDS
+// operations in order; this keeps the compiler, which sees a lane by itself, to it, and costs no instruction.
+__device__ __forceinline__ void wave_exchange()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
 template <bool FIRST, typename A, typename B> struct Either { typedef A type; };
 template <typename A, typename B> struct Either<false, A, B> { typedef B type; };
 
@@ -240,7 +249,7 @@ __global__ void __launch_bounds__(BM / (32 * TM) * (BN / (32 * TN)) * 64) bdgdn_
                         else to = to_e<Y>(fmaf((float)acc[i][j][4 * q + e], as[e] * ws[j], bias[j]));
                     }
             }
-        // (a wave reads what it wrote itself: its LDS operations are in order)
+        wave_exchange();
 #pragma unroll
         for (int it = 0; it < GROUP * 32 * PIECES / 64; ++it) {
             const int r = it * (64 / PIECES) + lane / PIECES, c = (lane % PIECES) * UNIT;
@@ -258,6 +267,7 @@ __global__ void __launch_bounds__(BM / (32 * TM) * (BN / (32 * TN)) * 64) bdgdn_
                     if (n + e < a.n) to[e] = v[e];
             }
         }
+        wave_exchange();   // (the next tiles take the same room)
     }
 }
 
