@@ -13,6 +13,9 @@ constexpr int64_t kFarthest = 1ll << 44;   // elements: strides and their produc
 
 bool aligned(const void *p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
+// Arrays of 32-bit numbers (NULL is aligned).
+template <typename... P> bool words(const P *...p) { return (aligned(p, 4) && ...); }
+
 int size_of(int dtype) { return dtype == BDGDN_BF16 ? 2 : 4; }
 
 bool type_ok(int dtype) { return dtype == BDGDN_BF16 || dtype == BDGDN_F32; }
@@ -219,7 +222,8 @@ int bdgdn_rope(const bdgdn_rope_desc_t *desc, const void *q, const void *k, cons
     if (!q || !q_out || !turns || with_k != (k != nullptr) || with_k != (k_out != nullptr)) return BDGDN_ERR_INVALID_ARG;
     if (seq_len && (desc->n_slots <= 0 || (!slot && desc->num_req > desc->n_slots))) return BDGDN_ERR_INVALID_ARG;
     const size_t size = size_of(desc->dtype);
-    if (!aligned(q, size) || !aligned(k, size) || !aligned(q_out, size) || !aligned(k_out, size) || !aligned(turns, 8))
+    if (!aligned(q, size) || !aligned(k, size) || !aligned(q_out, size) || !aligned(k_out, size) || !aligned(turns, 8) ||
+        !words(pos, seq_len, slot, count))
         return BDGDN_ERR_INVALID_ARG;
     if ((q == q_out && !same(desc, desc->h_q, desc->q, desc->q_out)) || (with_k && k == k_out && !same(desc, desc->h_k, desc->k, desc->k_out)))
         return BDGDN_ERR_INVALID_ARG;
@@ -322,7 +326,7 @@ int bdgdn_logits(const bdgdn_logits_desc_t *desc, const void *logits, const int3
     if (history && (desc->n_slots <= 0 || (!slot && desc->num_req > desc->n_slots))) return BDGDN_ERR_INVALID_ARG;
     if (history && desc->n_slots > 1 && desc->history_stride < desc->vocab) return BDGDN_ERR_INVALID_ARG;
     if (!aligned(logits, size_of(desc->dtype)) || !aligned(out, size_of(desc->out_dtype)) || !aligned(mask, 8) ||
-        !aligned(history, 4) || !aligned(allow, 4))
+        !words(history, allow, slot, token, count, repetition, presence, frequency, bias_token, bias))
         return BDGDN_ERR_INVALID_ARG;
     if (logits == out && (desc->dtype != desc->out_dtype || (desc->num_req > 1 && desc->req_stride != desc->out_req_stride) ||
                           (desc->nodes > 1 && desc->row_stride != desc->out_row_stride)))
@@ -346,7 +350,7 @@ int bdgdn_history_add(int32_t num_req, int32_t nodes, int32_t vocab, int32_t n_s
     if (num_req < 0 || nodes < 0 || vocab <= 0 || n_slots <= 0 || !stride_ok(history_stride)) return BDGDN_ERR_INVALID_ARG;
     if ((n_slots > 1 && history_stride < vocab) || (prompt != 0 && prompt != 1)) return BDGDN_ERR_INVALID_ARG;
     if (num_req == 0 || nodes == 0) return BDGDN_OK;
-    if (!history || !token || !aligned(history, 4) || (!slot && num_req > n_slots)) return BDGDN_ERR_INVALID_ARG;
+    if (!history || !token || !words(history, slot, token, path, count) || (!slot && num_req > n_slots)) return BDGDN_ERR_INVALID_ARG;
     return status_of(launch_history_add(num_req, nodes, vocab, n_slots, history_stride, history, slot, token, path, count,
                                         prompt, static_cast<hipStream_t>(stream)));
 }
