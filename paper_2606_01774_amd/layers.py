@@ -95,14 +95,15 @@ def bind(lib):
 
 
 # ------------------------------------------------------------------ marshalling
-def _here(stream, names, *tensors):
-    """The tensors are on the device that the call runs on; its raw stream.  (A small call costs what its
-    marshalling does: what is usual is one comparison a tensor.)"""
+def _here(stream, names, *tensors, need=1):
+    """The tensors are on the device that the call runs on, the first `need` of them given; its raw stream.  (A
+    small call costs what its marshalling does: what is usual is one comparison a tensor.)"""
     at = _current_device()
     if stream is not None and stream.device_index != at:
         raise ValueError(f"the stream is on device {stream.device_index}, the call runs on device {at}")
-    if tensors[0] is None:
-        raise ValueError(f"{names.split()[0]} must be a device tensor")
+    for i in range(need):
+        if tensors[i] is None:
+            raise ValueError(f"{names.split()[i]} must be a device tensor")
     for t in tensors:
         if t is not None and not (isinstance(t, _Tensor) and t.is_cuda and t.get_device() == at):
             name = names.split()[[i for i, u in enumerate(tensors) if u is t][0]]
@@ -175,7 +176,7 @@ def bdgdn_rope(q, turns, k=None, *, pos=None, seq_len=None, slot=None, count=Non
     out.  Returns q_out, or (q_out, k_out)."""
     lib = load_library()
     here = _here(stream, "q turns k pos seq_len slot count q_out k_out",
-                 q, turns, k, pos, seq_len, slot, count, q_out, k_out)
+                 q, turns, k, pos, seq_len, slot, count, q_out, k_out, need=2)
     dt, shape = q.dtype, q.shape
     if k is None and k_out is not None:
         raise ValueError("k_out without k")
@@ -384,7 +385,7 @@ def bdgdn_history_add(history, token, *, slot=None, path=None, count=None, promp
     (BDGDN_HISTORY_PROMPT)."""
     lib = load_library()
     here = _here(stream, "history token slot path count",
-                 history, token, slot, path, count)
+                 history, token, slot, path, count, need=2)
     if history.dim() != 2 or history.dtype is not _I32 or (history.shape[1] > 1 and history.stride(1) != 1):
         raise ValueError("history must be [n_slots, V] int32 with contiguous rows")
     if token.dim() != 2:
@@ -446,7 +447,7 @@ def bdgdn_quant_matmul(a, a_scale, w, w_scale, *, bias=None, out=None, out_dtype
     w_scale[j] sum_k a[i, k] w[j, k] + bias[j], exact in its integer sums."""
     lib = load_library()
     here = _here(stream, "a a_scale w w_scale bias out workspace",
-                 a, a_scale, w, w_scale, bias, out, workspace)
+                 a, a_scale, w, w_scale, bias, out, workspace, need=4)
     if a.dtype is not _I8 or w.dtype is not _I8:
         raise ValueError(f"a and w must be {_I8}")
     if out is not None:
