@@ -5,7 +5,7 @@ import torch
 
 import paper_2606_01774_amd as bd
 from paper_2606_01774_amd import layers
-from test_layer_abi import FAKE, INV, _call_logits, _call_rope, _logits, _rope
+from test_layer_abi import FAKE, INV, WS, _call_logits, _call_rope, _logits, _rope
 
 
 @pytest.mark.parametrize("name", ["pos", "len", "slot", "count"])
@@ -25,6 +25,25 @@ def test_history_add_rejects_arrays_off_their_words(name):
     ok = dict(R=2, N=3, V=10, slots=4, stride=10, history=FAKE, slot=FAKE, token=FAKE, path=FAKE, count=FAKE, prompt=0)
     for off in (1, 2, 3):
         assert bd.load_library().bdgdn_history_add(*dict(ok, **{name: FAKE + off}).values(), None) == INV, off
+
+
+@pytest.mark.parametrize("m,n,k", [(70, 40, 130944), (200, 150, 16384), (70, 75, 16384), (130, 129, 8192)])
+def test_quant_matmul_asks_for_the_workspace_of_its_parts(m, n, k):
+    desc = layers.QuantMatmulDesc(m, n, k, bd.BDGDN_F32, k, k, n)
+    need = bd.bdgdn_quant_matmul_workspace(desc)
+    assert need > 0 and need % (m * n * 4) == 0      # whole sums, at least two of them
+    assert need >= 2 * m * n * 4
+
+    def call(ws, size):
+        return bd.load_library().bdgdn_quant_matmul(desc, FAKE, FAKE, FAKE, FAKE, None, FAKE, ws, size, None)
+
+    assert call(FAKE, need - 1) == WS and call(FAKE, 0) == WS and call(None, need) == WS and call(None, 1 << 40) == WS
+    assert call(FAKE + 128, need) == INV
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 512, 2048), (16, 40, 130944), (64, 512, 2048), (500, 512, 2048), (4096, 4096, 1024), (0, 40, 130944)])
+def test_quant_matmul_needs_no_workspace_for_one_part(m, n, k):
+    assert bd.bdgdn_quant_matmul_workspace(layers.QuantMatmulDesc(m, n, k, bd.BDGDN_F32, k, k, n)) == 0
 
 
 # ------------------------------------------------------------------ the binding
