@@ -208,8 +208,8 @@ class Decoder:
 
     def round(self, anchor, slot, drafts=7, temperature=1.0):
         """One round with a drafted chain.  Returns (tokens [R, 1 + drafts] of the block,
-        n_accept, the next anchor, status); the last anchor stays that of a request whose status is not
-        BDGDN_CACHE_DONE."""
+        n_accept, the next anchor, status).  A request whose status is not BDGDN_CACHE_DONE has taken in
+        nothing: it goes on with the anchor that it came with."""
         token = [anchor]
         for _ in range(drafts):
             token.append(self._draft(self.drafter[token[-1].long()], temperature).to(torch.int32))

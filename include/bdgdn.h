@@ -863,7 +863,7 @@ typedef struct {
  * N = 1).  Row n of request r holds the logits after node n.  For token t, c is how often t has
  * been generated, in the history of slot[r] or by a node that n's mask word names, and t is
  * seen where c > 0 or the prompt holds it:
- *     x = seen ? (x > 0 ? x / repetition : x repetition) : x
+ *     x = seen ? (x > 0 ? x (1 / repetition) : x repetition) : x      (1 / repetition in fp32)
  *     x = x - (c > 0 ? presence : 0) - frequency c
  *     x = x + bias,   -inf where the grammar does not allow t
  *   logits       [R][N][V] of dtype (rows contiguous)

@@ -10,13 +10,13 @@
 // in a second kernel, in order.
 //
 // Bound by memory: 16384 rows of 4096 with gate and fp32 residual 273 us, 1476 MB at 5.4 TB/s, and 4.6 for the
-// weights' sums (12.6 MB); 16384 x 16 heads of 128 with their gate 97 us, 470 MB at 4.9;
-// bf16 heads of 64 and 256 3.8.  The 512 lanes of a
+// weights' sums (12.6 MB); 16384 x 16 heads of 128 with their gate 96 us, 470 MB at 4.9;
+// bf16 heads of 64 and 256 86 us, 335 MB at 3.9, where the vector units are busy in 85 % of the cycles.  The 512 lanes of a
 // workgroup take 150 to 180 registers each, so a compute unit has one, and what keeps memory busy is
 // the next row, loaded while this one is worked on (443 us without it, in workgroups of 1024).  Twice the
 // workgroups leave twice the partial sums, and take 293 us.  Rows of 8192 take two chunks to a lane, none
-// ahead: 3.9 TB/s.  Beyond that the sums fill the registers and rows are read again from the caches,
-// with spills: 1.0 TB/s at 16384.
+// ahead: 8192 x 8192 with gate and fp32 residual 361 us, 4.1 TB/s.  Beyond that the sums fill the registers and rows are
+// read again from the caches, with spills: 4096 x 16384 1060 us, 1.4 TB/s.
 #include "norm.hpp"
 
 namespace bdgdn {

@@ -2,8 +2,8 @@
 // norm in front of the next, in one pass over the row (include/bdgdn.h, bdgdn_norm_fwd).
 //
 // Bound by memory: 16384 rows of 4096 with gate and fp32 residual 177 us, 940 MB at 5.3 TB/s (a copy of 512
-// MB: 5.4); rows of 8192 5.2, of 1024 5.2, of 4091 4.8, heads of 128 with their gate 5.2, of 64 and
-// 256 in bf16 4.2 (rows get as many lanes as they fill: 16 and 64 lanes to them take 1.7 times as long).  One row of 4096 3.5 us,
+// MB: 5.4); rows of 8192 5.2, of 1024 5.2, of 4091 4.8, heads of 128 with their gate 5.2, of 100 2.8 (16384 x 16 of
+// them in fp32 74 us: the last 4 elements of each go one at a time), of 64 and 256 in bf16 4.2 (rows get as many lanes as they fill: 16 and 64 lanes to them take 1.7 times as long).  One row of 4096 3.5 us,
 // of which a launch is two.  Without a bound on registers: one that lets six waves share a SIMD keeps loads
 // from overlapping (rows of 1024: 94 us without, 170 with).
 #include "norm.hpp"

@@ -2,11 +2,13 @@
 // (include/bdgdn.h, bdgdn_quant_rows, bdgdn_quant_matmul): sums of products are 32-bit integers from
 // the matrix cores, exact in any order, and the scales meet them on the way out.
 //
-// 8191 x 8192 x 4096: rows quantised in 23 us (101 MB at 4.4 TB/s), the product in 260, 2.1 POP/s (a
-// library's product of 8192 x 8192 x 4096 8-bit integers, without scales: 1.9; the matrix cores' bound is 5).
-// At that bound a wave's 128 x 64 outputs take 96 bytes of LDS reads a clock and unit of the 128 there are, beside
-// the 32 that come in.  512 x 6144 x 2048: 3 and 14.5 us, 0.9 POP/s, 192 tiles for 256 compute units.
-// 3 x 8192 x 4096: 2.6 and 10.4 us, 34 MB of weights at 3.2 TB/s, of which the launch and the first loads
+// 8191 x 8192 x 4096: rows quantised in 23 to 25 us (101 MB at 4.2 TB/s; the vector units are always busy), the
+// product in 264 to 276, 2.0 POP/s (a library's product of 8192 x 8192 x 4096 8-bit integers, without scales: 1.9;
+// the matrix cores' bound is 5).  The matrix cores are busy in 52 % of the cycles, LDS in 41 %, and a wave spends
+// 39 % of its time waiting for loads and at barriers (counters; 508000 cycles in 276 us are 1.85 GHz): neither of the
+// two is the bound, the wait between a step and the next is.  512 x 6144 x 2048: 3 to 4 and 14.8 us, 0.9 POP/s, 192
+// tiles for 256 compute units, matrix cores busy in 27 % of the cycles.
+// 3 x 8192 x 4096: 3 and 10.6 us, 34 MB of weights at 3.2 TB/s, of which the launch and the first loads
 // are some 4.
 #include "norm.hpp"
 

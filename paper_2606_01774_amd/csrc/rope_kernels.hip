@@ -158,7 +158,8 @@ template <typename E, bool PAIRS> hipError_t launch(RopeArgs &a, hipStream_t s)
     // 93 with all heads at once
     int heads_log = log_up(a.h);
     while (heads_log > 0 && ((long)rows << (a.item_log + heads_log - 1)) >= 4 * 524288) --heads_log;
-    // (or one to every place, where a quarter of them would have no head: 22270 rows of 18 heads of 64: 31 us, 24 with half the lanes)
+    // (or one to every place, where a quarter of them or more would have no head.  22270 rows of 18 heads of 64: 41 us, 34 with
+    // half the lanes, of 24 42 and 37.  Fewer idle ones: 28 heads of 64 43 and 40, of 128 68 and 70; 40 of 64 54 and 55)
     if (4 * a.h <= 3 << heads_log && ((long)rows << (a.item_log + heads_log - 1)) >= 524288) --heads_log;
     a.sub_log = heads_log < 8 - a.item_log ? heads_log : 8 - a.item_log;
     a.row_log = 8 - a.item_log - a.sub_log;
